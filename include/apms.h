@@ -484,7 +484,7 @@ apms_status apms_selftest_wait_report(apms_ctx* ctx, int leave_reported);
 int64_t     apms_launch_count(const apms_ctx* ctx);
 
 /* Message of the last failure on this context (ctx == NULL: of the last failed
- * apms_create, apms_ipc_open or apms_ipc_close on this thread).  Never NULL. */
+ * apms_create, apms_ipc_open, apms_ipc_close or context-less call on this thread).  Never NULL. */
 const char* apms_last_error(const apms_ctx* ctx);
 
 /* Free the context (and its workspace if it allocated one).  NULL is ignored. */
@@ -531,6 +531,97 @@ void        apms_destroy(apms_ctx* ctx);
 #define APMS_NOALLOC_MAX_TILES 16384
 apms_status apms_compress_noalloc(const float* z_dev, int64_t d, int64_t chunk,
                                   uint32_t* bits_dev, float* scales_dev, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators that a training program runs next to the step.  (The paper has no counterpart:
+ * Algorithm 1 starts from a worker's flat stochastic gradient and says nothing of how a model
+ * with many tensors arrives there.)  None takes a context; all work on the current device, enqueue their
+ * kernels on `cuda_stream` (a cudaStream_t passed as void*, NULL = the legacy default stream) and
+ * return without synchronising; the message of a failure is read with apms_last_error(NULL)
+ * on the calling thread.  Element types are apms_grad_type throughout. */
+
+/* --- the norm of many tensors, and clipping ------------------------------------------------
+ *
+ * A list of tensors (a model's gradients): `count` tensors, tensor t of numel[t] elements of types[t].
+ * With cols and row_strides (both NULL, or both of `count` entries) tensor t is numel[t] / cols[t] rows of cols[t]
+ * consecutive elements, row_strides[t] >= cols[t] elements apart; a contiguous tensor has
+ * cols[t] = row_strides[t] = numel[t].  Elements are counted row by row.  numel 0 is allowed.
+ * The list holds sizes only: the addresses are given to each call, so they may change from call to call.
+ * apms_tensors_bind gives it caller-owned device memory (>= apms_tensors_workspace_bytes, 256-byte aligned)
+ * for its tables and partial sums, on the current device; it copies the tables there and synchronises
+ * `cuda_stream`.  Required before the first call.  One list's calls share that memory: calls that may
+ * overlap on the GPU (different streams with no ordering between them) need a list each. */
+typedef struct apms_tensors apms_tensors;
+apms_status apms_tensors_create(apms_tensors** out, int count, const int64_t* numel, const apms_grad_type* types,
+                                const int64_t* cols, const int64_t* row_strides);
+size_t      apms_tensors_workspace_bytes(const apms_tensors* list);
+apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t bytes, void* cuda_stream);
+void        apms_tensors_destroy(apms_tensors* list);
+
+/* norm_dev[0] = ||g||_2 over all tensors, norms_dev[t] (NULL or `count` floats) = ||g_t||_2.  Squares are summed in
+ * binary64, in an order fixed by the list alone; the roots are rounded once to binary32.  NaN and infinities
+ * propagate.  tensors_dev: HOST array of `count` device addresses, each aligned to its element size
+ * (the address of an empty tensor is not looked at). */
+apms_status apms_grad_norm(apms_tensors* list, const void* const* tensors_dev, float* norm_dev, float* norms_dev,
+                           void* cuda_stream);
+
+/* Clipping by the global norm: with c = 1 where norm <= max_norm, else max_norm / norm (formed in binary64, rounded
+ * once to binary32), every element becomes g * c, formed in binary32 and rounded once to the output's type.  (So a
+ * NaN norm makes everything NaN, and an infinite one leaves zeros, and NaN where the infinities were.)
+ * flat_dev == NULL: in place; no two tensors of the list may share memory.  Otherwise the tensors are left alone
+ * and the results are written, in list order, to flat_dev (sum of numel elements of flat_type, 16-byte
+ * aligned): the flat gradient that the step functions take.  flat_dev may be the memory the tensors are
+ * views of only if each tensor is contiguous, of flat_type and already in its place there.
+ * max_norm >= 0; infinity gathers without clipping.  norm_dev (one float) receives the norm before clipping. */
+apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float max_norm, void* flat_dev,
+                            apms_grad_type flat_type, float* norm_dev, void* cuda_stream);
+
+/* --- root-mean-square norm at a residual junction, and its gradient -----------------------
+ *
+ * Per row of `width` elements:  h = x + residual (h = x without one),
+ *   rstd = 1 / sqrt(mean(h^2) + eps),  y = h * rstd * weight.
+ * All in binary32 from the unrounded h; every output is rounded once, from binary32.
+ * x: x_type, rows x_stride elements apart; residual: x_type or binary32, or NULL; weight: `width` elements of x_type or
+ * binary32; h: written (contiguous rows, residual_type) if there is a residual, ignored otherwise; rstd: `rows` floats,
+ * written.  y: contiguous rows, of x_type - or, where scales is not NULL, e4m3 bytes: per group of `group`
+ * consecutive elements of a row (group = 0: the whole row; 128: the last group of a row may be shorter),
+ *   a = max |y|,  scale = a / 448,  q = e4m3(y * (448 / a)), nearest even,
+ * scales: rows x ceil(width / group) floats.  A group whose a is below 2^-100 has scale 0 and q = 0; a NaN or
+ * an infinity in a group shows in its scale.  Inputs need only be aligned to their element size. */
+typedef struct {
+    int64_t rows, width;
+    const void* x;        int64_t x_stride;        apms_grad_type x_type;
+    const void* residual; int64_t residual_stride; apms_grad_type residual_type;
+    const void* weight;   apms_grad_type weight_type;
+    float       eps;
+    void*       h;
+    void*       y;
+    float*      scales;   int64_t group;
+    float*      rstd;
+} apms_rms_norm_args;
+apms_status apms_rms_norm(const apms_rms_norm_args* args, void* cuda_stream);
+
+/* Gradients of that: with xh = h * rstd and a = weight * dy,
+ *   dx = rstd * (a - xh * mean(a * xh)) + dh,   dweight = sum over rows of dy * xh,
+ * dh (NULL or rows of h_type, dh_stride apart) being the gradient that arrives on the residual stream (on the
+ * output h).  dx is the gradient of x and of the residual alike: written to dx (dy_type, contiguous rows) and, where
+ * dresidual is not NULL, to dresidual (h_type, contiguous rows) too.  h: dy_type or binary32.  dweight: `width`
+ * elements of weight_type, summed in binary32 in an order fixed by the shape alone.
+ * workspace_dev: apms_rms_norm_backward_workspace_bytes(rows, width), 16-byte aligned. */
+typedef struct {
+    int64_t rows, width;
+    const void* dy;       int64_t dy_stride;       apms_grad_type dy_type;
+    const void* h;        int64_t h_stride;        apms_grad_type h_type;
+    const void* weight;   apms_grad_type weight_type;
+    const float* rstd;
+    const void* dh;       int64_t dh_stride;
+    void*       dx;
+    void*       dresidual;
+    void*       dweight;
+    void*       workspace_dev; size_t workspace_bytes;
+} apms_rms_norm_backward_args;
+size_t      apms_rms_norm_backward_workspace_bytes(int64_t rows, int64_t width);
+apms_status apms_rms_norm_backward(const apms_rms_norm_backward_args* args, void* cuda_stream);
 
 #ifdef __cplusplus
 }

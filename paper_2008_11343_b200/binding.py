@@ -96,7 +96,36 @@ SIGNATURES = {
     "apms_last_error": (C.c_char_p, [C.c_void_p]),
     "apms_destroy": (None, [C.c_void_p]),
     "apms_compress_noalloc": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "apms_tensors_create": (C.c_int, [C.POINTER(C.c_void_p), C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "apms_tensors_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "apms_tensors_bind": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "apms_tensors_destroy": (None, [C.c_void_p]),
+    "apms_grad_norm": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "apms_clip_grads": (C.c_int, [C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
+    "apms_rms_norm": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_rms_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "apms_rms_norm_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
 }
+
+
+class RmsNormArgs(C.Structure):
+    """Mirror of the C struct apms_rms_norm_args."""
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("x_type", C.c_int),
+                ("residual", C.c_void_p), ("residual_stride", C.c_int64), ("residual_type", C.c_int),
+                ("weight", C.c_void_p), ("weight_type", C.c_int), ("eps", C.c_float),
+                ("h", C.c_void_p), ("y", C.c_void_p), ("scales", C.c_void_p), ("group", C.c_int64), ("rstd", C.c_void_p)]
+
+
+class RmsNormBackwardArgs(C.Structure):
+    """Mirror of the C struct apms_rms_norm_backward_args."""
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64),
+                ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("dy_type", C.c_int),
+                ("h", C.c_void_p), ("h_stride", C.c_int64), ("h_type", C.c_int),
+                ("weight", C.c_void_p), ("weight_type", C.c_int), ("rstd", C.c_void_p),
+                ("dh", C.c_void_p), ("dh_stride", C.c_int64),
+                ("dx", C.c_void_p), ("dresidual", C.c_void_p), ("dweight", C.c_void_p),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 _lib: Optional[C.CDLL] = None
 
@@ -423,6 +452,59 @@ def apms_compress_noalloc(z_ptr: int, d: int, chunk: int, bits_ptr: int, scales_
     st = load().apms_compress_noalloc(z_ptr, d, chunk, bits_ptr, scales_ptr, stream or None)
     if st != OK:
         raise ApmsError(st, load().apms_last_error(None).decode())
+
+
+# Operators beside the step (see operators.py for torch tensors).  Their messages are the calling thread's.
+
+def _check_thread(st):
+    if st != OK:
+        raise ApmsError(st, load().apms_last_error(None).decode())
+
+
+def apms_tensors_create(numel: Sequence[int], types: Sequence[int], cols: Optional[Sequence[int]] = None,
+                        row_strides: Optional[Sequence[int]] = None) -> int:
+    n, h = len(numel), C.c_void_p()
+    strided = None if cols is None else ((C.c_int64 * n)(*cols), (C.c_int64 * n)(*row_strides))
+    _check_thread(load().apms_tensors_create(C.byref(h), n, (C.c_int64 * n)(*numel), (C.c_int * n)(*types),
+                                             *(strided or (None, None))))
+    return h.value
+
+
+def apms_tensors_workspace_bytes(h) -> int:
+    return int(load().apms_tensors_workspace_bytes(h))
+
+
+def apms_tensors_bind(h, workspace_ptr: int, nbytes: int, stream: int):
+    _check_thread(load().apms_tensors_bind(h, workspace_ptr, nbytes, stream))
+
+
+def apms_tensors_destroy(h):
+    load().apms_tensors_destroy(h)
+
+
+def apms_grad_norm(h, tensor_ptrs, norm_ptr: int, norms_ptr: Optional[int], stream: int):
+    """tensor_ptrs: a buffer of 64-bit device addresses (ctypes array or array.array('Q')), one per tensor."""
+    _check_thread(load().apms_grad_norm(h, _address(tensor_ptrs), norm_ptr, norms_ptr, stream))
+
+
+def apms_clip_grads(h, tensor_ptrs, max_norm: float, flat_ptr: Optional[int], flat_type: int, norm_ptr: int, stream: int):
+    _check_thread(load().apms_clip_grads(h, _address(tensor_ptrs), max_norm, flat_ptr, flat_type, norm_ptr, stream))
+
+
+def _address(ptrs) -> int:
+    return ptrs.buffer_info()[0] if hasattr(ptrs, "buffer_info") else C.addressof(ptrs)
+
+
+def apms_rms_norm(args: RmsNormArgs, stream: int):
+    _check_thread(load().apms_rms_norm(C.addressof(args), stream))
+
+
+def apms_rms_norm_backward_workspace_bytes(rows: int, width: int) -> int:
+    return int(load().apms_rms_norm_backward_workspace_bytes(rows, width))
+
+
+def apms_rms_norm_backward(args: RmsNormBackwardArgs, stream: int):
+    _check_thread(load().apms_rms_norm_backward(C.addressof(args), stream))
 
 
 # --- convenience wrapper: handle + torch workspace + stream ---------------------------------

@@ -8,38 +8,60 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SRC = os.path.join(CSRC, "apms.cu")                      # the one translation unit; it includes the .cuh files
+# The translation units and what each includes: apms.cu the context and the kernels of the step, operators.cu the op_* files.
+UNITS = {"apms.cu": lambda f: not f.startswith("op"), "operators.cu": lambda f: f.startswith("op") or f == "errors.h"}
 HDR = os.path.join(ROOT, "include", "apms.h")
+BUILD = os.path.join(HERE, "_build")                     # objects of the units
 LIB = os.path.join(HERE, "libapms.so")
 LIB_CHECKED = os.path.join(HERE, "libapms_checked.so")   # the same source with -DAPMS_BOUNDS_CHECK (debugging aid)
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-fmad=false", "-prec-div=true", "-prec-sqrt=true", "-ftz=false",
-    "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
+    "-Xcompiler", "-fPIC", "-Xptxas", "-v",
     "-I", os.path.join(ROOT, "include"),
 ]
 
 
+def _sources(unit: str) -> list:
+    return [HDR] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h")) and UNITS[unit](f)]
+
+
+def _older(out: str, sources: list) -> bool:
+    return not os.path.exists(out) or os.path.getmtime(out) < max(os.path.getmtime(f) for f in sources)
+
+
 def is_stale(lib: str = LIB) -> bool:
-    if not os.path.exists(lib):
-        return True
-    sources = [HDR] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))]
-    return os.path.getmtime(lib) < max(os.path.getmtime(f) for f in sources)
+    return any(_older(lib, _sources(unit)) for unit in UNITS)
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
-    """Compile libapms.so, or with checked=True libapms_checked.so (every kernel access validated on the device)."""
+    """Compile libapms.so, or with checked=True libapms_checked.so (every access of the step's kernels validated on the
+    device).  The units are compiled side by side; without `force` only those whose sources are newer than their object."""
     lib = LIB_CHECKED if checked else LIB
     if not force and not is_stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    tmp = lib + f".tmp{os.getpid()}"
     extra = ["-DAPMS_BOUNDS_CHECK"] if checked else []
-    proc = subprocess.run([nvcc, *NVCC_FLAGS, *extra, SRC, "-o", tmp], capture_output=True, text=True)
-    if verbose or proc.returncode != 0:
-        sys.stderr.write(proc.stdout + proc.stderr)
+    pid, running, objects = os.getpid(), [], []
+    for unit in UNITS:
+        obj = os.path.join(BUILD, unit.replace(".cu", "_checked.o" if checked else ".o"))
+        objects.append(obj)
+        if force or _older(obj, _sources(unit)):
+            os.makedirs(BUILD, exist_ok=True)
+            cmd = [nvcc, *NVCC_FLAGS, *extra, "-c", os.path.join(CSRC, unit), "-o", f"{obj}.{pid}"]
+            running.append((obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    for obj, proc in running:
+        said = proc.communicate()[0]
+        if verbose or proc.returncode != 0:
+            sys.stderr.write(said)
+        if proc.returncode != 0:
+            raise RuntimeError(f"nvcc failed building {os.path.basename(obj)}")
+        os.replace(f"{obj}.{pid}", obj)
+    tmp = lib + f".tmp{pid}"
+    proc = subprocess.run([nvcc, *NVCC_FLAGS[:2], "-shared", *objects, "-o", tmp], capture_output=True, text=True)
     if proc.returncode != 0:
-        raise RuntimeError(f"nvcc failed building {os.path.basename(lib)}")
+        sys.stderr.write(proc.stdout + proc.stderr)
+        raise RuntimeError(f"nvcc failed linking {os.path.basename(lib)}")
     os.replace(tmp, lib)
     return lib
 

@@ -35,7 +35,7 @@
 #include <vector>
 
 #include "apms.h"
-
+#include "errors.h"
 
 #include "device_common.cuh"
 #include "kernels_adam.cuh"
@@ -128,10 +128,12 @@ bool make_layout(int64_t d, int n, int64_t chunk, Layout* L, size_t guard = 0, s
     return true;
 }
 
-thread_local char g_create_error[256] = "";
+thread_local char g_create_error[kThreadErrorBytes] = "";
 
 struct EventPair { cudaEvent_t a, b; };
 }  // namespace
+
+char* apms_thread_error() { return g_create_error; }
 
 struct apms_ctx {
     Layout L;

@@ -1,6 +1,6 @@
 // Constants, tunables and the small device helpers every kernel uses (loads and stores,
 // the per-element arithmetic with its roundings pinned, sign-word packing, block sums).
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

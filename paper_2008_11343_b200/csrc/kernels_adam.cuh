@@ -1,5 +1,5 @@
 // Warmup phase: the fused Adam step on the worker-averaged gradient (Section 3.2).
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

@@ -1,6 +1,6 @@
 // Momentum replacement and model update (Section 3.3 steps 5-6), the variants' update kernels,
 // and the kernels that materialise errors and momentum for state reads.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

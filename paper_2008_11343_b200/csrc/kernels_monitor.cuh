@@ -1,5 +1,5 @@
 // Error-norm monitor and the bounded-wait self-test kernel.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

@@ -1,6 +1,6 @@
 // Server side (Section 3.3 step 4): the register-staged kernel and the kernel that streams its
 // tiles through a shared-memory ring, optionally fused with the model update.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

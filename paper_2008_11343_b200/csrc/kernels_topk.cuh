@@ -1,5 +1,5 @@
 // Top-k compressor (Section 5.1, second item): worker and server kernels.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

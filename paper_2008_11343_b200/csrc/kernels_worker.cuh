@@ -1,6 +1,6 @@
 // Worker side of a compression-phase step (Section 3.3 steps 1-2): general and fine-tiled kernels,
 // and the kernels that finish the per-chunk scales.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

@@ -1,5 +1,5 @@
 // The allocation-free compressor entry point (apms_compress_noalloc) and its kernel.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 // ------------------------------------------------------------------------------------------

@@ -1,5 +1,5 @@
 // Mapping of chunks to work items for the general worker and server kernels.
-// Part of libapms.so: included by apms.cu, which is the only translation unit.
+// Part of libapms.so: included by apms.cu.
 #pragma once
 
 namespace {

@@ -1,0 +1,632 @@
+"""The operators beside the step against plain forms in binary64.
+
+Tolerances, from the rounding of one operation (u = 2^-24 in binary32; an output type with p significand bits rounds by
+u_T = 2^-p, and by half the smallest subnormal near zero):
+
+  norm       squares are exact or summed with at most 8 roundings in binary32 before binary64 takes over (8u, halved by the
+             root), and the root is rounded once: below 2^-21.
+  clip       the factor has the norm's error and its own rounding, the product one more, the output type one: 2^-20 + u_T.
+  rms norm   h is rounded once (u); a sum of n non-negative terms in any order that adds at most m of them in a row is off by
+             at most (m + log-depth) u: m <= width / 32 + 64 here; halved by the root; y has three products and u_T.
+  8 bits     spacing of e4m3: half a step is 2^-4 of the value, or 2^-10 of the scale below the smallest normal (2^-6).
+  backward   dx = rstd (a - xh mean(a xh)) + dh: errors relative to the terms, not to their difference; the mean's sum is relative
+             to the sum of magnitudes.  dweight: a sum over the rows in any order, (rows + 64) u of the sum of magnitudes.
+"""
+import itertools
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2008_11343_b200 import binding as B
+from paper_2008_11343_b200 import operators as O
+
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+ROUND = {F32: (2.0 ** -24, 2.0 ** -150), BF16: (2.0 ** -8, 2.0 ** -134), F16: (2.0 ** -11, 2.0 ** -25)}
+EPS = 1e-6
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def near(got, want, tolerance, what=""):
+    """|got - want| <= tolerance elementwise; equal where want is infinite or NaN."""
+    got, want = got.double(), want.double()
+    assert got.shape == want.shape, what
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fine), what
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    tolerance = torch.as_tensor(tolerance, dtype=torch.float64, device=got.device).expand(got.shape)
+    off = torch.where(fine, (got - want).abs() - tolerance, torch.zeros_like(got))
+    if off.numel():
+        worst = off.argmax()
+        assert off.max() <= 0, f"{what}: {got.flatten()[worst]} instead of {want.flatten()[worst]}, tolerance {tolerance.flatten()[worst]}"
+
+
+# ------------------------------------------------------------------------------------------ norm and clipping
+
+SIZES = [0, 1, 2, 3, 7, 8, 31, 4095, 4097, 8191, 8192, 8193, 16384, 16391, 100_003, 0, 5]
+
+
+def tensors_of(sizes, dtypes, seed, shift=0):
+    """Tensors `shift` elements behind a 512-byte boundary, scales over three decades."""
+    g, made = gen(seed), []
+    for k, (n, t) in enumerate(zip(sizes, itertools.cycle(dtypes))):
+        made.append(torch.empty(n + shift, dtype=t, device="cuda")[shift:].normal_(0.0, 10.0 ** (-(k % 4)), generator=g))
+    return made
+
+
+def norms64(tensors):
+    squares = torch.stack([t.double().square().sum() for t in tensors])
+    return squares.sum().sqrt(), squares.sqrt()
+
+
+def clipped64(tensors, max_norm):
+    norm = float(norms64(tensors)[0])
+    c = 1.0 if norm <= max_norm else max_norm / norm
+    return [t.double() * c for t in tensors]
+
+
+def flat_tolerance(want, dtype):
+    rel, least = ROUND[dtype]
+    return want.abs() * (2.0 ** -20 + rel) + least
+
+
+@pytest.mark.parametrize("dtypes", [(F32,), (BF16,), (F16,), (BF16, F32, F16)], ids=str)
+@pytest.mark.parametrize("shift", [0, 1, 3, 4])
+def test_norm_of_a_list(dtypes, shift):
+    ts = tensors_of(SIZES, dtypes, 1, shift)
+    norm, norms = O.TensorList(ts).grad_norm(ts)
+    want, wants = norms64(ts)
+    assert norm.dtype == norms.dtype == F32 and norm.shape == () and norms.shape == (len(ts),)
+    near(norm, want, want * 2.0 ** -21)
+    near(norms, wants, wants * 2.0 ** -21)
+
+
+@pytest.mark.parametrize("sizes", [[1], [0], [0, 0, 0], [5_000_011], [3] * 1100, [70_000] * 3 + [1] * 520 + [9000] * 7], ids=lambda s: f"{len(s)}x{s[0]}")
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_and_flat_gradient_of_short_and_long_lists(sizes, dtype):
+    ts = tensors_of(sizes, (dtype,), 2)
+    tl = O.TensorList(ts)
+    norm, norms = tl.grad_norm(ts)
+    want, wants = norms64(ts)
+    near(norm, want, want * 2.0 ** -21)
+    near(norms, wants, wants * 2.0 ** -21)
+    flat = torch.empty(tl.numel, dtype=F32, device="cuda")
+    limit = float(want) / 3
+    near(tl.clip_grads(ts, limit, out=flat), want, want * 2.0 ** -21)
+    wanted = torch.cat(clipped64(ts, limit))
+    near(flat, wanted, flat_tolerance(wanted, F32))
+
+
+@pytest.mark.parametrize("out", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("dtypes", [(F32,), (BF16,), (F16,), (BF16, F32, F16)], ids=str)
+@pytest.mark.parametrize("shift", [0, 1, 6])
+@pytest.mark.parametrize("limit", [0.5, 1e6])
+def test_clipping_into_the_flat_gradient(dtypes, out, shift, limit):
+    ts = tensors_of(SIZES, dtypes, 3, shift)
+    before = [t.clone() for t in ts]
+    tl = O.TensorList(ts)
+    room = torch.full((tl.numel + 64,), 77.0, dtype=out, device="cuda")
+    norm = tl.clip_grads(ts, limit, out=room[:tl.numel])
+    want, _ = norms64(ts)
+    near(norm, want, want * 2.0 ** -21)
+    wanted = torch.cat(clipped64(before, limit))
+    near(room[:tl.numel], wanted, flat_tolerance(wanted, out))
+    assert (room[tl.numel:] == 77.0).all() and all(torch.equal(a, b) for a, b in zip(ts, before))
+    if limit > 1e5 and all(t == out for t in dtypes):
+        assert torch.equal(room[:tl.numel], torch.cat(before))               # nothing clipped, nothing rounded
+
+
+@pytest.mark.parametrize("dtypes", [(F32,), (BF16,), (F16,), (BF16, F32, F16)], ids=str)
+@pytest.mark.parametrize("shift", [0, 1, 5])
+def test_clipping_in_place(dtypes, shift):
+    ts = tensors_of(SIZES, dtypes, 4, shift)
+    before = [t.clone() for t in ts]
+    tl = O.TensorList(ts)
+    norm = tl.clip_grads(ts, 0.25)
+    want, _ = norms64(before)
+    near(norm, want, want * 2.0 ** -21)
+    for t, w in zip(ts, clipped64(before, 0.25)):
+        near(t, w, flat_tolerance(w, t.dtype))
+    again = [t.clone() for t in ts]
+    tl.clip_grads(ts, 1e6)                                                   # below the limit: nothing changes
+    assert all(torch.equal(a, b) for a, b in zip(ts, again))
+
+
+def test_views_of_a_bucket_at_odd_offsets():
+    sizes = [5, 8193, 1, 33_333, 70_001, 16]
+    bucket = torch.empty(sum(sizes) + 1, dtype=BF16, device="cuda").normal_(generator=gen(5))
+    ts, at = [], 1
+    for n in sizes:
+        ts.append(bucket[at:at + n])
+        at += n
+    tl = O.TensorList(ts)
+    for out in (F32, BF16):
+        flat = torch.empty(tl.numel, dtype=out, device="cuda")
+        tl.clip_grads(ts, 3.0, out=flat)
+        wanted = torch.cat(clipped64(ts, 3.0))
+        near(flat, wanted, flat_tolerance(wanted, out))
+    before, edge = [t.clone() for t in ts], bucket[0].clone()
+    tl.clip_grads(ts, 3.0)
+    for t, w in zip(ts, clipped64(before, 3.0)):
+        near(t, w, flat_tolerance(w, BF16))
+    assert torch.equal(bucket[0], edge)
+
+
+def test_a_flat_gradient_that_the_tensors_are_views_of():
+    flat = torch.empty(50_000, device="cuda").normal_(generator=gen(6))
+    ts = [flat[:20_001], flat[20_001:20_001], flat[20_001:]]
+    tl, before = O.TensorList(ts), flat.clone()
+    tl.clip_grads(ts, 1.0, out=flat)
+    want = clipped64([before], 1.0)[0]
+    near(flat, want, flat_tolerance(want, F32))
+    swapped = [ts[2], ts[1], ts[0]]
+    with pytest.raises(B.ApmsError, match="overlaps the flat gradient"):
+        O.TensorList(swapped).clip_grads(swapped, 1.0, out=flat)
+    with pytest.raises(B.ApmsError, match="overlap in memory"):
+        twice = [flat[:100], flat[50:150]]
+        O.TensorList(twice).clip_grads(twice, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+def test_column_slices_of_one_matrix(dtype):
+    m = torch.empty(301, 1000, dtype=dtype, device="cuda").normal_(generator=gen(7))
+    deep = torch.empty(7, 3, 96, dtype=dtype, device="cuda").normal_(generator=gen(8))
+    ts = [m[:, :333], m[:, 333:340], m[:, 340:1000], deep[:, :, 5:70], torch.ones(3, dtype=dtype, device="cuda"), m[:, :0]]
+    before = [t.clone() for t in ts]
+    tl = O.TensorList(ts)
+    norm, norms = tl.grad_norm(ts)
+    want, wants = norms64(before)
+    near(norm, want, want * 2.0 ** -21)
+    near(norms, wants, wants * 2.0 ** -21)
+    flat = torch.empty(tl.numel, dtype=F32, device="cuda")
+    tl.clip_grads(ts, 1.0, out=flat)
+    wanted = torch.cat([w.flatten() for w in clipped64(before, 1.0)])
+    near(flat, wanted, flat_tolerance(wanted, F32))
+    rest = deep[:, :, 70:].clone()
+    tl.clip_grads(ts, 1.0)
+    for t, w in zip(ts, clipped64(before, 1.0)):
+        near(t, w, flat_tolerance(w, dtype))
+    assert torch.equal(deep[:, :, 70:], rest)
+
+
+def test_values_whose_squares_leave_binary32():
+    for scale in (1e-30, 1e30):
+        for dtype in (F32, BF16):
+            ts = [(torch.ones(n, device="cuda") * scale).to(dtype) for n in (1, 5000, 40_000)]
+            norm, norms = O.TensorList(ts).grad_norm(ts)
+            want, wants = norms64(ts)
+            near(norm, want, want * 2.0 ** -21)
+            near(norms, wants, wants * 2.0 ** -21)
+    mixed = [torch.tensor([1e-25, 0.0, -3e-25], device="cuda").to(BF16), torch.zeros(4096, dtype=BF16, device="cuda")]
+    norm, norms = O.TensorList(mixed).grad_norm(mixed)
+    near(norms, norms64(mixed)[1], norms64(mixed)[1] * 2.0 ** -21)
+    half = [torch.full((3000,), 65504.0, dtype=F16, device="cuda"), torch.full((3000,), 2.0 ** -24, dtype=F16, device="cuda")]
+    norm, norms = O.TensorList(half).grad_norm(half)
+    near(norms, norms64(half)[1], norms64(half)[1] * 2.0 ** -21)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_infinities_and_nan(dtype, bad):
+    ts = tensors_of([1000, 20_000, 64], (dtype,), 9)
+    ts[1][19_999] = bad
+    tl = O.TensorList(ts)
+    norm, norms = tl.grad_norm(ts)
+    want, wants = norms64(ts)
+    near(norm, want, 0.0)
+    near(norms, wants, torch.where(torch.isfinite(wants), wants, torch.zeros_like(wants)) * 2.0 ** -21)
+    flat = torch.empty(tl.numel, dtype=dtype, device="cuda")
+    tl.clip_grads(ts, 1.0, out=flat)
+    if bad != bad:
+        assert torch.isnan(flat).all()
+    else:
+        assert torch.isnan(flat[20_999]) and torch.isnan(flat).sum() == 1 and (flat.nan_to_num() == 0).all()
+    tl.clip_grads(ts, float("inf"), out=flat)                                 # gathers what is there
+    assert torch.equal(flat.nan_to_num(5.0, 6.0, 7.0), torch.cat(ts).nan_to_num(5.0, 6.0, 7.0))
+
+
+def test_a_limit_of_zero_and_gradients_of_zero():
+    ts = [torch.zeros(9000, device="cuda"), torch.zeros(3, device="cuda")]
+    tl = O.TensorList(ts)
+    flat = torch.full((9003,), 5.0, device="cuda")
+    assert float(tl.clip_grads(ts, 0.0, out=flat)) == 0.0 and (flat == 0).all()
+    ts[1].fill_(2.0)
+    assert abs(float(tl.clip_grads(ts, 0.0, out=flat)) - 12 ** 0.5) < 1e-6 and (flat == 0).all()
+
+
+def test_the_same_list_again_on_other_tensors_streams_and_in_a_graph():
+    ts = tensors_of([70_000, 33, 9000], (BF16, F32), 10)
+    tl = O.TensorList(ts)
+    flat = torch.empty(tl.numel, device="cuda")
+    first = float(tl.clip_grads(ts, 1.0, out=flat))
+    kept = flat.clone()
+    for _ in range(20):                                                       # bit for bit, whatever ran in between
+        assert float(tl.clip_grads(ts, 1.0, out=flat)) == first and torch.equal(flat, kept)
+    others = [t * 2 for t in ts]
+    assert abs(float(tl.grad_norm(others)[0]) / first - 2.0) < 1e-6
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        flat2 = torch.empty_like(flat)
+        norm2 = tl.clip_grads(ts, 1.0, out=flat2)
+    norm3 = tl.clip_grads(ts, 1.0, out=flat)
+    torch.cuda.synchronize()
+    assert float(norm2) == float(norm3) == first and torch.equal(flat, kept) and torch.equal(flat2, kept)
+    graph = torch.cuda.CUDAGraph()
+    flat.zero_()
+    with torch.cuda.stream(side):
+        tl.clip_grads(ts, 1.0, out=flat)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        norm = tl.clip_grads(ts, 1.0, out=flat)
+    for t in ts:
+        t.mul_(4)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert abs(float(norm) / first - 4.0) < 1e-6
+    near(flat, kept.double(), kept.double().abs() * 2.0 ** -18)
+
+
+def test_a_list_refuses_other_tensors():
+    ts = tensors_of([100, 64], (F32,), 11)
+    tl = O.TensorList(ts)
+    for other in ([ts[0]], [ts[1], ts[0]], [ts[0], ts[1].bfloat16()], [ts[0], ts[1].cpu()], [ts[0], torch.ones(128, device="cuda")[::2]]):
+        with pytest.raises(ValueError):
+            tl.grad_norm(other)
+    for out in (torch.empty(163, device="cuda"), torch.empty(164), torch.empty(328, device="cuda")[::2], torch.empty(164, dtype=torch.int32, device="cuda")):
+        with pytest.raises(ValueError):
+            tl.clip_grads(ts, 1.0, out=out)
+    with pytest.raises(B.ApmsError, match="16-byte aligned"):
+        tl.clip_grads(ts, 1.0, out=torch.empty(165, device="cuda")[1:])
+    for limit in (-1.0, float("nan")):
+        with pytest.raises(B.ApmsError, match="max_norm"):
+            tl.clip_grads(ts, limit)
+    with pytest.raises(ValueError, match="float32, bfloat16 or float16"):
+        O.TensorList([torch.ones(3, dtype=torch.int32, device="cuda")])
+    m = torch.ones(8, 9, device="cuda")
+    sliced = O.TensorList([m[:, :4]])
+    with pytest.raises(ValueError, match="strides"):
+        sliced.grad_norm([torch.ones(8, 4, device="cuda")])
+
+
+# ------------------------------------------------------------------------------------------ RMS norm
+
+KINDS = [(F32, F32, F32), (BF16, BF16, BF16), (BF16, F32, F32), (BF16, None, F32), (F16, F16, F16), (F16, F32, F16), (F16, None, F16), (F32, None, F32)]
+WIDTHS = [1, 2, 3, 7, 8, 64, 100, 127, 128, 129, 256, 384, 768, 1000, 1001, 1024, 2048, 2056, 4096, 5000, 8192, 12_288, 16_384, 16_392, 20_001, 32_768, 40_000]
+
+
+def activation(rows, width, dtype, seed, pad=0, shift=0, scale=1.0):
+    g = gen(seed)
+    m = torch.empty(rows * (width + pad) + shift, dtype=dtype, device="cuda").normal_(0.0, scale, generator=g)
+    return m[shift:].view(rows, width + pad)[:, :width]
+
+
+def weight_of(width, dtype, seed):
+    return (1.0 + 0.2 * torch.empty(width, device="cuda").normal_(generator=gen(seed))).to(dtype)
+
+
+def chain(width):
+    return (width / 32 + 64) * U
+
+
+def forward64(x, w, r):
+    h = x.double() if r is None else x.double() + r.double()
+    rstd = 1.0 / (h.square().mean(-1, keepdim=True) + EPS).sqrt()
+    return h, rstd[..., 0], h * rstd * w.double()
+
+
+def check_forward(x, w, r, got):
+    y, h, rstd = got
+    h64, rstd64, y64 = forward64(x, w, r)
+    width = x.shape[-1]
+    rstd_tol = chain(width) / 2 + 4 * U
+    assert y.dtype == x.dtype and rstd.dtype == F32 and y.shape == x.shape and rstd.shape == x.shape[:-1]
+    near(rstd, rstd64, rstd64 * rstd_tol, "rstd")
+    if r is None:
+        assert h is x
+    else:
+        rel, least = ROUND[r.dtype]
+        near(h, h64, h64.abs() * rel + (x.double().abs() + r.double().abs()) * U + least, "h")
+    rel, least = ROUND[x.dtype]
+    small = (x.double().abs() + (0 if r is None else r.double().abs())) * U * rstd64[..., None] * w.double().abs()
+    near(y, y64, y64.abs() * (rstd_tol + 4 * U + rel) + small + least, "y")
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_norm_at_a_junction(kind, width):
+    dt, rt, wt = kind
+    for rows in (1, 3, 37):
+        x = activation(rows, width, dt, 1)
+        r = None if rt is None else activation(rows, width, rt, 2, scale=3.0)
+        w = weight_of(width, wt, 3)
+        check_forward(x, w, r, O.rms_norm_forward(x, w, r, eps=EPS))
+
+
+@pytest.mark.parametrize("kind", KINDS[:4], ids=str)
+@pytest.mark.parametrize("width,pad,shift", [(768, 8, 0), (768, 0, 8), (768, 3, 0), (768, 0, 1), (1001, 7, 0), (4096, 4096, 0), (4096, 1, 5), (64, 40, 4), (20_000, 16, 3)])
+def test_norm_of_slices_and_shifted_rows(kind, width, pad, shift):
+    dt, rt, wt = kind
+    x = activation(29, width, dt, 4, pad, shift)
+    r = None if rt is None else activation(29, width, rt, 5, pad=2 * pad)
+    w = weight_of(width + 1, wt, 6)[1:]                                      # not on a 16-byte boundary either
+    check_forward(x, w, r, O.rms_norm_forward(x, w, r, eps=EPS))
+
+
+def test_many_rows_more_dimensions_and_orders():
+    x = activation(70_001, 64, BF16, 7)
+    w = weight_of(64, BF16, 8)
+    check_forward(x, w, x, O.rms_norm_forward(x, w, x, eps=EPS))
+    x = activation(24, 256, F32, 9).view(2, 3, 4, 256)
+    check_forward(x, weight_of(256, F32, 8), x, O.rms_norm_forward(x, weight_of(256, F32, 8), x, eps=EPS))
+    turned = x.transpose(0, 2)
+    check_forward(turned, weight_of(256, F32, 8), turned, O.rms_norm_forward(turned, weight_of(256, F32, 8), turned, eps=EPS))
+    for shape in ((0, 64), (2, 0, 64)):
+        none = torch.empty(shape, device="cuda")
+        y, h, rstd = O.rms_norm_forward(none, weight_of(64, F32, 8), none)
+        assert y.shape == h.shape == shape and rstd.shape == shape[:-1]
+        q, scales, _, _ = O.rms_norm_fp8(none, weight_of(64, F32, 8))
+        assert q.shape == shape and scales.shape == shape[:-1] + (1,)
+
+
+def check_fp8(x, w, r, group, got):
+    q, scales, h, rstd = got
+    h64, rstd64, y64 = forward64(x, w, r)
+    width = x.shape[-1]
+    size = group or width
+    groups = -(-width // size)
+    assert q.dtype == torch.float8_e4m3fn and q.shape == x.shape and scales.shape == x.shape[:-1] + (groups,)
+    tol = chain(width) / 2 + 8 * U
+    small = (x.double().abs() + (0 if r is None else r.double().abs())) * U * rstd64[..., None] * w.double().abs()
+    parts, offs = y64.abs().split(size, -1), small.split(size, -1)
+    want = torch.stack([p.amax(-1) for p in parts], -1) / 448.0
+    slack = torch.stack([p.amax(-1) for p in offs], -1) / 448.0
+    near(scales, want, want * tol + slack, "scales")
+    near(rstd, rstd64, rstd64 * tol, "rstd")
+    each = scales.double().repeat_interleave(size, -1)[..., :width]
+    near(q.double() * each, y64, y64.abs() * (2.0 ** -4 + tol) + each * 2.0 ** -10 * (1 + tol) + small * 1.1, "q")
+    if r is not None:
+        rel, least = ROUND[r.dtype]
+        near(h, h64, h64.abs() * rel + (x.double().abs() + r.double().abs()) * U + least, "h")
+
+
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_eight_bit_output(kind, width, group):
+    dt, rt, wt = kind
+    for rows in (1, 5):
+        x = activation(rows, width, dt, 11)
+        r = None if rt is None else activation(rows, width, rt, 12)
+        w = weight_of(width, wt, 13)
+        check_fp8(x, w, r, group, O.rms_norm_fp8(x, w, r, eps=EPS, group=group))
+
+
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("width,pad,shift", [(768, 8, 0), (768, 3, 0), (768, 0, 1), (1000, 0, 3), (5000, 24, 0)])
+def test_eight_bit_output_of_slices(width, pad, shift, group):
+    x = activation(19, width, BF16, 14, pad, shift)
+    r = activation(19, width, BF16, 15, pad=pad)
+    w = weight_of(width, BF16, 16)
+    check_fp8(x, w, r, group, O.rms_norm_fp8(x, w, r, eps=EPS, group=group))
+
+
+@pytest.mark.parametrize("group", [0, 128])
+def test_eight_bit_groups_of_zeros_and_of_tiny_values(group):
+    x = activation(4, 384, F32, 17)
+    w = weight_of(384, F32, 18)
+    x[1] = 0.0
+    x[2, 128:256] = 0.0
+    w[256:] *= 1e-35                                                         # y below 2^-100 there: counts as zero
+    q, scales, _, rstd = O.rms_norm_fp8(x, w, eps=EPS, group=group)
+    assert (q[1].float() == 0).all() and (scales[1] == 0).all() and abs(float(rstd[1]) * EPS ** 0.5 - 1) < 1e-6
+    assert (q[2, 128:256].float() == 0).all()
+    if group:
+        assert scales[2, 1] == 0 and (scales[:, 2] == 0).all() and (q[:, 256:].float() == 0).all() and (scales[0, :2] > 0).all()
+    assert torch.isfinite(scales).all() and torch.isfinite(q.float()).all()
+
+
+@pytest.mark.parametrize("width", [129, 1024, 4096, 40_000])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_bad_row_stays_in_its_row(width, bad):
+    x = activation(9, width, BF16, 19)
+    w = weight_of(width, BF16, 20)
+    good = O.rms_norm_forward(x, w, x)
+    good8 = O.rms_norm_fp8(x, w, x)
+    x2 = x.clone()
+    x2[4, width // 2] = bad
+    y, h, rstd = O.rms_norm_forward(x2, w, x2)
+    q, scales, _, _ = O.rms_norm_fp8(x2, w, x2)
+    rest = [k for k in range(9) if k != 4]
+    assert torch.equal(y[rest], good[0][rest]) and torch.equal(rstd[rest], good[2][rest]) and torch.equal(scales[rest], good8[1][rest])
+    assert torch.equal(q[rest].view(torch.uint8), good8[0][rest].view(torch.uint8))
+    assert torch.isnan(y[4, width // 2]) and not torch.isfinite(scales[4, 0])
+    if bad != bad:
+        assert torch.isnan(y[4]).all() and torch.isnan(rstd[4])
+    else:
+        assert rstd[4] == 0
+
+
+def test_large_and_small_activations():
+    for scale in (1e-20, 1e-3, 1e4, 1e15):
+        x = activation(5, 1024, F32, 21, scale=scale)
+        w = weight_of(1024, F32, 22)
+        h = x.double()
+        rstd64 = 1.0 / (h.square().mean(-1) + EPS).sqrt()
+        y, _, rstd = O.rms_norm_forward(x, w, eps=EPS)
+        near(rstd, rstd64, rstd64 * (chain(1024) / 2 + 4 * U))
+        want = h * rstd64[:, None] * w.double()
+        near(y, want, want.abs() * (chain(1024) + 8 * U) + 2.0 ** -149)
+
+
+# ------------------------------------------------------------------------------------------ backward
+
+def backward64(dy, h, w, rstd, dh):
+    dy, h, w, rstd = dy.double(), h.double(), w.double(), rstd.double()[:, None]
+    xh = h * rstd
+    a = dy * w
+    mean = (a * xh).mean(-1, keepdim=True)
+    spread = (a * xh).abs().mean(-1, keepdim=True)
+    inner = rstd * (a - xh * mean)
+    dx = inner if dh is None else inner + dh.double()
+    n = h.shape[-1]
+    tol = rstd * (a.abs() * 4 * U + (xh * mean).abs() * 6 * U + xh.abs() * spread * (chain(n) + 6 * U)) + (inner.abs() + dx.abs()) * 2 * U
+    return dx, tol, (dy * xh).sum(0), (dy * xh).abs().sum(0)
+
+
+def check_backward(dy, h, w, rstd, dh, got):
+    dx64, tol, dw64, dw_spread = backward64(dy, h, w, rstd, dh)
+    dx, dw, *dr = got
+    rel, least = ROUND[dy.dtype]
+    assert dx.dtype == dy.dtype and dw.dtype == w.dtype and len(dr) == (h.dtype != dy.dtype)
+    near(dx, dx64, tol + dx64.abs() * rel + least, "dx")
+    if dr:
+        near(dr[0], dx64, tol + dx64.abs() * U, "dresidual")
+    rel, least = ROUND[w.dtype]
+    near(dw, dw64, dw_spread * (dy.shape[0] + 64) * U + dw64.abs() * rel + least, "dweight")
+
+
+@pytest.mark.parametrize("kind", [(F32, F32, F32), (BF16, BF16, BF16), (BF16, F32, F32), (F16, F16, F32), (F16, F32, F16), (BF16, BF16, F32)], ids=str)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_gradients(kind, width):
+    dt, ht, wt = kind
+    for rows, carried in ((1, True), (5, False), (151, True)):
+        dy = activation(rows, width, dt, 31, scale=0.1)
+        h = activation(rows, width, ht, 32, scale=2.0)
+        dh = activation(rows, width, ht, 33, scale=0.1) if carried else None
+        w = weight_of(width, wt, 34)
+        rstd = (1.0 / (h.double().square().mean(-1) + EPS).sqrt()).float()
+        check_backward(dy, h, w, rstd, dh, O.rms_norm_backward(dy, h, w, rstd, dh))
+
+
+@pytest.mark.parametrize("kind", [(F32, F32, F32), (BF16, BF16, BF16), (BF16, F32, F32)], ids=str)
+@pytest.mark.parametrize("width,pad,shift", [(768, 8, 0), (768, 3, 0), (768, 0, 1), (1001, 7, 0), (4096, 4096, 0), (64, 40, 4), (20_000, 16, 3)])
+def test_gradients_of_slices(kind, width, pad, shift):
+    dt, ht, wt = kind
+    dy = activation(43, width, dt, 35, pad, shift, scale=0.1)
+    h = activation(43, width, ht, 36, pad=2 * pad)
+    dh = activation(43, width, ht, 37, pad=pad, scale=0.1)
+    w = weight_of(width + 1, wt, 38)[1:]
+    rstd = (1.0 / (h.double().square().mean(-1) + EPS).sqrt()).float()
+    check_backward(dy, h, w, rstd, dh, O.rms_norm_backward(dy, h, w, rstd, dh))
+
+
+@pytest.mark.parametrize("rows,width", [(0, 64), (40_003, 64), (3000, 1024), (2049, 4096)])
+def test_gradients_of_few_and_many_rows(rows, width):
+    dy = activation(rows, width, BF16, 39, scale=0.1)
+    h = activation(rows, width, BF16, 40)
+    w = weight_of(width, BF16, 41)
+    rstd = (1.0 / (h.double().square().mean(-1) + EPS).sqrt()).float()
+    got = O.rms_norm_backward(dy, h, w, rstd, dy)
+    check_backward(dy, h, w, rstd, dy, got)
+    for _ in range(5):                                                        # the same bits every time
+        again = O.rms_norm_backward(dy, h, w, rstd, dy)
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_gradient_against_differences():
+    """Central differences of the binary64 form, step 1e-5: their own error is about step^2 and 2^-52 / step, 1e-9 of the values here."""
+    rows, width = 3, 40
+    x, r, w = (activation(rows, width, F32, 51), activation(rows, width, F32, 52), weight_of(width, F32, 53))
+    cy, ch = activation(rows, width, F32, 54).double(), activation(rows, width, F32, 55).double()
+
+    def loss(x64, r64, w64):
+        h = x64 + r64
+        return float((h / (h.square().mean(-1, keepdim=True) + EPS).sqrt() * w64 * cy).sum() + (h * ch).sum())
+
+    leaves = [t.clone().requires_grad_() for t in (x, r, w)]
+    y, h = O.rms_norm(leaves[0], leaves[2], leaves[1], eps=EPS)
+    ((y * cy.float()).sum() + (h * ch.float()).sum()).backward()
+    base = [t.double() for t in (x, r, w)]
+    for which, leaf in enumerate(leaves):
+        for k in range(0, leaf.numel(), 7):
+            ends = []
+            for sign in (1, -1):
+                moved = [t.clone() for t in base]
+                moved[which].view(-1)[k] += sign * 1e-5
+                ends.append(loss(*moved))
+            want = (ends[0] - ends[1]) / 2e-5
+            assert abs(float(leaf.grad.view(-1)[k]) - want) < 2e-5 * max(1.0, abs(want))
+
+
+@pytest.mark.parametrize("rt", [None, F32, BF16], ids=str)
+def test_gradients_through_autograd(rt):
+    x = activation(64, 768, BF16, 61).requires_grad_()
+    r = None if rt is None else activation(64, 768, rt, 62).requires_grad_()
+    w = weight_of(768, F32, 63).requires_grad_()
+    cy = activation(64, 768, BF16, 64, scale=0.1)
+    ch = activation(64, 768, rt or BF16, 65, scale=0.1)
+    out = O.rms_norm(x, w, r, eps=EPS)
+    y, h = out if rt else (out, None)
+    torch.autograd.backward([y] + ([h] if rt else []), [cy] + ([ch] if rt else []))
+    _, kept, rstd = O.rms_norm_forward(x.detach(), w.detach(), None if r is None else r.detach(), eps=EPS)
+    check_backward(cy, kept, w.detach(), rstd, ch if rt else None,
+                   (x.grad, w.grad) + ((r.grad,) if rt == F32 else ()))
+    if rt == BF16:
+        assert torch.equal(r.grad, x.grad)
+    if rt:                                                                    # only the stream is used
+        x.grad = r.grad = w.grad = None
+        O.rms_norm(x, w, r, eps=EPS)[1].backward(ch)
+        assert w.grad is None and torch.equal(x.grad, ch.to(BF16)) and torch.equal(r.grad, ch)
+
+
+def test_outputs_end_where_they_end():
+    """Through the C calls, outputs inside larger buffers: nothing before or behind them changes."""
+    for dt, rt, width in ((BF16, BF16, 1000), (BF16, F32, 1001), (F32, F32, 129), (F16, F16, 4096), (BF16, BF16, 40_000)):
+        rows, off = 11, 64
+        x, r, w = activation(rows, width, dt, 71), activation(rows, width, rt, 72), weight_of(width, dt, 73)
+        rstd_room = torch.full((rows + 2 * off,), 9.0, device="cuda")
+        rooms = {"y": dt, "h": rt, "dx": dt}
+        rooms = {k: torch.full((rows * width + 2 * off,), 9.0, dtype=t, device="cuda") for k, t in rooms.items()}
+        dr = torch.full((rows * width + 2 * off,), 9.0, device="cuda")
+        dw = torch.full((width + 2 * off,), 9.0, dtype=dt, device="cuda")
+        stream = torch.cuda.current_stream().cuda_stream
+
+        def at(t):
+            return t.data_ptr() + off * t.element_size()
+
+        tx, tr = O._TYPES[dt], O._TYPES[rt]
+        B.apms_rms_norm(B.RmsNormArgs(rows=rows, width=width, x=x.data_ptr(), x_stride=width, x_type=tx, residual=r.data_ptr(), residual_stride=width,
+                                      residual_type=tr, weight=w.data_ptr(), weight_type=tx, eps=EPS, h=at(rooms["h"]), y=at(rooms["y"]),
+                                      rstd=at(rstd_room)), stream)
+        y, h, rstd = (t[off:-off] for t in (rooms["y"], rooms["h"], rstd_room))
+        check_forward(x, w, r, (y.view(rows, width), h.view(rows, width), rstd))
+        need = B.apms_rms_norm_backward_workspace_bytes(rows, width)
+        ws = torch.full((need + 1024,), 7, dtype=torch.uint8, device="cuda")
+        args = B.RmsNormBackwardArgs(rows=rows, width=width, dy=x.data_ptr(), dy_stride=width, dy_type=tx, h=at(rooms["h"]), h_stride=width, h_type=tr,
+                                     weight=w.data_ptr(), weight_type=tx, rstd=at(rstd_room), dx=at(rooms["dx"]), dweight=at(dw),
+                                     dresidual=at(dr) if tr != tx else None, workspace_dev=ws.data_ptr(), workspace_bytes=need)
+        B.apms_rms_norm_backward(args, stream)
+        got = (rooms["dx"][off:-off].view(rows, width), dw[off:-off]) + ((dr[off:-off].view(rows, width),) if tr != tx else ())
+        check_backward(x, h.view(rows, width), w, rstd, None, got)
+        for t in (*rooms.values(), rstd_room, dw, dr):
+            assert (t[:off] == 9.0).all() and (t[-off:] == 9.0).all()
+        assert (ws[need:] == 7).all()
+        q = torch.full((rows * width + 2 * off,), 9, dtype=torch.uint8, device="cuda")
+        for group in (0, 128):
+            groups = -(-width // (group or width))
+            scales = torch.full((rows * groups + 2 * off,), 9.0, device="cuda")
+            B.apms_rms_norm(B.RmsNormArgs(rows=rows, width=width, x=x.data_ptr(), x_stride=width, x_type=tx, weight=w.data_ptr(), weight_type=tx, eps=EPS,
+                                          y=q.data_ptr() + off, scales=at(scales), group=group, rstd=at(rstd_room)), stream)
+            check_fp8(x, w, None, group, (q[off:-off].view(torch.float8_e4m3fn).view(rows, width), scales[off:-off].view(rows, groups), x, rstd_room[off:-off]))
+            assert (q[:off] == 9).all() and (q[-off:] == 9).all() and (scales[:off] == 9).all() and (scales[-off:] == 9).all()
+
+
+def test_the_norm_refuses_what_does_not_fit():
+    x, w = activation(4, 64, BF16, 81), weight_of(64, BF16, 82)
+    rstd = torch.ones(4, device="cuda")
+    for bad in (lambda: O.rms_norm_forward(x, w[:63]), lambda: O.rms_norm_forward(x, w.half()), lambda: O.rms_norm_forward(x, w, x[:3]),
+                lambda: O.rms_norm_forward(x, w, x.half()), lambda: O.rms_norm_forward(x, w.cpu()), lambda: O.rms_norm_forward(x.int(), w),
+                lambda: O.rms_norm_forward(x[:, :0], w[:0]), lambda: O.rms_norm_fp8(x, w, group=64), lambda: O.rms_norm_forward(x, w, x.cpu()),
+                lambda: O.rms_norm_backward(x, x, w, rstd[:3]), lambda: O.rms_norm_backward(x, x.half(), w, rstd),
+                lambda: O.rms_norm_backward(x, x, w, rstd, x.float()), lambda: O.rms_norm_backward(x, x[:2], w, rstd),
+                lambda: O.rms_norm_backward(x, x, w, rstd.double())):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(B.ApmsError, match="eps"):
+        O.rms_norm_forward(x, w, eps=-1.0)
