@@ -18,13 +18,51 @@ __device__ __forceinline__ void store_element(void* p, int64_t i, int type, floa
     else static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
 
-// Sum over the block's threads in a fixed order; valid in every thread.  smem: one T per warp.  May be called again
-// with the same smem.
+// Two 16-bit elements in a word, the first in the low half.
+template <int TYPE>
+__device__ __forceinline__ float2 unpack16(uint32_t w)
+{
+    if (TYPE == APMS_GRAD_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack16(float a, float b)
+{
+    if (TYPE == APMS_GRAD_BF16) { const __nv_bfloat162 v = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&v); }
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// 32 bytes in one access (sm_100's widest); p is 32-byte aligned.
+__device__ __forceinline__ void load32(uint32_t* w, const void* p)
+{
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* w)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void load16(uint32_t* w, const void* p)
+{
+    const uint4 v = *static_cast<const uint4*>(p);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+}
+
+// Sums in a fixed order, valid in every thread: over a warp, and over the block's threads (smem: one T per warp; may be
+// used again by the next call).
 template <class T>
-__device__ __forceinline__ T block_total(T v, T* smem)
+__device__ __forceinline__ T warp_total(T v)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <class T>
+__device__ __forceinline__ T block_total(T v, T* smem)
+{
+    v = warp_total(v);
     const int warps = (blockDim.x + 31) / 32;
     __syncthreads();
     if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = v;
@@ -32,6 +70,28 @@ __device__ __forceinline__ T block_total(T v, T* smem)
     T t = smem[0];
     for (int w = 1; w < warps; ++w) t += smem[w];
     return t;
+}
+
+// Programmatic dependent launch: the stream's next kernel may start its CTAs once all of this one's have come here, and reads
+// what this one leaves only after its own wait_for_last_kernel(), which returns when this kernel is complete.
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// early: the kernel calls wait_for_last_kernel() and the stream's last kernel was launched by the same call of the library.
+template <class... Params, class... Args>
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t shared, cudaStream_t stream, bool early, const Args&... args)
+{
+    cudaLaunchAttribute attribute = {};
+    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = shared;
+    config.stream = stream;
+    config.attrs = &attribute;
+    config.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&config, kernel, Params(args)...);
 }
 
 inline size_t element_size(int type) { return type == APMS_GRAD_F32 ? 4 : 2; }

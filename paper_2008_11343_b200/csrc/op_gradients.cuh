@@ -9,45 +9,104 @@
 
 namespace {
 
-constexpr int kGradThreads = 256;
-constexpr int kTileBytes = 32768;        // of a tensor's elements
+constexpr int kTileBytes = 32768;        // of a tensor's elements: one CTA's registers hold them, all loads in flight at once
+constexpr int kNormThreads = 128;        // 256 bytes a thread (64 to 256 threads, 8 to 64 KB tiles: 192 to 326 us on 1.34 GB; 128 and 32 KB the fastest)
+constexpr int kScaleThreads = 256;       // 128 bytes a thread (with 256 the registers cost more CTAs than the loads bring)
+constexpr int kGroupTiles = 1024;        // consecutive tiles of one tensor whose sums one warp adds up
+constexpr int kTotalThreads = 512;
 constexpr int kListPointers = 500;       // tensors' addresses in a launch's arguments
 
-struct TileRecord {
+struct __align__(16) TileRecord {
     int64_t first;                       // first element, counted inside its tensor
     int64_t out;                         // ... and inside the whole list (its place in the flat gradient)
+    int64_t numel;                       // the tensor's
     int32_t length;
     int32_t tensor;
+    int32_t type, contiguous;            // the tensor's, here too: one load tells a CTA all it needs
 };
+struct GroupRecord { int32_t tile0, tiles; };      // a group: up to kGroupTiles consecutive tiles of one tensor
 struct TensorRecord {
-    int64_t cols, stride;                // rows of `cols` consecutive elements, `stride` apart
+    int64_t numel, cols, stride;                // rows of `cols` consecutive elements, `stride` apart
     int32_t type;
     int32_t contiguous;
-    int32_t tile0, tiles;
+    int32_t group0, groups;
 };
 struct TensorPointers { const void* p[kListPointers]; };
 
-// Where element e of a tensor lies.
-__device__ __forceinline__ int64_t element_place(const TensorRecord& t, int64_t e)
+// The list's tables and sums in its workspace.
+struct ListMemory {
+    const TileRecord* tiles;
+    const TensorRecord* tensors;
+    const GroupRecord* group;
+    double *tile_sum, *group_sum;
+    unsigned* ticket;                    // zero between calls: the CTA that draws the last one puts it back
+    float* factor;
+    int count, groups;
+};
+
+// Where the elements of a tile of a tensor in rows lie; one 64-bit division a thread, then 32-bit ones.
+struct RowWalk {
+    int64_t row0, col0, cols, stride;
+    __device__ RowWalk(const TensorRecord& t, int64_t first) : row0(first / t.cols), col0(first - row0 * t.cols), cols(t.cols), stride(t.stride) {}
+    __device__ int64_t place(int k) const
+    {
+        const int64_t x = col0 + k;
+        const int64_t q = cols > (1 << 30) ? (int64_t)(x >= cols) : (int64_t)((uint32_t)x / (uint32_t)cols);
+        return (row0 + q) * stride + (x - q * cols);
+    }
+};
+
+// Square of the elements in a word, added to acc.  In binary64, so that nothing a finite gradient holds over- or underflows;
+// joining products in binary32 first was no faster for binary32 and slower for the 16-bit types (the checks it needs).
+template <int TYPE>
+__device__ __forceinline__ void add_squares(double& acc, uint32_t w)
 {
-    return t.contiguous ? e : e / t.cols * t.stride + e % t.cols;
+    if (TYPE == APMS_GRAD_F32) {
+        const double g = (double)__uint_as_float(w);
+        acc = fma(g, g, acc);
+    } else {
+        const float2 g = unpack16<TYPE>(w);
+        acc = fma((double)g.x, (double)g.x, acc);
+        acc = fma((double)g.y, (double)g.y, acc);
+    }
 }
 
-__global__ void __launch_bounds__(kGradThreads)
-k_tile_squares(const __grid_constant__ TensorPointers ptrs, int tensor0, const TileRecord* __restrict__ tiles, int64_t tile0,
-               const TensorRecord* __restrict__ tensors, double* __restrict__ partial)
+template <int TYPE>
+__device__ __forceinline__ double tile_squares(const void* tensor, const TensorRecord* tensors, const TileRecord& tile)
 {
-    __shared__ double red[kGradThreads / 32];
-    const TileRecord tile = tiles[tile0 + blockIdx.x];
-    const TensorRecord t = tensors[tile.tensor];
-    const void* p = ptrs.p[tile.tensor - tensor0];
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2, V = 32 / ES, LOADS = kTileBytes / 32 / kNormThreads;
     double acc = 0.0;
-    for (int k = threadIdx.x; k < tile.length; k += kGradThreads) {
-        const double g = (double)load_element(p, element_place(t, tile.first + k), t.type);
-        acc = fma(g, g, acc);
+    if (!tile.contiguous) {
+        const RowWalk walk(tensors[tile.tensor], tile.first);
+        for (int k = threadIdx.x; k < tile.length; k += kNormThreads) {
+            const double g = (double)load_element(tensor, walk.place(k), TYPE);
+            acc = fma(g, g, acc);
+        }
+        return acc;
     }
-    acc = block_total(acc, red);
-    if (threadIdx.x == 0) partial[tile0 + blockIdx.x] = acc;
+    const char* p = static_cast<const char*>(tensor) + tile.first * ES;
+    const int head = min(tile.length, (int)((32 - ((uintptr_t)p & 31)) & 31) / ES);       // elements up to the first 32-byte boundary
+    const int vectors = (tile.length - head) / V;
+    const char* body = p + head * ES;
+    uint32_t w[LOADS][8];
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+        const int at = k * kNormThreads + threadIdx.x;
+        if (at < vectors) load32(w[k], body + at * 32);
+        else for (int j = 0; j < 8; ++j) w[k][j] = 0;
+    }
+    const int loose = tile.length - vectors * V;                                          // before and behind the body, below 2 V
+    if (threadIdx.x < loose) {
+        const int k = threadIdx.x < head ? threadIdx.x : threadIdx.x + vectors * V;
+        const double g = (double)load_element(p, k, TYPE);
+        acc = g * g;
+    }
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) add_squares<TYPE>(acc, w[k][j]);
+    }
+    return acc;
 }
 
 __device__ __forceinline__ float clip_factor(double squares, float max_norm)
@@ -56,39 +115,199 @@ __device__ __forceinline__ float clip_factor(double squares, float max_norm)
     return (isinf(max_norm) || (float)norm <= max_norm) ? 1.0f : (float)((double)max_norm / norm);
 }
 
-// One CTA: the tensors' sums, then the list's.
-__global__ void __launch_bounds__(kGradThreads)
-k_list_norm(const TensorRecord* __restrict__ tensors, int count, const double* __restrict__ partial, float* __restrict__ norm,
-            float* __restrict__ norms, float max_norm, float* __restrict__ factor)
+// Sums of squares of the tiles.  A CTA holds one tile in registers and leaves: nothing
+// is counted and nobody is waited for (a ticket per tile, by which the last CTA would know to finish the sum, kept the CTAs
+// on the SMs for the fence and the atomic's round trip: 256 us instead of 197 us on 1.34 GB).
+__global__ void __launch_bounds__(kNormThreads)
+k_tile_squares(const __grid_constant__ TensorPointers ptrs, int tensor0, int64_t tile0, const __grid_constant__ ListMemory m)
 {
-    __shared__ double red[kGradThreads / 32];
+    __shared__ double red[kNormThreads / 32];
+    allow_next_kernel();
+    const TileRecord tile = m.tiles[tile0 + blockIdx.x];
+    const void* p = ptrs.p[tile.tensor - tensor0];
+    double acc = tile.type == APMS_GRAD_F32 ? tile_squares<APMS_GRAD_F32>(p, m.tensors, tile)
+               : tile.type == APMS_GRAD_BF16 ? tile_squares<APMS_GRAD_BF16>(p, m.tensors, tile) : tile_squares<APMS_GRAD_F16>(p, m.tensors, tile);
+    acc = warp_total(acc);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = acc;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kNormThreads / 32; ++w) acc += red[w];
+        m.tile_sum[tile0 + blockIdx.x] = acc;
+    }
+}
+
+// A warp adds the tiles of a group; the CTA that is done last (a ticket each) adds the groups, tensor by tensor, and the tensors.
+// Every sum runs in an order fixed by the list, whoever forms it.
+__global__ void __launch_bounds__(kTotalThreads)
+k_list_norm(const __grid_constant__ ListMemory m, float* __restrict__ norm, float* __restrict__ norms, float max_norm)
+{
+    __shared__ double red[kTotalThreads / 32];
+    __shared__ bool last;
+    allow_next_kernel();
+    const int group = blockIdx.x * (kTotalThreads / 32) + threadIdx.x / 32, lane = threadIdx.x & 31;
+    GroupRecord g = {0, 0};
+    if (group < m.groups) g = m.group[group];
+    int g0 = 0, groups = 0;                          // of this thread's first tensor, for the last CTA
+    if (threadIdx.x < m.count) { g0 = m.tensors[threadIdx.x].group0; groups = m.tensors[threadIdx.x].groups; }
+    wait_for_last_kernel();
+    double acc = 0.0;
+#pragma unroll 8
+    for (int k = lane; k < g.tiles; k += 32) acc += m.tile_sum[g.tile0 + k];
+    acc = warp_total(acc);
+    if (lane == 0 && group < m.groups) m.group_sum[group] = acc;
+    __syncthreads();
+    if (gridDim.x > 1) {
+        if (threadIdx.x == 0) {
+            __threadfence();
+            last = atomicAdd(m.ticket, 1u) == gridDim.x - 1;
+            __threadfence();
+        }
+        __syncthreads();
+        if (!last) return;
+        if (threadIdx.x == 0) *m.ticket = 0;
+    }
     double total = 0.0;
-    for (int t = threadIdx.x; t < count; t += kGradThreads) {
+    for (int k = threadIdx.x; k < m.count; k += kTotalThreads) {
         double s = 0.0;
-        for (int k = 0; k < tensors[t].tiles; ++k) s += partial[tensors[t].tile0 + k];
-        if (norms) norms[t] = (float)sqrt(s);
+#pragma unroll 8
+        for (int j = 0; j < groups; ++j) s += __ldcg(m.group_sum + g0 + j);
+        if (norms) norms[k] = (float)sqrt(s);
         total += s;
+        if (k + kTotalThreads < m.count) { g0 = m.tensors[k + kTotalThreads].group0; groups = m.tensors[k + kTotalThreads].groups; }
     }
     total = block_total(total, red);
     if (threadIdx.x == 0) {
         *norm = (float)sqrt(total);
-        *factor = clip_factor(total, max_norm);
+        *m.factor = clip_factor(total, max_norm);
     }
 }
 
-__global__ void __launch_bounds__(kGradThreads)
-k_scale_tiles(const __grid_constant__ TensorPointers ptrs, int tensor0, const TileRecord* __restrict__ tiles, int64_t tile0,
-              const TensorRecord* __restrict__ tensors, void* flat, int flat_type, const float* __restrict__ factor)
+// ELEMENTS (8, or 16 where a 16-bit type is involved: 32 bytes of the narrower type) consecutive elements at p as they lie in
+// memory.  p is 32-byte aligned, or 16-byte aligned, or `shift` bytes behind such a boundary, the same for the whole tile:
+// a shifted read takes the aligned 16-byte pieces around it and puts the bytes together (a thread's last piece is its neighbour's first, so it comes from L1).
+template <int TYPE, int ELEMENTS>
+struct Piece {
+    static constexpr int WORDS = ELEMENTS * (TYPE == APMS_GRAD_F32 ? 4 : 2) / 4;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const char* p, int shift)
+    {
+        if (shift == 0 && ((uintptr_t)p & 16) == 0) {
+#pragma unroll
+            for (int k = 0; k < WORDS; k += 8) load32(w + k, p + 4 * k);
+            return;
+        }
+        uint32_t a[WORDS + 4];
+#pragma unroll
+        for (int k = 0; k < WORDS; k += 4) load16(a + k, p - shift + 4 * k);
+        if (shift) load16(a + WORDS, p - shift + 4 * WORDS);
+        else a[WORDS] = a[WORDS + 1] = a[WORDS + 2] = a[WORDS + 3] = 0;
+        const int words = shift >> 2, bits = (shift & 3) * 8;
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            const uint32_t lo = words == 0 ? a[k] : words == 1 ? a[k + 1] : words == 2 ? a[k + 2] : a[k + 3];
+            const uint32_t hi = words == 0 ? a[k + 1] : words == 1 ? a[k + 2] : words == 2 ? a[k + 3] : a[k + 4];
+            w[k] = __funnelshift_r(lo, hi, bits);
+        }
+    }
+    __device__ __forceinline__ void values(float* f) const
+    {
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            if (TYPE == APMS_GRAD_F32) f[k] = __uint_as_float(w[k]);
+            else { const float2 g = unpack16<TYPE>(w[k]); f[2 * k] = g.x; f[2 * k + 1] = g.y; }
+        }
+    }
+    // f rounded to TYPE, at a 32-byte aligned p
+    static __device__ __forceinline__ void store(char* p, const float* f)
+    {
+        uint32_t v[WORDS];
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) v[k] = TYPE == APMS_GRAD_F32 ? __float_as_uint(f[k]) : pack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(f[(2 * k) % ELEMENTS], f[(2 * k + 1) % ELEMENTS]);
+#pragma unroll
+        for (int k = 0; k < WORDS; k += 8) store32(p + 4 * k, v + k);
+    }
+};
+
+__device__ __forceinline__ float factor_when_ready(const float* factor)
 {
-    const TileRecord tile = tiles[tile0 + blockIdx.x];
-    const TensorRecord t = tensors[tile.tensor];
-    void* p = const_cast<void*>(ptrs.p[tile.tensor - tensor0]);
-    const float c = *factor;
-    for (int k = threadIdx.x; k < tile.length; k += kGradThreads) {
-        const int64_t at = element_place(t, tile.first + k);
-        const float g = load_element(p, at, t.type) * c;
-        if (flat) store_element(flat, tile.out + k, flat_type, g);
-        else store_element(p, at, t.type, g);
+    wait_for_last_kernel();
+    return __ldcg(factor);
+}
+
+// One tile times the factor, from SRC to DST elements at `out`.  The elements are loaded before the factor is waited for.
+template <int SRC, int DST>
+__device__ __forceinline__ void scale_tile(const void* tensor, const TensorRecord* tensors, const TileRecord& tile, char* out, const float* factor, bool in_place)
+{
+    constexpr int SS = SRC == APMS_GRAD_F32 ? 4 : 2, DS = DST == APMS_GRAD_F32 ? 4 : 2;
+    constexpr int N = SS == 4 && DS == 4 ? 8 : 16, PIECES = kTileBytes / SS / N / kScaleThreads;
+    if (!tile.contiguous) {
+        const RowWalk walk(tensors[tile.tensor], tile.first);
+        const float c = factor_when_ready(factor);
+        if (in_place && c == 1.0f) return;
+        for (int k = threadIdx.x; k < tile.length; k += kScaleThreads) {
+            const int64_t at = walk.place(k);
+            const float g = load_element(tensor, at, SRC) * c;
+            if (in_place) store_element(const_cast<void*>(tensor), at, SRC, g);
+            else store_element(out, k, DST, g);
+        }
+        return;
+    }
+    const char* p = static_cast<const char*>(tensor) + tile.first * SS;
+    const int head = min(tile.length, (int)((32 - ((uintptr_t)out & 31)) & 31) / DS);     // elements up to the output's first 32-byte boundary
+    const char* from = p + head * SS;
+    const int shift = (int)((uintptr_t)from & 15);
+    int pieces = (tile.length - head) / N, skip = 0;
+    if (shift) {                                   // shifted reads inside the tensor only; the pieces at its ends go one by one
+        const char* lo = static_cast<const char*>(tensor);
+        const char* hi = lo + tile.numel * SS;
+        if (pieces && from - shift < lo) skip = 1;
+        if (pieces && from - shift + (int64_t)pieces * (N * SS) + 16 > hi) --pieces;
+        if (skip > pieces) skip = pieces;
+    }
+    Piece<SRC, N> v[PIECES];
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int at = k * kScaleThreads + threadIdx.x;
+        if (at >= skip && at < pieces) v[k].load(from + at * (N * SS), shift);
+    }
+    const float c = factor_when_ready(factor);
+    if (in_place && c == 1.0f) return;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int at = k * kScaleThreads + threadIdx.x;
+        if (at >= skip && at < pieces) {
+            float f[N];
+            v[k].values(f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] *= c;
+            Piece<DST, N>::store(out + (head + at * N) * DS, f);
+        }
+    }
+    const int before = head + skip * N, behind = head + pieces * N;                       // one by one: [0, before) and [behind, length)
+    for (int k = threadIdx.x; k < before + tile.length - behind; k += kScaleThreads) {
+        const int e = k < before ? k : k - before + behind;
+        store_element(out, e, DST, load_element(p, e, SRC) * c);
+    }
+}
+
+// DST < 0: in place.  The tiles are taken in the norm's order backwards: its last ones may still be in L2.
+template <int DST>
+__global__ void __launch_bounds__(kScaleThreads)
+k_scale_tiles(const __grid_constant__ TensorPointers ptrs, int tensor0, int64_t tile0, const __grid_constant__ ListMemory m, char* flat)
+{
+    const TileRecord tile = m.tiles[tile0 + gridDim.x - 1 - blockIdx.x];
+    const void* p = ptrs.p[tile.tensor - tensor0];
+    if (DST < 0) {
+        char* out = static_cast<char*>(const_cast<void*>(p)) + tile.first * (tile.type == APMS_GRAD_F32 ? 4 : 2);
+        if (tile.type == APMS_GRAD_F32) scale_tile<APMS_GRAD_F32, APMS_GRAD_F32>(p, m.tensors, tile, out, m.factor, true);
+        else if (tile.type == APMS_GRAD_BF16) scale_tile<APMS_GRAD_BF16, APMS_GRAD_BF16>(p, m.tensors, tile, out, m.factor, true);
+        else scale_tile<APMS_GRAD_F16, APMS_GRAD_F16>(p, m.tensors, tile, out, m.factor, true);
+    } else {
+        constexpr int D = DST < 0 ? 0 : DST;
+        char* out = flat + tile.out * (D == APMS_GRAD_F32 ? 4 : 2);
+        if (tile.type == APMS_GRAD_F32) scale_tile<APMS_GRAD_F32, D>(p, m.tensors, tile, out, m.factor, false);
+        else if (tile.type == APMS_GRAD_BF16) scale_tile<APMS_GRAD_BF16, D>(p, m.tensors, tile, out, m.factor, false);
+        else scale_tile<APMS_GRAD_F16, D>(p, m.tensors, tile, out, m.factor, false);
     }
 }
 
@@ -97,20 +316,24 @@ k_scale_tiles(const __grid_constant__ TensorPointers ptrs, int tensor0, const Ti
 struct apms_tensors {
     std::vector<TensorRecord> tensors;
     std::vector<TileRecord> tiles;
-    std::vector<int64_t> numel;
+    std::vector<GroupRecord> groups;
+    std::vector<int> tile0;              // first tile of each tensor, and behind the last
     int64_t total;
-    TileRecord* d_tiles;
-    TensorRecord* d_tensors;
-    double* d_partial;
-    float* d_factor;
+    ListMemory m;                        // m.tiles == nullptr: no workspace yet
 
-    size_t place(size_t* tensors_at, size_t* partial_at, size_t* factor_at) const
+    // Byte offsets of the tables and sums in the workspace.
+    struct Places { size_t tensors, groups, tile_sum, group_sum, ticket, bytes; };
+    Places places() const
     {
         auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-        *tensors_at = up(tiles.size() * sizeof(TileRecord));
-        *partial_at = *tensors_at + up(tensors.size() * sizeof(TensorRecord));
-        *factor_at = *partial_at + up(tiles.size() * sizeof(double));
-        return *factor_at + 256;
+        Places p;
+        p.tensors = up(tiles.size() * sizeof(TileRecord));
+        p.groups = p.tensors + up(tensors.size() * sizeof(TensorRecord));
+        p.tile_sum = p.groups + up(groups.size() * sizeof(GroupRecord));
+        p.group_sum = p.tile_sum + up(tiles.size() * sizeof(double));
+        p.ticket = p.group_sum + up(groups.size() * sizeof(double));     // and the factor behind it
+        p.bytes = p.ticket + 256;
+        return p;
     }
 };
 
@@ -131,53 +354,61 @@ apms_status apms_tensors_create(apms_tensors** out, int count, const int64_t* nu
                                  (long long)numel[t], (long long)cols[t], (long long)row_strides[t]);
     }
     try {
-        apms_tensors* list = new apms_tensors();
+        std::unique_ptr<apms_tensors> list(new apms_tensors());
         int64_t at = 0;
         for (int t = 0; t < count; ++t) {
             TensorRecord r = {};
+            r.numel = numel[t];
             r.type = types[t];
             r.contiguous = !cols || row_strides[t] == cols[t] || cols[t] == numel[t];
             r.cols = r.contiguous ? numel[t] : cols[t];
             r.stride = r.contiguous ? numel[t] : row_strides[t];
-            r.tile0 = (int32_t)list->tiles.size();
             const int64_t per_tile = kTileBytes / (int64_t)element_size(types[t]);
-            for (int64_t e = 0; e < numel[t]; e += per_tile) {
-                if (list->tiles.size() >= 0x7fffffff) { delete list; return operator_fail(APMS_ERR_INVALID_ARG, "apms_tensors_create: the list is too long"); }
-                list->tiles.push_back({e, at + e, (int32_t)std::min(per_tile, numel[t] - e), t});
+            const int64_t tiles = (numel[t] + per_tile - 1) / per_tile;
+            if ((int64_t)list->tiles.size() + tiles > 0x7fffffff) return operator_fail(APMS_ERR_INVALID_ARG, "apms_tensors_create: the list is too long");
+            r.group0 = (int32_t)list->groups.size();
+            list->tile0.push_back((int)list->tiles.size());
+            for (int64_t k = 0; k < tiles; ++k) {
+                if (k % kGroupTiles == 0) list->groups.push_back({(int32_t)list->tiles.size(), (int32_t)std::min<int64_t>(kGroupTiles, tiles - k)});
+                list->tiles.push_back({k * per_tile, at + k * per_tile, numel[t], (int32_t)std::min(per_tile, numel[t] - k * per_tile), t, r.type, r.contiguous});
             }
-            r.tiles = (int32_t)list->tiles.size() - r.tile0;
+            r.groups = (int32_t)list->groups.size() - r.group0;
             list->tensors.push_back(r);
-            list->numel.push_back(numel[t]);
             at += numel[t];
         }
         list->total = at;
-        *out = list;
+        list->tile0.push_back((int)list->tiles.size());
+        *out = list.release();
     } catch (const std::bad_alloc&) {
         return operator_fail(APMS_ERR_OOM, "apms_tensors_create: host allocation failed");
     }
     return APMS_OK;
 }
 
-size_t apms_tensors_workspace_bytes(const apms_tensors* list)
-{
-    size_t a, b, c;
-    return list ? list->place(&a, &b, &c) : 0;
-}
+size_t apms_tensors_workspace_bytes(const apms_tensors* list) { return list ? list->places().bytes : 0; }
 
 apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t bytes, void* cuda_stream)
 {
     if (!list || !workspace_dev || ((uintptr_t)workspace_dev & 255u)) return operator_fail(APMS_ERR_INVALID_ARG, "apms_tensors_bind: needs a list and a 256-byte aligned workspace");
-    size_t tensors_at, partial_at, factor_at;
-    if (bytes < list->place(&tensors_at, &partial_at, &factor_at)) return operator_fail(APMS_ERR_OOM, "apms_tensors_bind: workspace smaller than apms_tensors_workspace_bytes()");
+    const apms_tensors::Places at = list->places();
+    if (bytes < at.bytes) return operator_fail(APMS_ERR_OOM, "apms_tensors_bind: workspace smaller than apms_tensors_workspace_bytes()");
     char* ws = (char*)workspace_dev;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws, list->tiles.data(), list->tiles.size() * sizeof(TileRecord), cudaMemcpyHostToDevice, stream));
-    OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws + tensors_at, list->tensors.data(), list->tensors.size() * sizeof(TensorRecord), cudaMemcpyHostToDevice, stream));
+    OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws + at.tensors, list->tensors.data(), list->tensors.size() * sizeof(TensorRecord), cudaMemcpyHostToDevice, stream));
+    OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws + at.groups, list->groups.data(), list->groups.size() * sizeof(GroupRecord), cudaMemcpyHostToDevice, stream));
+    OPERATOR_CUDA("apms_tensors_bind", cudaMemsetAsync(ws + at.ticket, 0, at.bytes - at.ticket, stream));
     OPERATOR_CUDA("apms_tensors_bind", cudaStreamSynchronize(stream));
-    list->d_tiles = (TileRecord*)ws;
-    list->d_tensors = (TensorRecord*)(ws + tensors_at);
-    list->d_partial = (double*)(ws + partial_at);
-    list->d_factor = (float*)(ws + factor_at);
+    ListMemory& m = list->m;
+    m.tiles = (const TileRecord*)ws;
+    m.tensors = (const TensorRecord*)(ws + at.tensors);
+    m.tile_sum = (double*)(ws + at.tile_sum);
+    m.group_sum = (double*)(ws + at.group_sum);
+    m.group = (const GroupRecord*)(ws + at.groups);
+    m.ticket = (unsigned*)(ws + at.ticket);
+    m.factor = (float*)(m.ticket + 1);
+    m.count = (int)list->tensors.size();
+    m.groups = (int)list->groups.size();
     return APMS_OK;
 }
 
@@ -189,50 +420,47 @@ namespace {
 
 apms_status check_addresses(const apms_tensors* list, const void* const* tensors_dev, const char* who)
 {
-    if (!list || !list->d_tiles) return operator_fail(APMS_ERR_BAD_STATE, "%s: the list has no workspace (apms_tensors_bind)", who);
+    if (!list || !list->m.tiles) return operator_fail(APMS_ERR_BAD_STATE, "%s: the list has no workspace (apms_tensors_bind)", who);
     if (!tensors_dev) return operator_fail(APMS_ERR_INVALID_ARG, "%s: tensors_dev is NULL", who);
     for (size_t t = 0; t < list->tensors.size(); ++t)
-        if (list->numel[t] && (!tensors_dev[t] || (uintptr_t)tensors_dev[t] % element_size(list->tensors[t].type)))
+        if (list->tensors[t].numel && (!tensors_dev[t] || (uintptr_t)tensors_dev[t] % element_size(list->tensors[t].type)))
             return operator_fail(APMS_ERR_INVALID_ARG, "%s: tensor %zu is at a NULL or misaligned address", who, t);
     return APMS_OK;
 }
 
-// The bytes tensor t spans, from its first element to behind its last.
-int64_t spanned_bytes(const apms_tensors* list, size_t t)
+// The bytes a tensor spans, from its first element to behind its last.
+int64_t spanned_bytes(const TensorRecord& r)
 {
-    const TensorRecord& r = list->tensors[t];
-    if (!list->numel[t]) return 0;
-    return ((list->numel[t] / r.cols - 1) * r.stride + r.cols) * (int64_t)element_size(r.type);
+    if (!r.numel) return 0;
+    return ((r.numel / r.cols - 1) * r.stride + r.cols) * (int64_t)element_size(r.type);
 }
 
-// Launches `kernel(pointers, first tensor, tiles, first tile, tensors, ...)` over the list's tiles, as many tensors at a
-// time as a launch's arguments hold addresses.
-template <class Kernel, class... Args>
-cudaError_t over_tiles(const apms_tensors* list, const void* const* tensors_dev, cudaStream_t stream, Kernel kernel, Args... args)
+// Launches `kernel(addresses, first tensor, first tile, memory, ...)` over the list's tiles, as many tensors at a time as a
+// launch's arguments hold addresses.  `early`: the first launch may begin while the kernel before it drains.
+template <class... Params, class... Args>
+cudaError_t over_tiles(const apms_tensors* list, const void* const* tensors_dev, cudaStream_t stream, int threads, bool early,
+                       void (*kernel)(TensorPointers, int, int64_t, ListMemory, Params...), Args... args)
 {
     const int count = (int)list->tensors.size();
     for (int t0 = 0; t0 < count; t0 += kListPointers) {
         const int t1 = std::min(count, t0 + kListPointers);
-        const int64_t first = list->tensors[t0].tile0, last = list->tensors[t1 - 1].tile0 + list->tensors[t1 - 1].tiles;
+        const int64_t first = list->tile0[t0], last = list->tile0[t1];
         if (first == last) continue;
         TensorPointers ptrs;
         memcpy(ptrs.p, tensors_dev + t0, (t1 - t0) * sizeof(void*));
-        kernel<<<(unsigned)(last - first), kGradThreads, 0, stream>>>(ptrs, t0, list->d_tiles, first, list->d_tensors, args...);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = launch(kernel, dim3((unsigned)(last - first)), threads, 0, stream, early, ptrs, t0, first, list->m, Params(args)...);
         if (e != cudaSuccess) return e;
+        early = false;
     }
     return cudaSuccess;
 }
 
-apms_status list_norm(apms_tensors* list, const void* const* tensors_dev, float* norm_dev, float* norms_dev, float max_norm,
-                      cudaStream_t stream, const char* who)
+cudaError_t list_norm(const apms_tensors* list, const void* const* tensors_dev, cudaStream_t stream, float* norm, float* norms, float max_norm)
 {
-    cudaError_t e = over_tiles(list, tensors_dev, stream, k_tile_squares, list->d_partial);
-    if (e == cudaSuccess) {
-        k_list_norm<<<1, kGradThreads, 0, stream>>>(list->d_tensors, (int)list->tensors.size(), list->d_partial, norm_dev, norms_dev, max_norm, list->d_factor);
-        e = cudaGetLastError();
-    }
-    return e == cudaSuccess ? APMS_OK : operator_fail(APMS_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+    const cudaError_t e = over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares);
+    if (e != cudaSuccess) return e;
+    const unsigned ctas = std::max(1u, (unsigned)((list->groups.size() + kTotalThreads / 32 - 1) / (kTotalThreads / 32)));
+    return launch(k_list_norm, dim3(ctas), kTotalThreads, 0, stream, !list->tiles.empty(), list->m, norm, norms, max_norm);
 }
 
 }  // namespace
@@ -244,7 +472,8 @@ apms_status apms_grad_norm(apms_tensors* list, const void* const* tensors_dev, f
     const apms_status st = check_addresses(list, tensors_dev, "apms_grad_norm");
     if (st != APMS_OK) return st;
     if (!norm_dev) return operator_fail(APMS_ERR_INVALID_ARG, "apms_grad_norm: norm_dev is NULL");
-    return list_norm(list, tensors_dev, norm_dev, norms_dev, INFINITY, (cudaStream_t)cuda_stream, "apms_grad_norm");
+    const cudaError_t e = list_norm(list, tensors_dev, (cudaStream_t)cuda_stream, norm_dev, norms_dev, INFINITY);
+    return e == cudaSuccess ? APMS_OK : operator_fail(APMS_ERR_CUDA, "apms_grad_norm: %s", cudaGetErrorString(e));
 }
 
 apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float max_norm, void* flat_dev, apms_grad_type flat_type,
@@ -259,8 +488,8 @@ apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float 
         if (!known_type(flat_type) || ((uintptr_t)flat_dev & 15u)) return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: flat_dev must be 16-byte aligned, of a known type");
         const uintptr_t f0 = (uintptr_t)flat_dev, es = element_size(flat_type), f1 = f0 + (uintptr_t)list->total * es;
         int64_t at = 0;
-        for (size_t t = 0; t < count; at += list->numel[t], ++t) {
-            const uintptr_t a0 = (uintptr_t)tensors_dev[t], a1 = a0 + (uintptr_t)spanned_bytes(list, t);
+        for (size_t t = 0; t < count; at += list->tensors[t].numel, ++t) {
+            const uintptr_t a0 = (uintptr_t)tensors_dev[t], a1 = a0 + (uintptr_t)spanned_bytes(list->tensors[t]);
             if (a0 == a1 || a1 <= f0 || a0 >= f1) continue;
             if (!list->tensors[t].contiguous || list->tensors[t].type != (int)flat_type || a0 != f0 + (uintptr_t)at * es)
                 return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: tensor %zu overlaps the flat gradient without being in its place there", t);
@@ -270,7 +499,7 @@ apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float 
             // of a tensor in rows its first row only: column slices of one matrix interleave without sharing elements
             std::vector<std::pair<uintptr_t, uintptr_t>> spans;
             for (size_t t = 0; t < count; ++t)
-                if (list->numel[t]) spans.push_back({(uintptr_t)tensors_dev[t], (uintptr_t)tensors_dev[t] + (uintptr_t)list->tensors[t].cols * element_size(list->tensors[t].type)});
+                if (list->tensors[t].numel) spans.push_back({(uintptr_t)tensors_dev[t], (uintptr_t)tensors_dev[t] + (uintptr_t)list->tensors[t].cols * element_size(list->tensors[t].type)});
             std::sort(spans.begin(), spans.end());
             for (size_t k = 1; k < spans.size(); ++k)
                 if (spans[k].first < spans[k - 1].second) return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: two tensors of the list overlap in memory; clip into a flat gradient instead");
@@ -278,9 +507,15 @@ apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float 
             return operator_fail(APMS_ERR_OOM, "apms_clip_grads: host allocation failed");
         }
     }
-    st = list_norm(list, tensors_dev, norm_dev, nullptr, max_norm, (cudaStream_t)cuda_stream, "apms_clip_grads");
-    if (st != APMS_OK) return st;
-    const cudaError_t e = over_tiles(list, tensors_dev, (cudaStream_t)cuda_stream, k_scale_tiles, flat_dev, (int)flat_type, (const float*)list->d_factor);
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    cudaError_t e = list_norm(list, tensors_dev, stream, norm_dev, nullptr, max_norm);
+    if (e == cudaSuccess) {
+        char* flat = (char*)flat_dev;
+        e = !flat ? over_tiles(list, tensors_dev, stream, kScaleThreads, true, k_scale_tiles<-1>, flat)
+          : flat_type == APMS_GRAD_F32 ? over_tiles(list, tensors_dev, stream, kScaleThreads, true, k_scale_tiles<APMS_GRAD_F32>, flat)
+          : flat_type == APMS_GRAD_BF16 ? over_tiles(list, tensors_dev, stream, kScaleThreads, true, k_scale_tiles<APMS_GRAD_BF16>, flat)
+          : over_tiles(list, tensors_dev, stream, kScaleThreads, true, k_scale_tiles<APMS_GRAD_F16>, flat);
+    }
     return e == cudaSuccess ? APMS_OK : operator_fail(APMS_ERR_CUDA, "apms_clip_grads: %s", cudaGetErrorString(e));
 }
 

@@ -7,6 +7,7 @@
 #include <cuda_fp8.h>
 #include <algorithm>
 #include <math.h>
+#include <memory>
 #include <new>
 #include <stdarg.h>
 #include <stdint.h>

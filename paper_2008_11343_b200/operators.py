@@ -16,6 +16,7 @@ import torch
 
 from . import binding as B
 
+_numel, _is_contiguous, _get_device, _data_ptr = (getattr(torch.Tensor, name) for name in ("numel", "is_contiguous", "get_device", "data_ptr"))
 _TYPES = {torch.float32: B.GRAD_F32, torch.bfloat16: B.GRAD_BF16, torch.float16: B.GRAD_F16}
 
 
@@ -88,17 +89,16 @@ class TensorList:
 
     def _addresses(self, tensors) -> array:
         """The tensors' addresses, once they are found to be laid out as the list's are."""
-        if [t.numel() for t in tensors] != self._numel or [t.dtype for t in tensors] != self._dtypes:
+        if list(map(_numel, tensors)) != self._numel or [t.dtype for t in tensors] != self._dtypes:
             raise ValueError("the tensors differ from the list's in number, size or type")
         if self._strides is None:
-            if not all([t.is_contiguous() for t in tensors]):
+            if not all(map(_is_contiguous, tensors)):
                 raise ValueError("a tensor is not contiguous, as it was when the list was made")
         elif [(t.shape, t.stride()) for t in tensors] != self._strides:
             raise ValueError("the tensors' strides differ from the list's")
-        where = {t.device for t in tensors}
-        if where != {self.device}:
-            raise ValueError(f"the tensors lie on {where}, the list on {self.device}")
-        return array("Q", [t.data_ptr() for t in tensors])
+        if set(map(_get_device, tensors)) != {self.device.index}:
+            raise ValueError(f"a tensor does not lie on {self.device}, as the list does")
+        return array("Q", map(_data_ptr, tensors))
 
     def _enter(self) -> int:
         stream = torch.cuda.current_stream(self.device)
