@@ -33,7 +33,206 @@ __device__ __forceinline__ void group_scale(uint32_t most_bits, float* scale, fl
     *inverse = none ? 0.0f : __fdiv_rn(kE4m3Max, a);
 }
 
-// One CTA per row, any width, stride and alignment: the row is read again for each of the passes.
+// How a warp lays its elements of a row over its lanes.  VECTOR: 16 bytes of the activations' type a lane (8 or 4 consecutive
+// elements), for rows that all start on a 16-byte boundary and hold whole 16-byte pieces.  Otherwise 4 elements a lane, 32 apart, so
+// that the accesses of a warp are consecutive.  A unit is what a warp's lanes hold at one time: 128 or 256 elements; a
+// group of 128 columns is then always a whole warp or half of one.
+template <int XT, bool VECTOR>
+struct Lanes {
+    static constexpr int E = VECTOR && XT != APMS_GRAD_F32 ? 8 : 4;      // elements a lane and unit
+    static constexpr int UNIT = 32 * E, GROUP_LANES = 128 / E;
+    // column of element j of a lane in a unit of the row
+    static __device__ __forceinline__ int column(int unit, int lane, int j) { return unit * UNIT + (VECTOR ? lane * E + j : lane + 32 * j); }
+};
+
+// E elements of type TYPE from column `unit`, 0 behind the width.
+template <int TYPE, class L, bool VECTOR>
+__device__ __forceinline__ void load_unit(float* f, const char* row, int unit, int lane, int width)
+{
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
+    if (VECTOR) {
+        const int c = L::column(unit, lane, 0);
+        uint32_t w[L::E * ES / 4];
+        if (c < width) {
+#pragma unroll
+            for (int k = 0; k < L::E * ES / 4; k += 4) load16(w + k, row + (int64_t)c * ES + 4 * k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < L::E * ES / 4; ++k) w[k] = 0;
+        }
+#pragma unroll
+        for (int k = 0; k < L::E * ES / 4; ++k) {
+            if (ES == 4) f[k] = __uint_as_float(w[k]);
+            else { const float2 v = unpack16<TYPE>(w[k]); f[(2 * k) % L::E] = v.x; f[(2 * k + 1) % L::E] = v.y; }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < L::E; ++j) {
+            const int c = L::column(unit, lane, j);
+            f[j] = c < width ? load_element(row, c, TYPE) : 0.0f;
+        }
+    }
+}
+
+template <int TYPE, class L, bool VECTOR>
+__device__ __forceinline__ void store_unit(char* row, const float* f, int unit, int lane, int width)
+{
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
+    if (VECTOR) {
+        const int c = L::column(unit, lane, 0);
+        if (c >= width) return;
+        uint32_t w[L::E * ES / 4];
+#pragma unroll
+        for (int k = 0; k < L::E * ES / 4; ++k)
+            w[k] = ES == 4 ? __float_as_uint(f[k]) : pack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(f[(2 * k) % L::E], f[(2 * k + 1) % L::E]);
+#pragma unroll
+        for (int k = 0; k < L::E * ES / 4; k += 4) *reinterpret_cast<uint4*>(row + (int64_t)c * ES + 4 * k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < L::E; ++j) {
+            const int c = L::column(unit, lane, j);
+            if (c < width) store_element(row, c, TYPE, f[j]);
+        }
+    }
+}
+
+template <class L, bool VECTOR>
+__device__ __forceinline__ void store_unit_e4m3(uint8_t* row, const float* f, int unit, int lane, int width)
+{
+    if (VECTOR) {
+        const int c = L::column(unit, lane, 0);
+        if (c >= width) return;
+        uint32_t w[L::E / 4];
+#pragma unroll
+        for (int k = 0; k < L::E / 4; ++k)
+            w[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[4 * k], f[4 * k + 1]), __NV_SATFINITE, __NV_E4M3) |
+                   (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[4 * k + 2], f[4 * k + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
+        if (L::E == 8) *reinterpret_cast<uint2*>(row + c) = make_uint2(w[0], w[L::E / 4 - 1]);
+        else *reinterpret_cast<uint32_t*>(row + c) = w[0];
+    } else {
+#pragma unroll
+        for (int j = 0; j < L::E; ++j) {
+            const int c = L::column(unit, lane, j);
+            if (c < width) row[c] = __nv_cvt_float_to_fp8(f[j], __NV_SATFINITE, __NV_E4M3);
+        }
+    }
+}
+
+constexpr int kTeamWarps = 16;                   // a row's at most: with 32 elements a lane, rows of up to 16,384
+
+// Combines a value of each of a team's warps (a row's); TEAM warps of consecutive index.  smem: one T per warp of the CTA.  Every
+// thread of the CTA calls it.
+template <class T, class Op>
+__device__ __forceinline__ T over_team(T v, T* smem, int team_warps, Op op)
+{
+    if (team_warps == 1) return v;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) smem[warp] = v;
+    __syncthreads();
+    const int first = warp / team_warps * team_warps;
+    v = lane < team_warps ? smem[first + lane] : T(0);
+#pragma unroll
+    for (int o = kTeamWarps; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// A team of `team_warps` warps a row, NU units a warp, the row in registers from the first load to the last store: x, the residual
+// and the weight are read once (the weight from L1 or L2 after the first rows), h and y written once.  A CTA ends with its row or rows:
+// the loads of the next CTAs cover the latency of this one's sum.
+template <int XT, int RT, bool VECTOR, int NU>
+__global__ void __launch_bounds__(kTeamWarps * 32)
+k_rms_team(const RmsArgs a, int64_t rows, int team_warps)
+{
+    using L = Lanes<XT, VECTOR>;
+    constexpr int XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2;
+    __shared__ float red[kTeamWarps];
+    __shared__ uint32_t red_most[kTeamWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
+    const int width = (int)a.width;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / 32 / team_warps) + team;
+    const bool here = row < rows;
+    const int in = here ? width : 0;                 // a team without a row loads nothing and stays for the barriers
+    float h[NU][L::E], w[NU][L::E];
+    const char* xr = static_cast<const char*>(a.x) + row * a.x_stride * XS;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) load_unit<XT, L, VECTOR>(h[u], xr, unit0 + u, lane, in);
+    if (a.r) {
+        const char* rr = static_cast<const char*>(a.r) + row * a.r_stride * RS;
+        float r[NU][L::E];
+#pragma unroll
+        for (int u = 0; u < NU; ++u) load_unit<RT, L, VECTOR>(r[u], rr, unit0 + u, lane, in);
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int j = 0; j < L::E; ++j) h[u][j] += r[u][j];
+    }
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        if (a.w_type == APMS_GRAD_F32) load_unit<APMS_GRAD_F32, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, in);
+        else load_unit<XT, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, in);
+    }
+    float acc = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < L::E; ++j) acc = fmaf(h[u][j], h[u][j], acc);
+    if (a.r) {
+        char* hr = static_cast<char*>(a.h) + row * a.width * RS;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) store_unit<RT, L, VECTOR>(hr, h[u], unit0 + u, lane, in);
+    }
+    acc = over_team(warp_total(acc), red, team_warps, [](float p, float q) { return p + q; });
+    const float rstd = __frsqrt_rn(acc / (float)width + a.eps);
+    if (here && unit0 == 0 && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < L::E; ++j) h[u][j] = h[u][j] * rstd * w[u][j];
+    if (!a.scales) {
+        char* yr = static_cast<char*>(a.y) + row * a.width * XS;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) store_unit<XT, L, VECTOR>(yr, h[u], unit0 + u, lane, in);
+        return;
+    }
+    uint32_t most[NU];
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        most[u] = 0;
+#pragma unroll
+        for (int j = 0; j < L::E; ++j) most[u] = max(most[u], L::column(unit0 + u, lane, j) < in ? magnitude_bits(h[u][j]) : 0u);
+    }
+    uint8_t* qr = static_cast<uint8_t*>(a.y) + row * a.width;
+    if (a.groups > 1 || a.group != a.width) {        // 128 columns: within a warp
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+#pragma unroll
+            for (int o = L::GROUP_LANES / 2; o > 0; o >>= 1) most[u] = max(most[u], __shfl_xor_sync(0xffffffffu, most[u], o));
+            float scale, inverse;
+            group_scale(most[u], &scale, &inverse);
+            const int c = L::column(unit0 + u, lane, 0);
+            if (lane % L::GROUP_LANES == 0 && c < in) a.scales[row * a.groups + c / 128] = scale;
+#pragma unroll
+            for (int j = 0; j < L::E; ++j) h[u][j] *= inverse;
+            store_unit_e4m3<L, VECTOR>(qr, h[u], unit0 + u, lane, in);
+        }
+    } else {
+        uint32_t m = most[0];
+#pragma unroll
+        for (int u = 1; u < NU; ++u) m = max(m, most[u]);
+        m = over_team(__reduce_max_sync(0xffffffffu, m), red_most, team_warps, [](uint32_t p, uint32_t q) { return max(p, q); });
+        float scale, inverse;
+        group_scale(m, &scale, &inverse);
+        if (here && unit0 == 0 && lane == 0) a.scales[row] = scale;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+#pragma unroll
+            for (int j = 0; j < L::E; ++j) h[u][j] *= inverse;
+            store_unit_e4m3<L, VECTOR>(qr, h[u], unit0 + u, lane, in);
+        }
+    }
+}
+
+// Rows wider than a team's registers hold: one CTA per row, any stride and alignment, read again for each pass.
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_rows(const RmsArgs a)
 {
@@ -136,6 +335,50 @@ k_rms_back_strips(const RmsBackArgs a)
     store_element(a.dw, c, a.w_type, acc);
 }
 
+// Teams of warps for rows of `units` units: as few warps as hold them, NU units each; several rows a CTA where that leaves it below
+// 128 threads.  0 threads: the rows are too wide.
+struct Team { int warps, threads, rows; };
+Team team_for(int64_t units, int nu)
+{
+    Team t = {(int)((units + nu - 1) / nu), 0, 0};
+    if (t.warps > kTeamWarps) return t;
+    t.rows = t.warps >= 4 ? 1 : 4 / t.warps;
+    t.threads = t.warps * t.rows * 32;
+    return t;
+}
+
+template <int XT, int RT, bool VECTOR>
+bool launch_team(const RmsArgs& a, int64_t rows, cudaStream_t stream, cudaError_t* e)
+{
+    using L = Lanes<XT, VECTOR>;
+    constexpr int MOST = 32 / L::E;                  // 32 elements a lane
+    const int64_t units = (a.width + L::UNIT - 1) / L::UNIT;
+    const int nu = units == 1 ? 1 : units == 2 ? 2 : MOST;
+    const Team t = team_for(units, nu);
+    if (!t.threads) return false;
+    const dim3 grid((unsigned)((rows + t.rows - 1) / t.rows));
+    *e = nu == 1 ? launch(k_rms_team<XT, RT, VECTOR, 1>, grid, t.threads, 0, stream, false, a, rows, t.warps)
+       : nu == 2 ? launch(k_rms_team<XT, RT, VECTOR, 2>, grid, t.threads, 0, stream, false, a, rows, t.warps)
+                 : launch(k_rms_team<XT, RT, VECTOR, MOST>, grid, t.threads, 0, stream, false, a, rows, t.warps);
+    return true;
+}
+
+template <bool VECTOR>
+bool launch_rows(const RmsArgs& a, int64_t rows, cudaStream_t stream, cudaError_t* e)
+{
+    const bool wide = a.r && a.r_type == APMS_GRAD_F32;
+    if (a.x_type == APMS_GRAD_F32) return launch_team<APMS_GRAD_F32, APMS_GRAD_F32, VECTOR>(a, rows, stream, e);
+    if (a.x_type == APMS_GRAD_BF16) return wide ? launch_team<APMS_GRAD_BF16, APMS_GRAD_F32, VECTOR>(a, rows, stream, e) : launch_team<APMS_GRAD_BF16, APMS_GRAD_BF16, VECTOR>(a, rows, stream, e);
+    return wide ? launch_team<APMS_GRAD_F16, APMS_GRAD_F32, VECTOR>(a, rows, stream, e) : launch_team<APMS_GRAD_F16, APMS_GRAD_F16, VECTOR>(a, rows, stream, e);
+}
+
+// Every row begins on a 16-byte boundary and holds whole 16-byte pieces.
+bool rows_of_16(const void* p, int64_t stride, int64_t width, int type)
+{
+    const int64_t es = (int64_t)element_size(type);
+    return !p || (((uintptr_t)p & 15u) == 0 && stride * es % 16 == 0 && width * es % 16 == 0);
+}
+
 bool aligned_to(const void* p, int type) { return (uintptr_t)p % element_size(type) == 0; }
 // The statistics stay in the activations' own type or in binary32.
 bool type_pair(int narrow, int wide) { return known_type(narrow) && known_type(wide) && (wide == narrow || wide == APMS_GRAD_F32); }
@@ -169,8 +412,13 @@ apms_status apms_rms_norm(const apms_rms_norm_args* args, void* cuda_stream)
     a.group = g.group ? g.group : g.width;
     a.groups = (g.width + a.group - 1) / a.group;
     a.x_type = g.x_type; a.r_type = g.residual_type; a.w_type = g.weight_type; a.eps = g.eps;
-    k_rms_rows<<<(unsigned)g.rows, kRmsThreads, 0, (cudaStream_t)cuda_stream>>>(a);
-    OPERATOR_CUDA("apms_rms_norm", cudaGetLastError());
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    const bool vector = rows_of_16(a.x, a.x_stride, a.width, a.x_type) && rows_of_16(a.r, a.r_stride, a.width, a.r_type) && rows_of_16(a.w, 0, a.width, a.x_type) &&
+                        rows_of_16(a.h, a.width, a.width, a.x_type) && (a.scales ? ((uintptr_t)a.y & 7u) == 0 && a.width % 8 == 0 : rows_of_16(a.y, a.width, a.width, a.x_type));
+    cudaError_t e = cudaSuccess;
+    if (!(vector ? launch_rows<true>(a, g.rows, stream, &e) : launch_rows<false>(a, g.rows, stream, &e)))
+        e = launch(k_rms_rows, dim3((unsigned)g.rows), kRmsThreads, 0, stream, false, a);
+    OPERATOR_CUDA("apms_rms_norm", e);
     return APMS_OK;
 }
 
