@@ -94,6 +94,27 @@ cudaError_t launch(void (*kernel)(Params...), dim3 grid, unsigned threads, size_
     return cudaLaunchKernelEx(&config, kernel, Params(args)...);
 }
 
+constexpr int kMostDevices = 64;
+struct Resident { std::atomic<int> ctas{0}; };
+
+// How many CTAs of a kernel the current device holds at once (at least one per SM); raises the kernel's limit of dynamic shared memory.
+cudaError_t resident_ctas(Resident* known, const void* kernel, int threads, size_t shared, int* ctas)
+{
+    int device = 0, sms = 0, each = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device >= kMostDevices) return cudaErrorInvalidDevice;
+    *ctas = known[device].ctas.load(std::memory_order_relaxed);
+    if (*ctas) return cudaSuccess;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, threads, shared);
+    if (e != cudaSuccess) return e;
+    *ctas = sms * std::max(1, each);
+    known[device].ctas.store(*ctas, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
 inline size_t element_size(int type) { return type == APMS_GRAD_F32 ? 4 : 2; }
 inline bool known_type(int type) { return type == APMS_GRAD_F32 || type == APMS_GRAD_BF16 || type == APMS_GRAD_F16; }
 

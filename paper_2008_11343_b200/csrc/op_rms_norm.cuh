@@ -288,6 +288,193 @@ struct RmsBackArgs {
     int dy_type, h_type, w_type;
 };
 
+// 16 bytes from global to shared memory without a register; both 16-byte aligned.  A thread copies what it reads itself,
+// so its own wait is all the order that is needed.
+__device__ __forceinline__ void copy16_async(const char* to_shared, const char* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to_shared)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
+
+// E elements of TYPE from the 16-byte pieces at p, `stride` bytes apart.
+template <int TYPE, int E>
+__device__ __forceinline__ void unpack_pieces(float* f, const char* p, int stride)
+{
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
+#pragma unroll
+    for (int k = 0; k < E * ES / 16; ++k) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p + k * stride);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (ES == 4) f[4 * k + j] = __uint_as_float(w[j]);
+            else { const float2 g = unpack16<TYPE>(w[j]); f[(8 * k + 2 * j) % E] = g.x; f[(8 * k + 2 * j + 1) % E] = g.y; }
+        }
+    }
+}
+
+// A CTA walks over rows, a team of warps each, and keeps its columns' share of dweight in registers; `partial` gets one row of shares per CTA.
+// The rows' operands come through a ring of STAGES rows in shared memory, each thread copying its own pieces
+// ahead (cp.async: neither registers nor a producer), because one row a CTA in flight at a time would not cover HBM's latency.
+// Rows that are not whole 16-byte pieces are loaded directly.
+template <int XT, int HT, bool VECTOR, int NU>
+struct BackShape {
+    using L = Lanes<XT, VECTOR>;
+    static constexpr int XS = XT == APMS_GRAD_F32 ? 4 : 2, HS = HT == APMS_GRAD_F32 ? 4 : 2;
+    static constexpr int P_DY = VECTOR ? NU * L::E * XS / 16 : 0, P_H = VECTOR ? NU * L::E * HS / 16 : 0, PIECES = P_DY + 2 * P_H;
+    static constexpr int STAGES = PIECES <= 6 ? 4 : PIECES <= 8 ? 3 : PIECES <= 12 ? 2 : 1;      // at most 400 bytes a thread
+    static constexpr int LANE_ELEMENTS = NU * L::E;
+    static constexpr int BYTES_A_THREAD = STAGES * PIECES * 16 > LANE_ELEMENTS * 4 ? STAGES * PIECES * 16 : LANE_ELEMENTS * 4;
+};
+
+template <int XT, int HT, bool VECTOR, int NU, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS)
+k_rms_back_team(const RmsBackArgs a, int team_warps)
+{
+    using S = BackShape<XT, HT, VECTOR, NU>;
+    using L = typename S::L;
+    constexpr int E = L::E, STAGES = S::STAGES, PIECE = 16 * THREADS;
+    extern __shared__ __align__(16) char ring[];
+    __shared__ float red[2][2 * kTeamWarps];         // a spare warp looks behind the last team's
+    allow_next_kernel();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
+    const int teams = THREADS / 32 / team_warps, width = (int)a.width;
+    const bool spare = team >= teams;                // warps behind the last whole team
+    char* mine = ring + threadIdx.x * 16;
+    const int64_t step = (int64_t)gridDim.x * teams;
+    const int64_t row0 = (int64_t)blockIdx.x * teams, row_mine = spare ? a.rows : row0 + team;
+
+    auto fetch = [&](int64_t row, int stage) {
+        if (VECTOR && row < a.rows) {
+            char* to = mine + stage * (S::PIECES * PIECE);
+            const char* dy = static_cast<const char*>(a.dy) + row * a.dy_stride * S::XS;
+            const char* h = static_cast<const char*>(a.h) + row * a.h_stride * S::HS;
+            const char* dh = static_cast<const char*>(a.dh) + row * a.dh_stride * S::HS;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const int c = L::column(unit0 + u, lane, 0);
+                if (c >= width) continue;
+                constexpr int DX = S::P_DY / NU, DH = S::P_H / NU;
+#pragma unroll
+                for (int k = 0; k < DX; ++k) copy16_async(to + (u * DX + k) * PIECE, dy + (int64_t)c * S::XS + 16 * k);
+#pragma unroll
+                for (int k = 0; k < DH; ++k) copy16_async(to + (S::P_DY + u * DH + k) * PIECE, h + (int64_t)c * S::HS + 16 * k);
+                if (a.dh) {
+#pragma unroll
+                    for (int k = 0; k < DH; ++k) copy16_async(to + (S::P_DY + S::P_H + u * DH + k) * PIECE, dh + (int64_t)c * S::HS + 16 * k);
+                }
+            }
+        }
+        if (VECTOR) commit_copies();
+    };
+
+    float w[NU][E], dw[NU][E];
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        if (a.w_type == APMS_GRAD_F32) load_unit<APMS_GRAD_F32, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, spare ? 0 : width);
+        else load_unit<XT, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, spare ? 0 : width);
+#pragma unroll
+        for (int j = 0; j < E; ++j) dw[u][j] = 0.0f;
+    }
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) fetch(row_mine + s * step, s);
+    float rstd = row_mine < a.rows ? a.rstd[row_mine] : 0.0f;
+    int stage = 0, flip = 0;
+    for (int64_t base = row0; base < a.rows; base += step) {           // the same number of rounds for all of the CTA's teams
+        const int64_t row = row_mine + (base - row0);
+        const bool here = row < a.rows;
+        const int in = here ? width : 0;
+        const float next_rstd = row + step < a.rows ? a.rstd[row + step] : 0.0f;
+        if (STAGES == 1) fetch(row, 0); else fetch(row + (STAGES - 1) * step, (stage + STAGES - 1) % STAGES);
+        if (VECTOR) wait_for_copies<STAGES - 1>();
+        const char* from = mine + stage * (S::PIECES * PIECE);
+        const char* dyr = static_cast<const char*>(a.dy) + row * a.dy_stride * S::XS;
+        const char* hr = static_cast<const char*>(a.h) + row * a.h_stride * S::HS;
+        float dy[NU][E], xh[NU][E];
+        float acc = 0.0f;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            if (VECTOR) {
+                unpack_pieces<XT, E>(dy[u], from + u * (S::P_DY / NU) * PIECE, PIECE);
+                unpack_pieces<HT, E>(xh[u], from + (S::P_DY + u * (S::P_H / NU)) * PIECE, PIECE);
+                if (L::column(unit0 + u, lane, 0) >= in) {             // nothing was copied there
+#pragma unroll
+                    for (int j = 0; j < E; ++j) dy[u][j] = xh[u][j] = 0.0f;
+                }
+            } else {
+                load_unit<XT, L, VECTOR>(dy[u], dyr, unit0 + u, lane, in);
+                load_unit<HT, L, VECTOR>(xh[u], hr, unit0 + u, lane, in);
+            }
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                xh[u][j] *= rstd;
+                acc = fmaf(w[u][j] * dy[u][j], xh[u][j], acc);
+            }
+        }
+        const float mean = over_team(warp_total(acc), red[flip], team_warps, [](float p, float q) { return p + q; }) / (float)width;
+        flip ^= 1;                                                     // one barrier a row: the next row's sums go elsewhere
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            float dx[E], dh[E];
+            if (a.dh) {
+                if (VECTOR) unpack_pieces<HT, E>(dh, from + (S::P_DY + S::P_H + u * (S::P_H / NU)) * PIECE, PIECE);
+                else load_unit<HT, L, VECTOR>(dh, static_cast<const char*>(a.dh) + row * a.dh_stride * S::HS, unit0 + u, lane, in);
+            }
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                dw[u][j] = fmaf(dy[u][j], xh[u][j], dw[u][j]);
+                dx[j] = rstd * (w[u][j] * dy[u][j] - xh[u][j] * mean);
+                if (a.dh) dx[j] += dh[j];
+            }
+            store_unit<XT, L, VECTOR>(static_cast<char*>(a.dx) + row * a.width * S::XS, dx, unit0 + u, lane, in);
+            if (a.dr) store_unit<HT, L, VECTOR>(static_cast<char*>(a.dr) + row * a.width * S::HS, dx, unit0 + u, lane, in);
+        }
+        rstd = next_rstd;
+        stage = STAGES == 1 ? 0 : (stage + 1) % STAGES;
+    }
+
+    // the CTA's shares: its teams' in order
+    if (VECTOR) wait_for_copies<0>();
+    __syncthreads();
+    float* shares = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = L::column(unit0 + u, lane, j);
+            if (!spare && c < width) shares[team * width + c] = dw[u][j];
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < width; c += THREADS) {
+        float s = shares[c];
+        for (int t = 1; t < teams; ++t) s += shares[t * width + c];
+        a.partial[(int64_t)blockIdx.x * width + c] = s;
+    }
+}
+
+// dweight from the CTAs' shares: 32 columns a CTA, each of its 32 warps a strip of the shares, the strips in order.
+__global__ void __launch_bounds__(1024)
+k_rms_back_shares(const RmsBackArgs a, int count)
+{
+    __shared__ float strips[32][33];
+    const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const int strip = threadIdx.x >> 5;
+    wait_for_last_kernel();
+    float acc = 0.0f;
+    if (c < a.width) {
+#pragma unroll 4
+        for (int k = strip; k < count; k += 32) acc += a.partial[k * a.width + c];
+    }
+    strips[strip][threadIdx.x & 31] = acc;
+    __syncthreads();
+    if (strip == 0 && c < a.width) {
+        for (int k = 1; k < 32; ++k) acc += strips[k][threadIdx.x & 31];
+        store_element(a.dw, c, a.w_type, acc);
+    }
+}
+
+// Rows wider than a team's registers hold.
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_back_rows(const RmsBackArgs a)
 {
@@ -325,16 +512,6 @@ k_rms_back_weight(const RmsBackArgs a)
     a.partial[blockIdx.y * a.width + c] = acc;
 }
 
-__global__ void __launch_bounds__(kRmsThreads)
-k_rms_back_strips(const RmsBackArgs a)
-{
-    const int64_t c = (int64_t)blockIdx.x * kRmsThreads + threadIdx.x;
-    if (c >= a.width) return;
-    float acc = 0.0f;
-    for (int s = 0; s < kStrips; ++s) acc += a.partial[s * a.width + c];
-    store_element(a.dw, c, a.w_type, acc);
-}
-
 // Teams of warps for rows of `units` units: as few warps as hold them, NU units each; several rows a CTA where that leaves it below
 // 128 threads.  0 threads: the rows are too wide.
 struct Team { int warps, threads, rows; };
@@ -370,6 +547,49 @@ bool launch_rows(const RmsArgs& a, int64_t rows, cudaStream_t stream, cudaError_
     if (a.x_type == APMS_GRAD_F32) return launch_team<APMS_GRAD_F32, APMS_GRAD_F32, VECTOR>(a, rows, stream, e);
     if (a.x_type == APMS_GRAD_BF16) return wide ? launch_team<APMS_GRAD_BF16, APMS_GRAD_F32, VECTOR>(a, rows, stream, e) : launch_team<APMS_GRAD_BF16, APMS_GRAD_BF16, VECTOR>(a, rows, stream, e);
     return wide ? launch_team<APMS_GRAD_F16, APMS_GRAD_F32, VECTOR>(a, rows, stream, e) : launch_team<APMS_GRAD_F16, APMS_GRAD_F16, VECTOR>(a, rows, stream, e);
+}
+
+constexpr int kMostShares = 512;
+
+template <int XT, int HT, bool VECTOR, int NU, int THREADS>
+cudaError_t launch_back(const RmsBackArgs& a, int team_warps, cudaStream_t stream)
+{
+    using S = BackShape<XT, HT, VECTOR, NU>;
+    constexpr size_t shared = (size_t)S::BYTES_A_THREAD * THREADS;
+    auto kernel = k_rms_back_team<XT, HT, VECTOR, NU, THREADS>;
+    static Resident resident[kMostDevices];          // asked once per kernel and device
+    int ctas = 0;
+    cudaError_t e = resident_ctas(resident, reinterpret_cast<const void*>(kernel), THREADS, shared, &ctas);
+    if (e != cudaSuccess) return e;
+    const int teams = THREADS / 32 / team_warps;
+    const int grid = (int)std::min<int64_t>((a.rows + teams - 1) / teams, std::min(kMostShares, ctas));
+    e = launch(kernel, dim3((unsigned)grid), THREADS, shared, stream, false, a, team_warps);
+    if (e != cudaSuccess) return e;
+    return launch(k_rms_back_shares, dim3((unsigned)((a.width + 31) / 32)), 1024, 0, stream, true, a, grid);
+}
+
+// Lane elements: 16 for rows that 8 warps hold so, then 16 warps with 16 and with 32; 8 for the narrowest rows.
+template <int XT, int HT, bool VECTOR>
+bool launch_back_width(const RmsBackArgs& a, cudaStream_t stream, cudaError_t* e)
+{
+    using L = Lanes<XT, VECTOR>;
+    constexpr int N8 = 8 / L::E, N16 = 16 / L::E, N32 = 32 / L::E;
+    const int64_t warps8 = (a.width + 32 * 8 - 1) / (32 * 8), warps16 = (a.width + 32 * 16 - 1) / (32 * 16), warps32 = (a.width + 32 * 32 - 1) / (32 * 32);
+    if (warps8 == 1) *e = launch_back<XT, HT, VECTOR, N8, 256>(a, 1, stream);
+    else if (warps16 <= 8) *e = launch_back<XT, HT, VECTOR, N16, 256>(a, (int)warps16, stream);
+    else if (warps16 <= 16) *e = launch_back<XT, HT, VECTOR, N16, 512>(a, (int)warps16, stream);
+    else if (warps32 <= 16) *e = launch_back<XT, HT, VECTOR, N32, 512>(a, (int)warps32, stream);
+    else return false;
+    return true;
+}
+
+template <bool VECTOR>
+bool launch_back_rows(const RmsBackArgs& a, cudaStream_t stream, cudaError_t* e)
+{
+    const bool wide = a.h_type == APMS_GRAD_F32;
+    if (a.dy_type == APMS_GRAD_F32) return launch_back_width<APMS_GRAD_F32, APMS_GRAD_F32, VECTOR>(a, stream, e);
+    if (a.dy_type == APMS_GRAD_BF16) return wide ? launch_back_width<APMS_GRAD_BF16, APMS_GRAD_F32, VECTOR>(a, stream, e) : launch_back_width<APMS_GRAD_BF16, APMS_GRAD_BF16, VECTOR>(a, stream, e);
+    return wide ? launch_back_width<APMS_GRAD_F16, APMS_GRAD_F32, VECTOR>(a, stream, e) : launch_back_width<APMS_GRAD_F16, APMS_GRAD_F16, VECTOR>(a, stream, e);
 }
 
 // Every row begins on a 16-byte boundary and holds whole 16-byte pieces.
@@ -425,7 +645,7 @@ apms_status apms_rms_norm(const apms_rms_norm_args* args, void* cuda_stream)
 size_t apms_rms_norm_backward_workspace_bytes(int64_t rows, int64_t width)
 {
     if (rows < 0 || rows > kMostRows || width < 1 || width > kMostWidth) return 0;
-    return (size_t)kStrips * (size_t)width * sizeof(float);
+    return (size_t)std::max<int64_t>(kStrips, std::min<int64_t>(rows, kMostShares)) * (size_t)width * sizeof(float);
 }
 
 apms_status apms_rms_norm_backward(const apms_rms_norm_backward_args* args, void* cuda_stream)
@@ -451,15 +671,18 @@ apms_status apms_rms_norm_backward(const apms_rms_norm_backward_args* args, void
     a.partial = (float*)g.workspace_dev;
     a.dy_type = g.dy_type; a.h_type = g.h_type; a.w_type = g.weight_type;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (g.rows) {
-        k_rms_back_rows<<<(unsigned)g.rows, kRmsThreads, 0, stream>>>(a);
-        OPERATOR_CUDA("apms_rms_norm_backward", cudaGetLastError());
+    cudaError_t e = cudaSuccess;
+    const bool vector = rows_of_16(a.dy, a.dy_stride, a.width, a.dy_type) && rows_of_16(a.h, a.h_stride, a.width, a.dy_type) && rows_of_16(a.dh, a.dh_stride, a.width, a.dy_type) &&
+                        rows_of_16(a.w, 0, a.width, a.dy_type) && rows_of_16(a.dx, a.width, a.width, a.dy_type) && rows_of_16(a.dr, a.width, a.width, a.dy_type);
+    if (!g.rows) {
+        e = launch(k_rms_back_shares, dim3((unsigned)((a.width + 31) / 32)), 1024, 0, stream, false, a, 0);
+    } else if (!(vector ? launch_back_rows<true>(a, stream, &e) : launch_back_rows<false>(a, stream, &e))) {
+        e = launch(k_rms_back_rows, dim3((unsigned)g.rows), kRmsThreads, 0, stream, false, a);
+        const unsigned columns = (unsigned)((g.width + kRmsThreads - 1) / kRmsThreads);
+        if (e == cudaSuccess) e = launch(k_rms_back_weight, dim3(columns, kStrips), kRmsThreads, 0, stream, false, a);
+        if (e == cudaSuccess) e = launch(k_rms_back_shares, dim3((unsigned)((a.width + 31) / 32)), 1024, 0, stream, false, a, kStrips);
     }
-    const unsigned columns = (unsigned)((g.width + kRmsThreads - 1) / kRmsThreads);
-    k_rms_back_weight<<<dim3(columns, kStrips), kRmsThreads, 0, stream>>>(a);
-    OPERATOR_CUDA("apms_rms_norm_backward", cudaGetLastError());
-    k_rms_back_strips<<<columns, kRmsThreads, 0, stream>>>(a);
-    OPERATOR_CUDA("apms_rms_norm_backward", cudaGetLastError());
+    OPERATOR_CUDA("apms_rms_norm_backward", e);
     return APMS_OK;
 }
 

@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <algorithm>
+#include <atomic>
 #include <math.h>
 #include <memory>
 #include <new>
