@@ -13,6 +13,8 @@ UNITS = {"apms.cu": lambda f: not f.startswith("op"), "operators.cu": lambda f: 
 HDR = os.path.join(ROOT, "include", "apms.h")
 BUILD = os.path.join(HERE, "_build")                     # objects of the units
 LIB = os.path.join(HERE, "libapms.so")
+EXT = os.path.join(HERE, "_operators.so")                # CPython extension: the operators beside the step on torch tensors
+EXT_SRC = os.path.join(CSRC, "torch_operators.cpp")
 LIB_CHECKED = os.path.join(HERE, "libapms_checked.so")   # the same source with -DAPMS_BOUNDS_CHECK (debugging aid)
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -31,7 +33,20 @@ def _older(out: str, sources: list) -> bool:
 
 
 def is_stale(lib: str = LIB) -> bool:
-    return any(_older(lib, _sources(unit)) for unit in UNITS)
+    return _older(EXT, [HDR, EXT_SRC]) or any(_older(lib, _sources(unit)) for unit in UNITS)
+
+
+def _extension_command(out: str) -> list:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(ROOT, "include"), sysconfig.get_path("include"), os.path.join(cuda, "include"), *cpp_extension.include_paths()]
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *(f"-isystem{d}" for d in include), EXT_SRC, "-o", out, *(f"-L{d}" for d in cpp_extension.library_paths()),
+            "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
@@ -43,6 +58,8 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     extra = ["-DAPMS_BOUNDS_CHECK"] if checked else []
     pid, running, objects = os.getpid(), [], []
+    if not checked and (force or _older(EXT, [HDR, EXT_SRC])):
+        running.append((EXT, subprocess.Popen(_extension_command(f"{EXT}.{pid}"), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for unit in UNITS:
         obj = os.path.join(BUILD, unit.replace(".cu", "_checked.o" if checked else ".o"))
         objects.append(obj)

@@ -26,6 +26,7 @@ U = 2.0 ** -24
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 ROUND = {F32: (2.0 ** -24, 2.0 ** -150), BF16: (2.0 ** -8, 2.0 ** -134), F16: (2.0 ** -11, 2.0 ** -25)}
 EPS = 1e-6
+TYPES = {F32: B.GRAD_F32, BF16: B.GRAD_BF16, F16: B.GRAD_F16}
 
 
 def gen(seed):
@@ -590,7 +591,7 @@ def test_outputs_end_where_they_end():
         def at(t):
             return t.data_ptr() + off * t.element_size()
 
-        tx, tr = O._TYPES[dt], O._TYPES[rt]
+        tx, tr = TYPES[dt], TYPES[rt]
         B.apms_rms_norm(B.RmsNormArgs(rows=rows, width=width, x=x.data_ptr(), x_stride=width, x_type=tx, residual=r.data_ptr(), residual_stride=width,
                                       residual_type=tr, weight=w.data_ptr(), weight_type=tx, eps=EPS, h=at(rooms["h"]), y=at(rooms["y"]),
                                       rstd=at(rstd_room)), stream)

@@ -110,9 +110,9 @@ def test_there_is_no_cpu_path():
 
 
 def test_rows_of_a_tensor():
-    t = torch.empty(6, 10)
-    assert O._rows_of(t) == (60, 60) and O._rows_of(t[:, 2:7]) == (5, 10) and O._rows_of(t[::2, :4]) == (4, 20)
-    assert O._rows_of(torch.empty(0, 3)) == (1, 1) and O._rows_of(torch.empty(2, 3, 8)[:, :, :5]) == (5, 8)
+    t, rows_of = torch.empty(6, 10), O._load().row_layout
+    assert rows_of(t) == (60, 60) and rows_of(t[:, 2:7]) == (5, 10) and rows_of(t[::2, :4]) == (4, 20)
+    assert rows_of(torch.empty(0, 3)) == (1, 1) and rows_of(torch.empty(2, 3, 8)[:, :, :5]) == (5, 8)
     for bad in (t.t(), t[:, ::2], torch.empty(2, 3, 8)[:, :2, :5], torch.empty(1, 4).expand(3, 4)):
         with pytest.raises(ValueError):
-            O._rows_of(bad)
+            rows_of(bad)
