@@ -33,6 +33,32 @@ __device__ __forceinline__ uint32_t pack16(float a, float b)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack16(float2 v) { return pack16<TYPE>(v.x, v.y); }
+
+// Two binary32 operations in one instruction (each half rounded to nearest as the scalar one is).
+__device__ __forceinline__ float2 from_pair(unsigned long long v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ unsigned long long to_pair(float2 a) { unsigned long long r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y)); return r; }
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(to_pair(a)), "l"(to_pair(b)));
+    return from_pair(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(to_pair(a)), "l"(to_pair(b)));
+    return from_pair(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(to_pair(a)), "l"(to_pair(b)), "l"(to_pair(c)));
+    return from_pair(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 // 32 bytes in one access (sm_100's widest); p is 32-byte aligned.
 __device__ __forceinline__ void load32(uint32_t* w, const void* p)
 {
@@ -94,6 +120,7 @@ cudaError_t launch(void (*kernel)(Params...), dim3 grid, unsigned threads, size_
     return cudaLaunchKernelEx(&config, kernel, Params(args)...);
 }
 
+constexpr size_t kMostShared = 220 * 1024;         // of a CTA's dynamic shared memory, with room for a kernel's fixed arrays
 constexpr int kMostDevices = 64;
 struct Resident { std::atomic<int> ctas{0}; };
 

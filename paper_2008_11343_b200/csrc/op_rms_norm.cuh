@@ -4,7 +4,6 @@
 //   h = x + r,  rstd = 1 / sqrt(mean(h^2) + eps),  y = h rstd w                      (per row)
 //   xh = h rstd,  a = w dy,  dx = rstd (a - xh mean(a xh)) + dh,  dw = sum_rows dy xh
 #pragma once
-
 namespace {
 
 constexpr int kRmsThreads = 256;
@@ -23,6 +22,19 @@ struct RmsArgs {
 
 // |v| as bits: ordered like the magnitudes, with infinity and then NaN above every number, so a maximum keeps NaN
 __device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+__device__ __forceinline__ float max_nan(float a, float b)          // NaN where either is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ float warp_most(float v, int lanes)       // over groups of `lanes` lanes
+{
+    for (int o = lanes / 2; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
 
 // A group's scale and what its elements are multiplied by.
 __device__ __forceinline__ void group_scale(uint32_t most_bits, float* scale, float* inverse)
@@ -45,59 +57,68 @@ struct Lanes {
     static __device__ __forceinline__ int column(int unit, int lane, int j) { return unit * UNIT + (VECTOR ? lane * E + j : lane + 32 * j); }
 };
 
-// E elements of type TYPE from column `unit`, 0 behind the width.
-template <int TYPE, class L, bool VECTOR>
-__device__ __forceinline__ void load_unit(float* f, const char* row, int unit, int lane, int width)
+// Elements from the words they lie in, in pairs.
+template <int TYPE, int WORDS>
+__device__ __forceinline__ void unpack_words(float2* f, const uint32_t* w)
 {
-    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
-    if (VECTOR) {
-        const int c = L::column(unit, lane, 0);
-        uint32_t w[L::E * ES / 4];
-        if (c < width) {
+    if (TYPE == APMS_GRAD_F32) {
 #pragma unroll
-            for (int k = 0; k < L::E * ES / 4; k += 4) load16(w + k, row + (int64_t)c * ES + 4 * k);
-        } else {
-#pragma unroll
-            for (int k = 0; k < L::E * ES / 4; ++k) w[k] = 0;
-        }
-#pragma unroll
-        for (int k = 0; k < L::E * ES / 4; ++k) {
-            if (ES == 4) f[k] = __uint_as_float(w[k]);
-            else { const float2 v = unpack16<TYPE>(w[k]); f[(2 * k) % L::E] = v.x; f[(2 * k + 1) % L::E] = v.y; }
-        }
+        for (int k = 0; k < WORDS; k += 2) f[k / 2] = make_float2(__uint_as_float(w[k]), __uint_as_float(w[k + 1]));
     } else {
 #pragma unroll
-        for (int j = 0; j < L::E; ++j) {
-            const int c = L::column(unit, lane, j);
-            f[j] = c < width ? load_element(row, c, TYPE) : 0.0f;
+        for (int k = 0; k < WORDS; ++k) f[k] = unpack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(w[k]);
+    }
+}
+
+// E elements of type TYPE of a unit of the row, in pairs; 0 behind the width.
+template <int TYPE, class L, bool VECTOR>
+__device__ __forceinline__ void load_unit(float2* f, const char* row, int unit, int lane, int width)
+{
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2, WORDS = L::E * ES / 4;
+    if (VECTOR) {
+        const int c = L::column(unit, lane, 0);
+        uint32_t w[WORDS];
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) w[k] = 0;
+        if (c < width) {
+#pragma unroll
+            for (int k = 0; k < WORDS; k += 4) load16(w + k, row + c * ES + 4 * k);
+        }
+        unpack_words<TYPE, WORDS>(f, w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < L::E; j += 2) {
+            const int c = L::column(unit, lane, j), c1 = L::column(unit, lane, j + 1);
+            f[j / 2].x = c < width ? load_element(row, c, TYPE) : 0.0f;
+            f[j / 2].y = c1 < width ? load_element(row, c1, TYPE) : 0.0f;
         }
     }
 }
 
 template <int TYPE, class L, bool VECTOR>
-__device__ __forceinline__ void store_unit(char* row, const float* f, int unit, int lane, int width)
+__device__ __forceinline__ void store_unit(char* row, const float2* f, int unit, int lane, int width)
 {
-    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2, WORDS = L::E * ES / 4;
     if (VECTOR) {
         const int c = L::column(unit, lane, 0);
         if (c >= width) return;
-        uint32_t w[L::E * ES / 4];
+        uint32_t w[WORDS];
 #pragma unroll
-        for (int k = 0; k < L::E * ES / 4; ++k)
-            w[k] = ES == 4 ? __float_as_uint(f[k]) : pack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(f[(2 * k) % L::E], f[(2 * k + 1) % L::E]);
+        for (int k = 0; k < WORDS; ++k)
+            w[k] = ES == 4 ? __float_as_uint(k & 1 ? f[(k / 2) % (L::E / 2)].y : f[(k / 2) % (L::E / 2)].x) : pack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(f[k % (L::E / 2)]);
 #pragma unroll
-        for (int k = 0; k < L::E * ES / 4; k += 4) *reinterpret_cast<uint4*>(row + (int64_t)c * ES + 4 * k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+        for (int k = 0; k < WORDS; k += 4) *reinterpret_cast<uint4*>(row + c * ES + 4 * k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
     } else {
 #pragma unroll
         for (int j = 0; j < L::E; ++j) {
             const int c = L::column(unit, lane, j);
-            if (c < width) store_element(row, c, TYPE, f[j]);
+            if (c < width) store_element(row, c, TYPE, j & 1 ? f[j / 2].y : f[j / 2].x);
         }
     }
 }
 
 template <class L, bool VECTOR>
-__device__ __forceinline__ void store_unit_e4m3(uint8_t* row, const float* f, int unit, int lane, int width)
+__device__ __forceinline__ void store_unit_e4m3(uint8_t* row, const float2* f, int unit, int lane, int width)
 {
     if (VECTOR) {
         const int c = L::column(unit, lane, 0);
@@ -105,15 +126,14 @@ __device__ __forceinline__ void store_unit_e4m3(uint8_t* row, const float* f, in
         uint32_t w[L::E / 4];
 #pragma unroll
         for (int k = 0; k < L::E / 4; ++k)
-            w[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[4 * k], f[4 * k + 1]), __NV_SATFINITE, __NV_E4M3) |
-                   (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[4 * k + 2], f[4 * k + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
+            w[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(f[2 * k], __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(f[2 * k + 1], __NV_SATFINITE, __NV_E4M3) << 16;
         if (L::E == 8) *reinterpret_cast<uint2*>(row + c) = make_uint2(w[0], w[L::E / 4 - 1]);
         else *reinterpret_cast<uint32_t*>(row + c) = w[0];
     } else {
 #pragma unroll
         for (int j = 0; j < L::E; ++j) {
             const int c = L::column(unit, lane, j);
-            if (c < width) row[c] = __nv_cvt_float_to_fp8(f[j], __NV_SATFINITE, __NV_E4M3);
+            if (c < width) row[c] = __nv_cvt_float_to_fp8(j & 1 ? f[j / 2].y : f[j / 2].x, __NV_SATFINITE, __NV_E4M3);
         }
     }
 }
@@ -136,103 +156,328 @@ __device__ __forceinline__ T over_team(T v, T* smem, int team_warps, Op op)
     return v;
 }
 
-// A team of `team_warps` warps a row, NU units a warp, the row in registers from the first load to the last store: x, the residual
-// and the weight are read once (the weight from L1 or L2 after the first rows), h and y written once.  A CTA ends with its row or rows:
-// the loads of the next CTAs cover the latency of this one's sum.
-template <int XT, int RT, bool VECTOR, int NU>
-__global__ void __launch_bounds__(kTeamWarps * 32)
-k_rms_team(const RmsArgs a, int64_t rows, int team_warps)
+// 16 bytes from global to shared memory without a register; both 16-byte aligned.  A thread copies what it reads itself,
+// so its own wait is all the order that is needed.
+__device__ __forceinline__ void copy16_async(const char* to_shared, const char* from)
 {
-    using L = Lanes<XT, VECTOR>;
-    constexpr int XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2;
-    __shared__ float red[kTeamWarps];
-    __shared__ uint32_t red_most[kTeamWarps];
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to_shared)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
+
+// E elements of TYPE, in pairs, from the 16-byte pieces at p, `stride` bytes apart.
+template <int TYPE, int E>
+__device__ __forceinline__ void unpack_pieces(float2* f, const char* p, int stride)
+{
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2, WORDS = E * ES / 4;
+    uint32_t w[WORDS];
+#pragma unroll
+    for (int k = 0; k < WORDS; k += 4) load16(w + k, p + k / 4 * stride);
+    unpack_words<TYPE, WORDS>(f, w);
+}
+
+// copies `bytes` (1 to 16) of the 16, the rest become zeros
+__device__ __forceinline__ void copy16_async(char* to_shared, const char* from, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(to_shared)), "l"(from), "r"(bytes) : "memory");
+}
+
+// A row of `count` elements of ES bytes at p into `room`, by the `threads` threads of a team; where its first element will be.
+template <int ES>
+__device__ __forceinline__ const char* stage_shifted(char* room, const char* p, int count, int t, int threads)
+{
+    const int shift = (int)((uintptr_t)p & 15);
+    const char* from = p - shift;
+    const int bytes = shift + count * ES;            // of the pieces from `from` on
+    const int first = shift ? 1 : 0;
+    if (first && t < (16 - shift) / ES && t < count) {
+        if (ES == 4) reinterpret_cast<uint32_t*>(room + shift)[t] = reinterpret_cast<const uint32_t*>(p)[t];
+        else reinterpret_cast<uint16_t*>(room + shift)[t] = reinterpret_cast<const uint16_t*>(p)[t];
+    }
+    for (int k = first + t; k * 16 < bytes; k += threads) copy16_async(room + k * 16, from + k * 16, min(16, bytes - k * 16));
+    return room + shift;
+}
+
+// What a row's team found in its first reading, over the team (all its threads get it): sum of squares, and with TAKE_MOST the largest magnitude.
+// Every thread of the CTA calls it.
+template <bool TAKE_MOST>
+__device__ __forceinline__ void join_team(float& squares, float& most, int team_warps, float* red, float* red_most)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    squares = warp_total(squares);
+    if (TAKE_MOST) most = warp_most(most, 32);
+    if (team_warps == 1) return;
+    if (lane == 0) { red[warp] = squares; red_most[warp] = most; }
+    __syncthreads();
+    const int at = warp / team_warps * team_warps + lane;
+    squares = warp_total(lane < team_warps ? red[at] : 0.0f);
+    if (TAKE_MOST) most = warp_most(lane < team_warps ? red_most[at] : 0.0f, 32);
+}
+
+// Narrow rows (up to 256 elements of 16 bits, 128 of 32), whole 16-byte pieces: TL lanes a row and R rows a lane, in registers, the weight loaded once for
+// them.  A row a warp left half its lanes without work at 128 columns (a head's width) and 32 bytes a lane in flight.
+template <int XT, int RT, int WT, int TL>
+__global__ void __launch_bounds__(128)
+k_rms_narrow(const RmsArgs a, int64_t rows)
+{
+    using L = Lanes<XT, true>;
+    constexpr int E = L::E, H = E / 2, R = 4, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2;
+    constexpr int GROUP = L::GROUP_LANES < TL ? L::GROUP_LANES : TL;
+    const int lane = threadIdx.x % TL, c = lane * E, width = (int)a.width;
+    const int64_t row0 = ((int64_t)blockIdx.x * (128 / TL) + threadIdx.x / TL) * R;
+    float2 h[R][H], w[H];
+#pragma unroll
+    for (int k = 0; k < R; ++k) load_unit<XT, L, true>(h[k], static_cast<const char*>(a.x) + (row0 + k) * a.x_stride * XS, 0, lane, row0 + k < rows ? width : 0);
+    if (a.r) {
+        float2 r[R][H];
+#pragma unroll
+        for (int k = 0; k < R; ++k) load_unit<RT, L, true>(r[k], static_cast<const char*>(a.r) + (row0 + k) * a.r_stride * RS, 0, lane, row0 + k < rows ? width : 0);
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+#pragma unroll
+            for (int j = 0; j < H; ++j) h[k][j] = add2(h[k][j], r[k][j]);
+    }
+    load_unit<WT, L, true>(w, static_cast<const char*>(a.w), 0, lane, width);
+    const bool row_scale = a.scales && a.group == a.width;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int64_t row = row0 + k;
+        const int in = row < rows ? width : 0;
+        float2 acc = both(0.0f);
+#pragma unroll
+        for (int j = 0; j < H; ++j) acc = fma2(h[k][j], h[k][j], acc);
+        float squares = acc.x + acc.y;
+#pragma unroll
+        for (int o = TL / 2; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
+        const float rstd = __frsqrt_rn(squares / (float)width + a.eps);
+        if (lane == 0 && in) a.rstd[row] = rstd;
+        if (a.r) store_unit<RT, L, true>(static_cast<char*>(a.h) + row * a.width * RS, h[k], 0, lane, in);
+#pragma unroll
+        for (int j = 0; j < H; ++j) h[k][j] = mul2(mul2(h[k][j], both(rstd)), w[j]);
+        if (!a.scales) {
+            store_unit<XT, L, true>(static_cast<char*>(a.y) + row * a.width * XS, h[k], 0, lane, in);
+            continue;
+        }
+        float m = 0.0f, scale, inverse;
+#pragma unroll
+        for (int j = 0; j < H; ++j) m = max_nan(m, max_nan(fabsf(h[k][j].x), fabsf(h[k][j].y)));
+        m = warp_most(c < in ? m : 0.0f, row_scale ? TL : GROUP);
+        group_scale(magnitude_bits(m), &scale, &inverse);
+        if (c < in && lane % (row_scale ? TL : GROUP) == 0) a.scales[row * a.groups + (row_scale ? 0 : c / 128)] = scale;
+#pragma unroll
+        for (int j = 0; j < H; ++j) h[k][j] = mul2(h[k][j], both(inverse));
+        store_unit_e4m3<L, true>(static_cast<uint8_t*>(a.y) + row * a.width, h[k], 0, lane, in);
+    }
+}
+
+// Rows of whole 16-byte pieces, through shared memory: x and the residual are copied there without registers, each thread copying what it
+// reads itself, and read twice - for the sums, and for the outputs.  Little of the row stays in registers, so more of it is in flight on an
+// SM: with the row in registers (binary32 beside the weight) 16384x4096 bfloat16 to 8 bits took 103 us, so 74 us; a CTA ends with its
+// row or rows, the next CTAs' copies cover the latency of its sum (persistent CTAs with a ring of rows: 87 us).
+// The row's 8-bit scale comes from max |h weight|, which the first reading can take: |y| is that times rstd, up to one rounding.
+template <int XT, int RT, int WT, int NU>
+__global__ void __launch_bounds__(kTeamWarps * 32)
+k_rms_staged(const RmsArgs a, int64_t rows, int team_warps)
+{
+    using L = Lanes<XT, true>;
+    constexpr int E = L::E, H = E / 2, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2, WS = WT == APMS_GRAD_F32 ? 4 : 2, DR = E * RS / 16, WORDS = E * WS / 4;
+    extern __shared__ __align__(16) char staged[];
+    __shared__ float red[kTeamWarps], red_most[kTeamWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
-    const int width = (int)a.width;
+    const int piece = 16 * blockDim.x, width = (int)a.width;
     const int64_t row = (int64_t)blockIdx.x * (blockDim.x / 32 / team_warps) + team;
     const bool here = row < rows;
     const int in = here ? width : 0;                 // a team without a row loads nothing and stays for the barriers
-    float h[NU][L::E], w[NU][L::E];
+    char* mine = staged + threadIdx.x * 16;          // a unit's pieces: x, then the residual's
+    const int per_unit = piece * (a.r ? 1 + DR : 1);
     const char* xr = static_cast<const char*>(a.x) + row * a.x_stride * XS;
-#pragma unroll
-    for (int u = 0; u < NU; ++u) load_unit<XT, L, VECTOR>(h[u], xr, unit0 + u, lane, in);
-    if (a.r) {
-        const char* rr = static_cast<const char*>(a.r) + row * a.r_stride * RS;
-        float r[NU][L::E];
-#pragma unroll
-        for (int u = 0; u < NU; ++u) load_unit<RT, L, VECTOR>(r[u], rr, unit0 + u, lane, in);
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-            for (int j = 0; j < L::E; ++j) h[u][j] += r[u][j];
-    }
+    const char* rr = static_cast<const char*>(a.r) + row * a.r_stride * RS;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-        if (a.w_type == APMS_GRAD_F32) load_unit<APMS_GRAD_F32, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, in);
-        else load_unit<XT, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, in);
-    }
-    float acc = 0.0f;
+        const int c = L::column(unit0 + u, lane, 0);
+        char* to = mine + u * per_unit;
+        if (c < in) {
+            copy16_async(to, xr + c * XS);
+            if (a.r) {
 #pragma unroll
-    for (int u = 0; u < NU; ++u)
+                for (int j = 0; j < DR; ++j) copy16_async(to + (1 + j) * piece, rr + c * RS + 16 * j);
+            }
+        } else {                                     // zeros, so that the sums need not ask
+            *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
+            if (a.r) {
 #pragma unroll
-        for (int j = 0; j < L::E; ++j) acc = fmaf(h[u][j], h[u][j], acc);
-    if (a.r) {
-        char* hr = static_cast<char*>(a.h) + row * a.width * RS;
-#pragma unroll
-        for (int u = 0; u < NU; ++u) store_unit<RT, L, VECTOR>(hr, h[u], unit0 + u, lane, in);
-    }
-    acc = over_team(warp_total(acc), red, team_warps, [](float p, float q) { return p + q; });
-    const float rstd = __frsqrt_rn(acc / (float)width + a.eps);
-    if (here && unit0 == 0 && lane == 0) a.rstd[row] = rstd;
-#pragma unroll
-    for (int u = 0; u < NU; ++u)
-#pragma unroll
-        for (int j = 0; j < L::E; ++j) h[u][j] = h[u][j] * rstd * w[u][j];
-    if (!a.scales) {
-        char* yr = static_cast<char*>(a.y) + row * a.width * XS;
-#pragma unroll
-        for (int u = 0; u < NU; ++u) store_unit<XT, L, VECTOR>(yr, h[u], unit0 + u, lane, in);
-        return;
-    }
-    uint32_t most[NU];
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        most[u] = 0;
-#pragma unroll
-        for (int j = 0; j < L::E; ++j) most[u] = max(most[u], L::column(unit0 + u, lane, j) < in ? magnitude_bits(h[u][j]) : 0u);
-    }
-    uint8_t* qr = static_cast<uint8_t*>(a.y) + row * a.width;
-    if (a.groups > 1 || a.group != a.width) {        // 128 columns: within a warp
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-#pragma unroll
-            for (int o = L::GROUP_LANES / 2; o > 0; o >>= 1) most[u] = max(most[u], __shfl_xor_sync(0xffffffffu, most[u], o));
-            float scale, inverse;
-            group_scale(most[u], &scale, &inverse);
-            const int c = L::column(unit0 + u, lane, 0);
-            if (lane % L::GROUP_LANES == 0 && c < in) a.scales[row * a.groups + c / 128] = scale;
-#pragma unroll
-            for (int j = 0; j < L::E; ++j) h[u][j] *= inverse;
-            store_unit_e4m3<L, VECTOR>(qr, h[u], unit0 + u, lane, in);
+                for (int j = 0; j < DR; ++j) *reinterpret_cast<uint4*>(to + (1 + j) * piece) = make_uint4(0, 0, 0, 0);
+            }
         }
-    } else {
-        uint32_t m = most[0];
-#pragma unroll
-        for (int u = 1; u < NU; ++u) m = max(m, most[u]);
-        m = over_team(__reduce_max_sync(0xffffffffu, m), red_most, team_warps, [](uint32_t p, uint32_t q) { return max(p, q); });
-        float scale, inverse;
-        group_scale(m, &scale, &inverse);
-        if (here && unit0 == 0 && lane == 0) a.scales[row] = scale;
+    }
+    commit_copies();
+    uint32_t weight[NU][WORDS];
+    auto load_weight = [&]() {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
+            const int c = L::column(unit0 + u, lane, 0);
 #pragma unroll
-            for (int j = 0; j < L::E; ++j) h[u][j] *= inverse;
-            store_unit_e4m3<L, VECTOR>(qr, h[u], unit0 + u, lane, in);
+            for (int k = 0; k < WORDS; ++k) weight[u][k] = 0;
+            if (c < in) {
+#pragma unroll
+                for (int k = 0; k < WORDS; k += 4) load16(weight[u] + k, static_cast<const char*>(a.w) + c * WS + 4 * k);
+            }
+        }
+    };
+    auto h_of = [&](float2* h, int u) {
+        unpack_pieces<XT, E>(h, mine + u * per_unit, piece);
+        if (a.r) {
+            float2 r[H];
+            unpack_pieces<RT, E>(r, mine + u * per_unit + piece, piece);
+#pragma unroll
+            for (int j = 0; j < H; ++j) h[j] = add2(h[j], r[j]);
+        }
+    };
+    const bool row_scale = a.scales && a.group == a.width;
+    if (row_scale) load_weight();                    // otherwise while the sum is under way
+    wait_for_copies<0>();
+    float2 acc = both(0.0f);
+    float most = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        float2 h[H];
+        h_of(h, u);
+#pragma unroll
+        for (int j = 0; j < H; ++j) acc = fma2(h[j], h[j], acc);
+        if (row_scale) {
+            float2 w[H];
+            unpack_words<WT, WORDS>(w, weight[u]);
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                const float2 v = mul2(h[j], w[j]);
+                most = max_nan(most, max_nan(fabsf(v.x), fabsf(v.y)));
+            }
+        }
+    }
+    if (!row_scale) load_weight();
+    float squares = acc.x + acc.y;
+    if (row_scale) join_team<true>(squares, most, team_warps, red, red_most);
+    else join_team<false>(squares, most, team_warps, red, red_most);
+    const float rstd = __frsqrt_rn(squares / (float)width + a.eps);
+    float scale = 0.0f, inverse = 0.0f;
+    if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
+    if (here && unit0 == 0 && lane == 0) {
+        a.rstd[row] = rstd;
+        if (row_scale) a.scales[row] = scale;
+    }
+    char* hr = static_cast<char*>(a.h) + row * a.width * RS;
+    char* yr = static_cast<char*>(a.y) + row * a.width * (a.scales ? 1 : XS);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        const int c = L::column(unit0 + u, lane, 0);
+        float2 h[H], w[H];
+        unpack_words<WT, WORDS>(w, weight[u]);
+        h_of(h, u);
+        if (a.r) store_unit<RT, L, true>(hr, h, unit0 + u, lane, in);
+#pragma unroll
+        for (int j = 0; j < H; ++j) h[j] = mul2(mul2(h[j], both(rstd)), w[j]);
+        if (!a.scales) {
+            store_unit<XT, L, true>(yr, h, unit0 + u, lane, in);
+            continue;
+        }
+        if (!row_scale) {                            // 128 columns: a warp or half of one
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < H; ++j) m = max_nan(m, max_nan(fabsf(h[j].x), fabsf(h[j].y)));
+            m = warp_most(c < in ? m : 0.0f, L::GROUP_LANES);        // zeros are NaN by now where rstd is infinite or NaN
+            group_scale(magnitude_bits(m), &scale, &inverse);
+            if (lane % L::GROUP_LANES == 0 && c < in) a.scales[row * a.groups + c / 128] = scale;
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) h[j] = mul2(h[j], both(inverse));
+        store_unit_e4m3<L, true>(reinterpret_cast<uint8_t*>(yr), h, unit0 + u, lane, in);
+    }
+}
+
+// Rows that do not start on 16-byte boundaries or hold a ragged number of bytes, through shared memory too: the 16-byte pieces that a row touches are
+// copied as they lie (its first bytes, up to a boundary, by plain loads: what is before them may not be the caller's), and
+// its elements read one by one from there, 32 lanes' consecutive.  Direct 2-byte loads need four times the
+// instructions in flight for the same bytes.
+template <int XT, int RT, int WT, int NU>
+__global__ void __launch_bounds__(kTeamWarps * 32)
+k_rms_shifted(const RmsArgs a, int64_t rows, int team_warps, int x_room, int r_room)
+{
+    using L = Lanes<XT, false>;
+    constexpr int E = L::E, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2;
+    extern __shared__ __align__(16) char staged[];
+    __shared__ float red[kTeamWarps], red_most[kTeamWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
+    const int width = (int)a.width, t = threadIdx.x - team * team_warps * 32, threads = team_warps * 32;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / 32 / team_warps) + team;
+    const bool here = row < rows;
+    const int in = here ? width : 0;
+    char* room = staged + team * (x_room + r_room);
+    const char* xs = stage_shifted<XS>(room, static_cast<const char*>(a.x) + row * a.x_stride * XS, in, t, threads);
+    const char* rs = a.r ? stage_shifted<RS>(room + x_room, static_cast<const char*>(a.r) + row * a.r_stride * RS, in, t, threads) : nullptr;
+    commit_copies();
+    float w[NU][E];
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = L::column(unit0 + u, lane, j);
+            w[u][j] = c < in ? load_element(a.w, c, WT) : 0.0f;
+        }
+    const bool row_scale = a.scales && a.group == a.width;
+    wait_for_copies<0>();
+    __syncthreads();
+    auto h_of = [&](int c) {
+        const float h = load_element(xs, c, XT);
+        return a.r ? h + load_element(rs, c, RT) : h;
+    };
+    float squares = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = L::column(unit0 + u, lane, j);
+            const float h = c < in ? h_of(c) : 0.0f;
+            squares = fmaf(h, h, squares);
+            if (row_scale) most = max_nan(most, fabsf(h * w[u][j]));
+        }
+    join_team<true>(squares, most, team_warps, red, red_most);
+    const float rstd = __frsqrt_rn(squares / (float)width + a.eps);
+    float scale = 0.0f, inverse = 0.0f;
+    if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
+    if (here && unit0 == 0 && lane == 0) {
+        a.rstd[row] = rstd;
+        if (row_scale) a.scales[row] = scale;
+    }
+    char* hr = static_cast<char*>(a.h) + row * a.width * RS;
+    char* yr = static_cast<char*>(a.y) + row * a.width * (a.scales ? 1 : XS);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        float y[E], m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = L::column(unit0 + u, lane, j);
+            const float h = c < in ? h_of(c) : 0.0f;
+            y[j] = h * rstd * w[u][j];
+            if (c < in) {
+                if (a.r) store_element(hr, c, RT, h);
+                if (!a.scales) store_element(yr, c, XT, y[j]);
+                m = max_nan(m, fabsf(y[j]));
+            }
+        }
+        if (!a.scales) continue;
+        if (!row_scale) {
+            group_scale(magnitude_bits(warp_most(m, 32)), &scale, &inverse);
+            if (lane == 0 && (unit0 + u) * L::UNIT < in) a.scales[row * a.groups + unit0 + u] = scale;
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = L::column(unit0 + u, lane, j);
+            if (c < in) reinterpret_cast<uint8_t*>(yr)[c] = __nv_cvt_float_to_fp8(y[j] * inverse, __NV_SATFINITE, __NV_E4M3);
         }
     }
 }
 
-// Rows wider than a team's registers hold: one CTA per row, any stride and alignment, read again for each pass.
+// Rows that do not fit into a CTA's shared memory: one CTA per row, any stride and alignment, read again for each pass.
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_rows(const RmsArgs a)
 {
@@ -287,32 +532,6 @@ struct RmsBackArgs {
     float* partial;
     int dy_type, h_type, w_type;
 };
-
-// 16 bytes from global to shared memory without a register; both 16-byte aligned.  A thread copies what it reads itself,
-// so its own wait is all the order that is needed.
-__device__ __forceinline__ void copy16_async(const char* to_shared, const char* from)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to_shared)), "l"(from) : "memory");
-}
-__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
-
-// E elements of TYPE from the 16-byte pieces at p, `stride` bytes apart.
-template <int TYPE, int E>
-__device__ __forceinline__ void unpack_pieces(float* f, const char* p, int stride)
-{
-    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
-#pragma unroll
-    for (int k = 0; k < E * ES / 16; ++k) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p + k * stride);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (ES == 4) f[4 * k + j] = __uint_as_float(w[j]);
-            else { const float2 g = unpack16<TYPE>(w[j]); f[(8 * k + 2 * j) % E] = g.x; f[(8 * k + 2 * j + 1) % E] = g.y; }
-        }
-    }
-}
 
 // A CTA walks over rows, a team of warps each, and keeps its columns' share of dweight in registers; `partial` gets one row of shares per CTA.
 // The rows' operands come through a ring of STAGES rows in shared memory, each thread copying its own pieces
@@ -369,13 +588,21 @@ k_rms_back_team(const RmsBackArgs a, int team_warps)
         if (VECTOR) commit_copies();
     };
 
-    float w[NU][E], dw[NU][E];
+    constexpr int H = E / 2;                         // pairs a unit
+    float2 w[NU][H], dw[NU][H];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         if (a.w_type == APMS_GRAD_F32) load_unit<APMS_GRAD_F32, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, spare ? 0 : width);
         else load_unit<XT, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, spare ? 0 : width);
 #pragma unroll
-        for (int j = 0; j < E; ++j) dw[u][j] = 0.0f;
+        for (int j = 0; j < H; ++j) dw[u][j] = both(0.0f);
+        if (VECTOR && L::column(unit0 + u, lane, 0) >= width) {        // nothing is ever copied there: zeros for good
+            for (int s = 0; s < STAGES; ++s)
+                for (int k = 0; k < S::PIECES; ++k) {
+                    const int of = k < S::P_DY ? k * NU / (S::P_DY + !VECTOR) : (k - S::P_DY) % (S::P_H + !VECTOR) * NU / (S::P_H + !VECTOR);
+                    if (of == u) *reinterpret_cast<uint4*>(mine + (s * S::PIECES + k) * PIECE) = make_uint4(0, 0, 0, 0);
+                }
+        }
     }
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) fetch(row_mine + s * step, s);
@@ -384,51 +611,53 @@ k_rms_back_team(const RmsBackArgs a, int team_warps)
     for (int64_t base = row0; base < a.rows; base += step) {           // the same number of rounds for all of the CTA's teams
         const int64_t row = row_mine + (base - row0);
         const bool here = row < a.rows;
-        const int in = here ? width : 0;
         const float next_rstd = row + step < a.rows ? a.rstd[row + step] : 0.0f;
         if (STAGES == 1) fetch(row, 0); else fetch(row + (STAGES - 1) * step, (stage + STAGES - 1) % STAGES);
         if (VECTOR) wait_for_copies<STAGES - 1>();
         const char* from = mine + stage * (S::PIECES * PIECE);
-        const char* dyr = static_cast<const char*>(a.dy) + row * a.dy_stride * S::XS;
-        const char* hr = static_cast<const char*>(a.h) + row * a.h_stride * S::HS;
-        float dy[NU][E], xh[NU][E];
-        float acc = 0.0f;
+        float2 dy[NU][H], xh[NU][H];
+        float2 acc = both(0.0f);
+        if (here) {
+            const char* dyr = static_cast<const char*>(a.dy) + row * a.dy_stride * S::XS;
+            const char* hr = static_cast<const char*>(a.h) + row * a.h_stride * S::HS;
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            if (VECTOR) {
-                unpack_pieces<XT, E>(dy[u], from + u * (S::P_DY / NU) * PIECE, PIECE);
-                unpack_pieces<HT, E>(xh[u], from + (S::P_DY + u * (S::P_H / NU)) * PIECE, PIECE);
-                if (L::column(unit0 + u, lane, 0) >= in) {             // nothing was copied there
-#pragma unroll
-                    for (int j = 0; j < E; ++j) dy[u][j] = xh[u][j] = 0.0f;
+            for (int u = 0; u < NU; ++u) {
+                if (VECTOR) {
+                    unpack_pieces<XT, E>(dy[u], from + u * (S::P_DY / NU) * PIECE, PIECE);
+                    unpack_pieces<HT, E>(xh[u], from + (S::P_DY + u * (S::P_H / NU)) * PIECE, PIECE);
+                } else {
+                    load_unit<XT, L, VECTOR>(dy[u], dyr, unit0 + u, lane, width);
+                    load_unit<HT, L, VECTOR>(xh[u], hr, unit0 + u, lane, width);
                 }
-            } else {
-                load_unit<XT, L, VECTOR>(dy[u], dyr, unit0 + u, lane, in);
-                load_unit<HT, L, VECTOR>(xh[u], hr, unit0 + u, lane, in);
             }
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                xh[u][j] *= rstd;
-                acc = fmaf(w[u][j] * dy[u][j], xh[u][j], acc);
-            }
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    xh[u][j] = mul2(xh[u][j], both(rstd));
+                    dw[u][j] = fma2(dy[u][j], xh[u][j], dw[u][j]);
+                    dy[u][j] = mul2(w[u][j], dy[u][j]);                // a = w dy from here on
+                    acc = fma2(dy[u][j], xh[u][j], acc);
+                }
         }
-        const float mean = over_team(warp_total(acc), red[flip], team_warps, [](float p, float q) { return p + q; }) / (float)width;
+        const float mean = over_team(warp_total(acc.x + acc.y), red[flip], team_warps, [](float p, float q) { return p + q; }) / (float)width;
         flip ^= 1;                                                     // one barrier a row: the next row's sums go elsewhere
+        if (here) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            float dx[E], dh[E];
-            if (a.dh) {
-                if (VECTOR) unpack_pieces<HT, E>(dh, from + (S::P_DY + S::P_H + u * (S::P_H / NU)) * PIECE, PIECE);
-                else load_unit<HT, L, VECTOR>(dh, static_cast<const char*>(a.dh) + row * a.dh_stride * S::HS, unit0 + u, lane, in);
-            }
+            for (int u = 0; u < NU; ++u) {
+                float2 dh[H];
+                if (a.dh) {
+                    if (VECTOR) unpack_pieces<HT, E>(dh, from + (S::P_DY + S::P_H + u * (S::P_H / NU)) * PIECE, PIECE);
+                    else load_unit<HT, L, VECTOR>(dh, static_cast<const char*>(a.dh) + row * a.dh_stride * S::HS, unit0 + u, lane, width);
+                }
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                dw[u][j] = fmaf(dy[u][j], xh[u][j], dw[u][j]);
-                dx[j] = rstd * (w[u][j] * dy[u][j] - xh[u][j] * mean);
-                if (a.dh) dx[j] += dh[j];
+                for (int j = 0; j < H; ++j) {
+                    dy[u][j] = mul2(fma2(xh[u][j], both(-mean), dy[u][j]), both(rstd));
+                    if (a.dh) dy[u][j] = add2(dy[u][j], dh[j]);
+                }
+                store_unit<XT, L, VECTOR>(static_cast<char*>(a.dx) + row * a.width * S::XS, dy[u], unit0 + u, lane, width);
+                if (a.dr) store_unit<HT, L, VECTOR>(static_cast<char*>(a.dr) + row * a.width * S::HS, dy[u], unit0 + u, lane, width);
             }
-            store_unit<XT, L, VECTOR>(static_cast<char*>(a.dx) + row * a.width * S::XS, dx, unit0 + u, lane, in);
-            if (a.dr) store_unit<HT, L, VECTOR>(static_cast<char*>(a.dr) + row * a.width * S::HS, dx, unit0 + u, lane, in);
         }
         rstd = next_rstd;
         stage = STAGES == 1 ? 0 : (stage + 1) % STAGES;
@@ -443,7 +672,7 @@ k_rms_back_team(const RmsBackArgs a, int team_warps)
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             const int c = L::column(unit0 + u, lane, j);
-            if (!spare && c < width) shares[team * width + c] = dw[u][j];
+            if (!spare && c < width) shares[team * width + c] = j & 1 ? dw[u][j / 2].y : dw[u][j / 2].x;
         }
     __syncthreads();
     for (int c = threadIdx.x; c < width; c += THREADS) {
@@ -524,29 +753,78 @@ Team team_for(int64_t units, int nu)
     return t;
 }
 
-template <int XT, int RT, bool VECTOR>
-bool launch_team(const RmsArgs& a, int64_t rows, cudaStream_t stream, cudaError_t* e)
+// The kernel of a shape; false: too wide for it.  Elements a lane: so many that about eight 16-byte pieces of x and residual are in flight
+// (bfloat16 with a residual at 16 / 32 / 64 elements: 45.7 / 44.5 / 51 us on 8192x4096, binary32 at 16 / 32: 82.6 / 84.0 us).
+template <int XT, int RT, int WT>
+struct RmsLaunch {
+    static constexpr int XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2;
+
+    template <int TL>
+    static cudaError_t narrow(const RmsArgs& a, int64_t rows, cudaStream_t stream)
+    {
+        const int64_t each = 128 / TL * 4;
+        return launch(k_rms_narrow<XT, RT, WT, TL>, dim3((unsigned)((rows + each - 1) / each)), 128, 0, stream, false, a, rows);
+    }
+
+    template <int NU>
+    static bool staged(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
+    {
+        const Team t = team_for(units, NU);
+        const size_t shared = (size_t)t.threads * NU * 16 * (a.r ? 1 + RS / XS : 1);
+        return t.threads && with_shared<k_rms_staged<XT, RT, WT, NU>>(t, shared, rows, stream, e, a, rows, t.warps);
+    }
+
+    template <int NU>
+    static bool shifted(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
+    {
+        const Team t = team_for(units, NU);
+        const int x_room = (int)((a.width * XS + 15 + 15) / 16 * 16), r_room = a.r ? (int)((a.width * RS + 15 + 15) / 16 * 16) : 0;
+        return t.threads && with_shared<k_rms_shifted<XT, RT, WT, NU>>(t, (size_t)t.rows * (x_room + r_room), rows, stream, e, a, rows, t.warps, x_room, r_room);
+    }
+
+    // KERNEL with as much shared memory as it asks for, within what a CTA can have
+    template <auto KERNEL, class... Args>
+    static bool with_shared(const Team& t, size_t shared, int64_t rows, cudaStream_t stream, cudaError_t* e, const Args&... args)
+    {
+        static Resident resident[kMostDevices];
+        int ctas = 0;
+        if (shared > kMostShared) return false;
+        *e = resident_ctas(resident, reinterpret_cast<const void*>(KERNEL), kTeamWarps * 32, kMostShared, &ctas);
+        if (*e == cudaSuccess) *e = launch(KERNEL, dim3((unsigned)((rows + t.rows - 1) / t.rows)), t.threads, shared, stream, false, args...);
+        return true;
+    }
+
+    static bool rows(const RmsArgs& a, int64_t rows, bool vector, cudaStream_t stream, cudaError_t* e)
+    {
+        if (!vector) {
+            const int units = (int)((a.width + 127) / 128);
+            return units == 1 ? shifted<1>(a, rows, units, stream, e) : units == 2 ? shifted<2>(a, rows, units, stream, e)
+                 : shifted<4>(a, rows, units, stream, e) || shifted<8>(a, rows, units, stream, e) || shifted<16>(a, rows, units, stream, e);
+        }
+        using L = Lanes<XT, true>;
+        const int lanes = (int)((a.width + L::E - 1) / L::E), units = (lanes + 31) / 32;
+        if (lanes <= 32) {
+            *e = lanes <= 8 ? narrow<8>(a, rows, stream) : lanes <= 16 ? narrow<16>(a, rows, stream) : narrow<32>(a, rows, stream);
+            return true;
+        }
+        if (units == 2) return staged<2>(a, rows, units, stream, e);
+        if ((a.r || units <= 4) && staged<4>(a, rows, units, stream, e)) return true;
+        return staged<8>(a, rows, units, stream, e) || staged<16>(a, rows, units, stream, e);
+    }
+};
+
+template <int XT, int RT>
+bool launch_rows(const RmsArgs& a, int64_t rows, bool vector, cudaStream_t stream, cudaError_t* e)
 {
-    using L = Lanes<XT, VECTOR>;
-    constexpr int MOST = 32 / L::E;                  // 32 elements a lane
-    const int64_t units = (a.width + L::UNIT - 1) / L::UNIT;
-    const int nu = units == 1 ? 1 : units == 2 ? 2 : MOST;
-    const Team t = team_for(units, nu);
-    if (!t.threads) return false;
-    const dim3 grid((unsigned)((rows + t.rows - 1) / t.rows));
-    *e = nu == 1 ? launch(k_rms_team<XT, RT, VECTOR, 1>, grid, t.threads, 0, stream, false, a, rows, t.warps)
-       : nu == 2 ? launch(k_rms_team<XT, RT, VECTOR, 2>, grid, t.threads, 0, stream, false, a, rows, t.warps)
-                 : launch(k_rms_team<XT, RT, VECTOR, MOST>, grid, t.threads, 0, stream, false, a, rows, t.warps);
-    return true;
+    return a.w_type == XT ? RmsLaunch<XT, RT, XT>::rows(a, rows, vector, stream, e) : RmsLaunch<XT, RT, APMS_GRAD_F32>::rows(a, rows, vector, stream, e);
 }
 
-template <bool VECTOR>
-bool launch_rows(const RmsArgs& a, int64_t rows, cudaStream_t stream, cudaError_t* e)
+bool launch_rms(const RmsArgs& a, int64_t rows, bool vector, cudaStream_t stream, cudaError_t* e)
 {
     const bool wide = a.r && a.r_type == APMS_GRAD_F32;
-    if (a.x_type == APMS_GRAD_F32) return launch_team<APMS_GRAD_F32, APMS_GRAD_F32, VECTOR>(a, rows, stream, e);
-    if (a.x_type == APMS_GRAD_BF16) return wide ? launch_team<APMS_GRAD_BF16, APMS_GRAD_F32, VECTOR>(a, rows, stream, e) : launch_team<APMS_GRAD_BF16, APMS_GRAD_BF16, VECTOR>(a, rows, stream, e);
-    return wide ? launch_team<APMS_GRAD_F16, APMS_GRAD_F32, VECTOR>(a, rows, stream, e) : launch_team<APMS_GRAD_F16, APMS_GRAD_F16, VECTOR>(a, rows, stream, e);
+    if (a.x_type == APMS_GRAD_F32) return launch_rows<APMS_GRAD_F32, APMS_GRAD_F32>(a, rows, vector, stream, e);
+    if (a.x_type == APMS_GRAD_BF16) return wide ? launch_rows<APMS_GRAD_BF16, APMS_GRAD_F32>(a, rows, vector, stream, e) : launch_rows<APMS_GRAD_BF16, APMS_GRAD_BF16>(a, rows, vector, stream, e);
+    return wide ? launch_rows<APMS_GRAD_F16, APMS_GRAD_F32>(a, rows, vector, stream, e) : launch_rows<APMS_GRAD_F16, APMS_GRAD_F16>(a, rows, vector, stream, e);
 }
 
 constexpr int kMostShares = 512;
@@ -636,7 +914,7 @@ apms_status apms_rms_norm(const apms_rms_norm_args* args, void* cuda_stream)
     const bool vector = rows_of_16(a.x, a.x_stride, a.width, a.x_type) && rows_of_16(a.r, a.r_stride, a.width, a.r_type) && rows_of_16(a.w, 0, a.width, a.x_type) &&
                         rows_of_16(a.h, a.width, a.width, a.x_type) && (a.scales ? ((uintptr_t)a.y & 7u) == 0 && a.width % 8 == 0 : rows_of_16(a.y, a.width, a.width, a.x_type));
     cudaError_t e = cudaSuccess;
-    if (!(vector ? launch_rows<true>(a, g.rows, stream, &e) : launch_rows<false>(a, g.rows, stream, &e)))
+    if (!launch_rms(a, g.rows, vector, stream, &e))
         e = launch(k_rms_rows, dim3((unsigned)g.rows), kRmsThreads, 0, stream, false, a);
     OPERATOR_CUDA("apms_rms_norm", e);
     return APMS_OK;
