@@ -14,6 +14,8 @@ constexpr int kNormThreads = 128;        // 256 bytes a thread (64 to 256 thread
 constexpr int kScaleThreads = 256;       // 128 bytes a thread (with 256 the registers cost more CTAs than the loads bring)
 constexpr int kGroupTiles = 1024;        // consecutive tiles of one tensor whose sums one warp adds up
 constexpr int kTotalThreads = 512;
+constexpr int kAloneTiles = kNormThreads;      // lists this short: the CTA that finishes last adds up
+constexpr int kOneTiles = 8192, kOneThreads = 1024;      // lists this short: one CTA adds up, from shared memory
 constexpr int kListPointers = 500;       // tensors' addresses in a launch's arguments
 
 struct __align__(16) TileRecord {
@@ -30,6 +32,7 @@ struct TensorRecord {
     int32_t type;
     int32_t contiguous;
     int32_t group0, groups;
+    int32_t tile0, tiles;
 };
 struct TensorPointers { const void* p[kListPointers]; };
 
@@ -115,11 +118,40 @@ __device__ __forceinline__ float clip_factor(double squares, float max_norm)
     return (isinf(max_norm) || (float)norm <= max_norm) ? 1.0f : (float)((double)max_norm / norm);
 }
 
-// Sums of squares of the tiles.  A CTA holds one tile in registers and leaves: nothing
-// is counted and nobody is waited for (a ticket per tile, by which the last CTA would know to finish the sum, kept the CTAs
-// on the SMs for the fence and the atomic's round trip: 256 us instead of 197 us on 1.34 GB).
+struct NormOut {
+    float *norm, *norms;                 // norms may be null
+    float max_norm;
+};
+
+// What the norm kernels end with; `total` valid in thread 0.
+__device__ __forceinline__ void put_norm(const ListMemory& m, const NormOut& out, double total)
+{
+    if (threadIdx.x) return;
+    *out.norm = (float)sqrt(total);
+    *m.factor = clip_factor(total, out.max_norm);
+}
+
+// True in every thread of the CTA that is last to come here; what the others wrote before is then visible to it.
+__device__ __forceinline__ bool last_cta(unsigned* ticket, bool* smem)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        *smem = atomicAdd(ticket, 1u) == gridDim.x - 1;
+        if (*smem) *ticket = 0;
+        __threadfence();
+    }
+    __syncthreads();
+    return *smem;
+}
+
+// Sums of squares of the tiles.  A CTA holds one tile in registers and leaves: nothing is counted and nobody is waited for (a ticket per
+// tile, by which the last CTA would know to add up, kept the CTAs on the SMs for the fence and the atomic's round trip: 256 us
+// instead of 197 us on 1.34 GB).  ALONE: lists of a CTA's worth of tiles or less, where that costs less than a second kernel.
+// All the sums of these kernels run in an order fixed by the list, whoever forms them.
+template <bool ALONE>
 __global__ void __launch_bounds__(kNormThreads)
-k_tile_squares(const __grid_constant__ TensorPointers ptrs, int tensor0, int64_t tile0, const __grid_constant__ ListMemory m)
+k_tile_squares(const __grid_constant__ TensorPointers ptrs, int tensor0, int64_t tile0, const __grid_constant__ ListMemory m, const __grid_constant__ NormOut out)
 {
     __shared__ double red[kNormThreads / 32];
     allow_next_kernel();
@@ -134,12 +166,63 @@ k_tile_squares(const __grid_constant__ TensorPointers ptrs, int tensor0, int64_t
         for (int w = 1; w < kNormThreads / 32; ++w) acc += red[w];
         m.tile_sum[tile0 + blockIdx.x] = acc;
     }
+    if (!ALONE) return;
+    __shared__ double sums[kAloneTiles];
+    __shared__ bool last;
+    int2 mine = make_int2(0, 0);                     // tiles of this thread's first tensor, read before the wait
+    if (threadIdx.x < m.count) mine = make_int2(m.tensors[threadIdx.x].tile0, m.tensors[threadIdx.x].tiles);
+    if (!last_cta(m.ticket, &last)) return;
+    if (threadIdx.x < gridDim.x) sums[threadIdx.x] = __ldcg(m.tile_sum + threadIdx.x);
+    __syncthreads();
+    double total = 0.0;
+    for (int t = threadIdx.x; t < m.count; t += kNormThreads) {
+        if (t >= kNormThreads) mine = make_int2(m.tensors[t].tile0, m.tensors[t].tiles);
+        double s = 0.0;
+        for (int k = 0; k < mine.y; ++k) s += sums[mine.x + k];
+        if (out.norms) out.norms[t] = (float)sqrt(s);
+        total += s;
+    }
+    put_norm(m, out, block_total(total, red));
 }
 
-// A warp adds the tiles of a group; the CTA that is done last (a ticket each) adds the groups, tensor by tensor, and the tensors.
-// Every sum runs in an order fixed by the list, whoever forms it.
+// Lists of up to 8192 tiles (256 MB): all tile sums come to one CTA's shared memory, a thread adds a tensor's, a warp those of a tensor of many.
+__global__ void __launch_bounds__(kOneThreads)
+k_one_norm(const __grid_constant__ ListMemory m, const __grid_constant__ NormOut out, int tiles)
+{
+    extern __shared__ double sums[];
+    __shared__ double red[kOneThreads / 32];
+    constexpr int FEW = 32;
+    allow_next_kernel();
+    const int lane = threadIdx.x & 31;
+    int2 mine = make_int2(0, 0);                     // tiles of this thread's first tensor
+    if (threadIdx.x < m.count) mine = make_int2(m.tensors[threadIdx.x].tile0, m.tensors[threadIdx.x].tiles);
+    wait_for_last_kernel();
+#pragma unroll 8
+    for (int k = threadIdx.x; k < tiles; k += kOneThreads) sums[k] = m.tile_sum[k];
+    __syncthreads();
+    double total = 0.0;
+    for (int t0 = 0; t0 < m.count; t0 += kOneThreads) {
+        const int t = t0 + threadIdx.x;
+        if (t0) mine = t < m.count ? make_int2(m.tensors[t].tile0, m.tensors[t].tiles) : make_int2(0, 0);
+        double s = 0.0;
+        if (mine.y <= FEW)
+            for (int k = 0; k < mine.y; ++k) s += sums[mine.x + k];
+        for (unsigned many = __ballot_sync(0xffffffffu, mine.y > FEW); many; many &= many - 1) {        // the warp together
+            const int who = __ffs(many) - 1, first = __shfl_sync(0xffffffffu, mine.x, who), count = __shfl_sync(0xffffffffu, mine.y, who);
+            double part = 0.0;
+            for (int k = lane; k < count; k += 32) part += sums[first + k];
+            part = warp_total(part);
+            if (lane == who) s = part;
+        }
+        if (t < m.count && out.norms) out.norms[t] = (float)sqrt(s);
+        total += s;
+    }
+    put_norm(m, out, block_total(total, red));
+}
+
+// Longer lists: a warp adds the tiles of a group, the CTA that is last (a ticket each) adds the groups, tensor by tensor, and the tensors.
 __global__ void __launch_bounds__(kTotalThreads)
-k_list_norm(const __grid_constant__ ListMemory m, float* __restrict__ norm, float* __restrict__ norms, float max_norm)
+k_list_norm(const __grid_constant__ ListMemory m, const __grid_constant__ NormOut out)
 {
     __shared__ double red[kTotalThreads / 32];
     __shared__ bool last;
@@ -155,52 +238,41 @@ k_list_norm(const __grid_constant__ ListMemory m, float* __restrict__ norm, floa
     for (int k = lane; k < g.tiles; k += 32) acc += m.tile_sum[g.tile0 + k];
     acc = warp_total(acc);
     if (lane == 0 && group < m.groups) m.group_sum[group] = acc;
-    __syncthreads();
-    if (gridDim.x > 1) {
-        if (threadIdx.x == 0) {
-            __threadfence();
-            last = atomicAdd(m.ticket, 1u) == gridDim.x - 1;
-            __threadfence();
-        }
-        __syncthreads();
-        if (!last) return;
-        if (threadIdx.x == 0) *m.ticket = 0;
-    }
+    if (!last_cta(m.ticket, &last)) return;
     double total = 0.0;
     for (int k = threadIdx.x; k < m.count; k += kTotalThreads) {
+        if (k >= kTotalThreads) { g0 = m.tensors[k].group0; groups = m.tensors[k].groups; }
         double s = 0.0;
 #pragma unroll 8
         for (int j = 0; j < groups; ++j) s += __ldcg(m.group_sum + g0 + j);
-        if (norms) norms[k] = (float)sqrt(s);
+        if (out.norms) out.norms[k] = (float)sqrt(s);
         total += s;
-        if (k + kTotalThreads < m.count) { g0 = m.tensors[k + kTotalThreads].group0; groups = m.tensors[k + kTotalThreads].groups; }
     }
-    total = block_total(total, red);
-    if (threadIdx.x == 0) {
-        *norm = (float)sqrt(total);
-        *m.factor = clip_factor(total, max_norm);
-    }
+    put_norm(m, out, block_total(total, red));
 }
 
-// ELEMENTS (8, or 16 where a 16-bit type is involved: 32 bytes of the narrower type) consecutive elements at p as they lie in
-// memory.  p is 32-byte aligned, or 16-byte aligned, or `shift` bytes behind such a boundary, the same for the whole tile:
-// a shifted read takes the aligned 16-byte pieces around it and puts the bytes together (a thread's last piece is its neighbour's first, so it comes from L1).
+// ELEMENTS consecutive elements at p as they lie in memory: 16 between 16-bit types, 8 where a type is binary32, so that the wider of
+// source and output is 32 bytes a lane.  p is aligned to the piece's bytes, or to 16, or `shift` bytes behind such a boundary,
+// the same for the whole tile: a shifted read takes the aligned 16-byte pieces around it and puts the bytes together (a thread's last
+// piece is its neighbour's first, so it comes from L1).
 template <int TYPE, int ELEMENTS>
 struct Piece {
     static constexpr int WORDS = ELEMENTS * (TYPE == APMS_GRAD_F32 ? 4 : 2) / 4;
     uint32_t w[WORDS];
     __device__ __forceinline__ void load(const char* p, int shift)
     {
-        if (shift == 0 && ((uintptr_t)p & 16) == 0) {
+        if (WORDS == 8 && shift == 0 && ((uintptr_t)p & 16) == 0) {
+            load32(w, p);
+            return;
+        }
+        if (shift == 0) {
 #pragma unroll
-            for (int k = 0; k < WORDS; k += 8) load32(w + k, p + 4 * k);
+            for (int k = 0; k < WORDS; k += 4) load16(w + k, p + 4 * k);
             return;
         }
         uint32_t a[WORDS + 4];
 #pragma unroll
-        for (int k = 0; k < WORDS; k += 4) load16(a + k, p - shift + 4 * k);
-        if (shift) load16(a + WORDS, p - shift + 4 * WORDS);
-        else a[WORDS] = a[WORDS + 1] = a[WORDS + 2] = a[WORDS + 3] = 0;
+        for (int k = 0; k < WORDS + 4; k += 4) load16(a + k, p - shift + 4 * k);
         const int words = shift >> 2, bits = (shift & 3) * 8;
 #pragma unroll
         for (int k = 0; k < WORDS; ++k) {
@@ -217,14 +289,14 @@ struct Piece {
             else { const float2 g = unpack16<TYPE>(w[k]); f[2 * k] = g.x; f[2 * k + 1] = g.y; }
         }
     }
-    // f rounded to TYPE, at a 32-byte aligned p
+    // f rounded to TYPE, at p aligned to the piece's bytes
     static __device__ __forceinline__ void store(char* p, const float* f)
     {
         uint32_t v[WORDS];
 #pragma unroll
         for (int k = 0; k < WORDS; ++k) v[k] = TYPE == APMS_GRAD_F32 ? __float_as_uint(f[k]) : pack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(f[(2 * k) % ELEMENTS], f[(2 * k + 1) % ELEMENTS]);
-#pragma unroll
-        for (int k = 0; k < WORDS; k += 8) store32(p + 4 * k, v + k);
+        if (WORDS == 8) store32(p, v);
+        else *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 };
 
@@ -239,7 +311,7 @@ template <int SRC, int DST>
 __device__ __forceinline__ void scale_tile(const void* tensor, const TensorRecord* tensors, const TileRecord& tile, char* out, const float* factor, bool in_place)
 {
     constexpr int SS = SRC == APMS_GRAD_F32 ? 4 : 2, DS = DST == APMS_GRAD_F32 ? 4 : 2;
-    constexpr int N = SS == 4 && DS == 4 ? 8 : 16, PIECES = kTileBytes / SS / N / kScaleThreads;
+    constexpr int N = SS == 2 && DS == 2 ? 16 : 8, PIECES = kTileBytes / SS / N / kScaleThreads;
     if (!tile.contiguous) {
         const RowWalk walk(tensors[tile.tensor], tile.first);
         const float c = factor_when_ready(factor);
@@ -367,6 +439,8 @@ apms_status apms_tensors_create(apms_tensors** out, int count, const int64_t* nu
             const int64_t tiles = (numel[t] + per_tile - 1) / per_tile;
             if ((int64_t)list->tiles.size() + tiles > 0x7fffffff) return operator_fail(APMS_ERR_INVALID_ARG, "apms_tensors_create: the list is too long");
             r.group0 = (int32_t)list->groups.size();
+            r.tile0 = (int32_t)list->tiles.size();
+            r.tiles = (int32_t)tiles;
             list->tile0.push_back((int)list->tiles.size());
             for (int64_t k = 0; k < tiles; ++k) {
                 if (k % kGroupTiles == 0) list->groups.push_back({(int32_t)list->tiles.size(), (int32_t)std::min<int64_t>(kGroupTiles, tiles - k)});
@@ -457,10 +531,19 @@ cudaError_t over_tiles(const apms_tensors* list, const void* const* tensors_dev,
 
 cudaError_t list_norm(const apms_tensors* list, const void* const* tensors_dev, cudaStream_t stream, float* norm, float* norms, float max_norm)
 {
-    const cudaError_t e = over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares);
+    const NormOut out = {norm, norms, max_norm};
+    const int tiles = (int)list->tiles.size();
+    if (tiles && tiles <= kAloneTiles && list->tensors.size() <= kListPointers) return over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares<true>, out);
+    cudaError_t e = over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares<false>, out);
     if (e != cudaSuccess) return e;
-    const unsigned ctas = std::max(1u, (unsigned)((list->groups.size() + kTotalThreads / 32 - 1) / (kTotalThreads / 32)));
-    return launch(k_list_norm, dim3(ctas), kTotalThreads, 0, stream, !list->tiles.empty(), list->m, norm, norms, max_norm);
+    if (tiles <= kOneTiles) {
+        static Resident resident[kMostDevices];
+        int ctas = 0;
+        e = resident_ctas(resident, reinterpret_cast<const void*>(k_one_norm), kOneThreads, kOneTiles * sizeof(double), &ctas);
+        return e != cudaSuccess ? e : launch(k_one_norm, dim3(1), kOneThreads, tiles * sizeof(double), stream, tiles > 0, list->m, out, tiles);
+    }
+    const unsigned ctas = (unsigned)((list->groups.size() + kTotalThreads / 32 - 1) / (kTotalThreads / 32));
+    return launch(k_list_norm, dim3(ctas), kTotalThreads, 0, stream, true, list->m, out);
 }
 
 }  // namespace
