@@ -105,14 +105,14 @@ __device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepco
 
 // early: the kernel calls wait_for_last_kernel() and the stream's last kernel was launched by the same call of the library.
 template <class... Params, class... Args>
-cudaError_t launch(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t shared, cudaStream_t stream, bool early, const Args&... args)
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, dim3 threads, size_t shared, cudaStream_t stream, bool early, const Args&... args)
 {
     cudaLaunchAttribute attribute = {};
     attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attribute.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t config = {};
     config.gridDim = grid;
-    config.blockDim = dim3(threads);
+    config.blockDim = threads;
     config.dynamicSmemBytes = shared;
     config.stream = stream;
     config.attrs = &attribute;

@@ -17,7 +17,7 @@ struct RmsArgs {
     float *scales, *rstd;
     int64_t group, groups;
     int x_type, r_type, w_type;
-    float eps;
+    float eps, inv_width;
 };
 
 // |v| as bits: ordered like the magnitudes, with infinity and then NaN above every number, so a maximum keeps NaN
@@ -95,45 +95,42 @@ __device__ __forceinline__ void load_unit(float2* f, const char* row, int unit, 
     }
 }
 
+// H pairs as TYPE (rounded once) or as e4m3, at an address aligned to their bytes (16 at most).
+template <int TYPE, int H>
+__device__ __forceinline__ void store_pairs(char* p, const float2* f)
+{
+    if (TYPE == APMS_GRAD_F32) {
+#pragma unroll
+        for (int k = 0; k < H; k += 2) *reinterpret_cast<float4*>(p + 8 * k) = make_float4(f[k].x, f[k].y, f[k + 1].x, f[k + 1].y);
+    } else {
+        constexpr int T = TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE;
+        if (H == 4) *reinterpret_cast<uint4*>(p) = make_uint4(pack16<T>(f[0]), pack16<T>(f[1]), pack16<T>(f[2 % H]), pack16<T>(f[3 % H]));
+        else *reinterpret_cast<uint2*>(p) = make_uint2(pack16<T>(f[0]), pack16<T>(f[1]));
+    }
+}
+template <int H>
+__device__ __forceinline__ void store_e4m3(char* p, const float2* f)
+{
+    uint32_t w[H / 2];
+#pragma unroll
+    for (int k = 0; k < H / 2; ++k)
+        w[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(f[2 * k], __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(f[2 * k + 1], __NV_SATFINITE, __NV_E4M3) << 16;
+    if (H == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[H / 2 - 1]);
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
+}
+
 template <int TYPE, class L, bool VECTOR>
 __device__ __forceinline__ void store_unit(char* row, const float2* f, int unit, int lane, int width)
 {
-    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2, WORDS = L::E * ES / 4;
+    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
     if (VECTOR) {
         const int c = L::column(unit, lane, 0);
-        if (c >= width) return;
-        uint32_t w[WORDS];
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k)
-            w[k] = ES == 4 ? __float_as_uint(k & 1 ? f[(k / 2) % (L::E / 2)].y : f[(k / 2) % (L::E / 2)].x) : pack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(f[k % (L::E / 2)]);
-#pragma unroll
-        for (int k = 0; k < WORDS; k += 4) *reinterpret_cast<uint4*>(row + c * ES + 4 * k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+        if (c < width) store_pairs<TYPE, L::E / 2>(row + c * ES, f);
     } else {
 #pragma unroll
         for (int j = 0; j < L::E; ++j) {
             const int c = L::column(unit, lane, j);
             if (c < width) store_element(row, c, TYPE, j & 1 ? f[j / 2].y : f[j / 2].x);
-        }
-    }
-}
-
-template <class L, bool VECTOR>
-__device__ __forceinline__ void store_unit_e4m3(uint8_t* row, const float2* f, int unit, int lane, int width)
-{
-    if (VECTOR) {
-        const int c = L::column(unit, lane, 0);
-        if (c >= width) return;
-        uint32_t w[L::E / 4];
-#pragma unroll
-        for (int k = 0; k < L::E / 4; ++k)
-            w[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(f[2 * k], __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(f[2 * k + 1], __NV_SATFINITE, __NV_E4M3) << 16;
-        if (L::E == 8) *reinterpret_cast<uint2*>(row + c) = make_uint2(w[0], w[L::E / 4 - 1]);
-        else *reinterpret_cast<uint32_t*>(row + c) = w[0];
-    } else {
-#pragma unroll
-        for (int j = 0; j < L::E; ++j) {
-            const int c = L::column(unit, lane, j);
-            if (c < width) row[c] = __nv_cvt_float_to_fp8(j & 1 ? f[j / 2].y : f[j / 2].x, __NV_SATFINITE, __NV_E4M3);
         }
     }
 }
@@ -161,6 +158,15 @@ __device__ __forceinline__ T over_team(T v, T* smem, int team_warps, Op op)
 __device__ __forceinline__ void copy16_async(const char* to_shared, const char* from)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to_shared)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy16_async(uint32_t to_shared, const char* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to_shared), "l"(from) : "memory");
+}
+__device__ __forceinline__ void put_zeros(uint32_t shared) { asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(shared), "r"(0) : "memory"); }
+__device__ __forceinline__ void load_shared16(uint32_t* w, uint32_t shared)
+{
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(shared) : "memory");
 }
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
@@ -249,7 +255,7 @@ k_rms_narrow(const RmsArgs a, int64_t rows)
         float squares = acc.x + acc.y;
 #pragma unroll
         for (int o = TL / 2; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
-        const float rstd = __frsqrt_rn(squares / (float)width + a.eps);
+        const float rstd = rsqrtf(squares * a.inv_width + a.eps);
         if (lane == 0 && in) a.rstd[row] = rstd;
         if (a.r) store_unit<RT, L, true>(static_cast<char*>(a.h) + row * a.width * RS, h[k], 0, lane, in);
 #pragma unroll
@@ -266,7 +272,7 @@ k_rms_narrow(const RmsArgs a, int64_t rows)
         if (c < in && lane % (row_scale ? TL : GROUP) == 0) a.scales[row * a.groups + (row_scale ? 0 : c / 128)] = scale;
 #pragma unroll
         for (int j = 0; j < H; ++j) h[k][j] = mul2(h[k][j], both(inverse));
-        store_unit_e4m3<L, true>(static_cast<uint8_t*>(a.y) + row * a.width, h[k], 0, lane, in);
+        if (c < in) store_e4m3<H>(static_cast<char*>(a.y) + row * a.width + c, h[k]);
     }
 }
 
@@ -275,122 +281,160 @@ k_rms_narrow(const RmsArgs a, int64_t rows)
 // SM: with the row in registers (binary32 beside the weight) 16384x4096 bfloat16 to 8 bits took 103 us, so 74 us; a CTA ends with its
 // row or rows, the next CTAs' copies cover the latency of its sum (persistent CTAs with a ring of rows: 87 us).
 // The row's 8-bit scale comes from max |h weight|, which the first reading can take: |y| is that times rstd, up to one rounding.
-template <int XT, int RT, int WT, int NU>
+// R rows a team where there are plenty: their sums meet at one barrier, and what a thread does once - indexes, the weight - serves all.
+template <int XT, int RT, int WT, int NU, int R>
 __global__ void __launch_bounds__(kTeamWarps * 32)
-k_rms_staged(const RmsArgs a, int64_t rows, int team_warps)
+k_rms_staged(const RmsArgs a, int64_t rows)
 {
     using L = Lanes<XT, true>;
     constexpr int E = L::E, H = E / 2, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2, WS = WT == APMS_GRAD_F32 ? 4 : 2, DR = E * RS / 16, WORDS = E * WS / 4;
     extern __shared__ __align__(16) char staged[];
-    __shared__ float red[kTeamWarps], red_most[kTeamWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
-    const int piece = 16 * blockDim.x, width = (int)a.width;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / 32 / team_warps) + team;
-    const bool here = row < rows;
-    const int in = here ? width : 0;                 // a team without a row loads nothing and stays for the barriers
-    char* mine = staged + threadIdx.x * 16;          // a unit's pieces: x, then the residual's
-    const int per_unit = piece * (a.r ? 1 + DR : 1);
-    const char* xr = static_cast<const char*>(a.x) + row * a.x_stride * XS;
-    const char* rr = static_cast<const char*>(a.r) + row * a.r_stride * RS;
+    __shared__ float red[2 * R * kTeamWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team_warps = blockDim.x >> 5;
+    const int c0 = warp * (NU * L::UNIT) + lane * E, width = (int)a.width;        // unit u of this lane begins at c0 + u UNIT
+    const int64_t row0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * R;
+    const int threads = blockDim.x * blockDim.y, piece = 16 * threads, per_unit = piece * (a.r ? 1 + DR : 1);
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(staged) + 16 * (threadIdx.y * blockDim.x + threadIdx.x);      // a unit's pieces: x, then the residual's
+    const char* xp = static_cast<const char*>(a.x) + row0 * a.x_stride * XS + c0 * XS;
+    const char* rp = static_cast<const char*>(a.r) + row0 * a.r_stride * RS + c0 * RS;
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        const int c = L::column(unit0 + u, lane, 0);
-        char* to = mine + u * per_unit;
-        if (c < in) {
-            copy16_async(to, xr + c * XS);
-            if (a.r) {
+    for (int k = 0; k < R; ++k) {
+        const int in = row0 + k < rows ? width : 0;                               // a missing row is zeros
 #pragma unroll
-                for (int j = 0; j < DR; ++j) copy16_async(to + (1 + j) * piece, rr + c * RS + 16 * j);
-            }
-        } else {                                     // zeros, so that the sums need not ask
-            *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
-            if (a.r) {
+        for (int u = 0; u < NU; ++u) {
+            const uint32_t to = mine + (k * NU + u) * per_unit;
+            if (c0 + u * L::UNIT < in) {
+                copy16_async(to, xp + u * (L::UNIT * XS));
+                if (a.r) {
 #pragma unroll
-                for (int j = 0; j < DR; ++j) *reinterpret_cast<uint4*>(to + (1 + j) * piece) = make_uint4(0, 0, 0, 0);
+                    for (int j = 0; j < DR; ++j) copy16_async(to + (1 + j) * piece, rp + u * (L::UNIT * RS) + 16 * j);
+                }
+            } else {                                                              // zeros, so that the sums need not ask
+                put_zeros(to);
+                if (a.r) {
+#pragma unroll
+                    for (int j = 0; j < DR; ++j) put_zeros(to + (1 + j) * piece);
+                }
             }
         }
+        xp += a.x_stride * XS;
+        rp += a.r_stride * RS;
     }
     commit_copies();
     uint32_t weight[NU][WORDS];
     auto load_weight = [&]() {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
-            const int c = L::column(unit0 + u, lane, 0);
 #pragma unroll
             for (int k = 0; k < WORDS; ++k) weight[u][k] = 0;
-            if (c < in) {
+            if (c0 + u * L::UNIT < width) {
 #pragma unroll
-                for (int k = 0; k < WORDS; k += 4) load16(weight[u] + k, static_cast<const char*>(a.w) + c * WS + 4 * k);
+                for (int k = 0; k < WORDS; k += 4) load16(weight[u] + k, static_cast<const char*>(a.w) + c0 * WS + u * (L::UNIT * WS) + 4 * k);
             }
         }
     };
-    auto h_of = [&](float2* h, int u) {
-        unpack_pieces<XT, E>(h, mine + u * per_unit, piece);
+    auto h_of = [&](float2* h, int k, int u) {
+        const uint32_t from = mine + (k * NU + u) * per_unit;
+        uint32_t w[E * RS / 4 > 4 ? E * RS / 4 : 4];
+        load_shared16(w, from);
+        unpack_words<XT, E * XS / 4>(h, w);
         if (a.r) {
             float2 r[H];
-            unpack_pieces<RT, E>(r, mine + u * per_unit + piece, piece);
+#pragma unroll
+            for (int j = 0; j < DR; ++j) load_shared16(w + 4 * j, from + (1 + j) * piece);
+            unpack_words<RT, E * RS / 4>(r, w);
 #pragma unroll
             for (int j = 0; j < H; ++j) h[j] = add2(h[j], r[j]);
         }
     };
     const bool row_scale = a.scales && a.group == a.width;
-    if (row_scale) load_weight();                    // otherwise while the sum is under way
+    if (row_scale) load_weight();                    // otherwise while the sums are under way
     wait_for_copies<0>();
-    float2 acc = both(0.0f);
-    float most = 0.0f;
+    float squares[R], most[R];
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        float2 h[H];
-        h_of(h, u);
+    for (int k = 0; k < R; ++k) {
+        float2 acc = both(0.0f);
+        most[k] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < H; ++j) acc = fma2(h[j], h[j], acc);
-        if (row_scale) {
-            float2 w[H];
-            unpack_words<WT, WORDS>(w, weight[u]);
+        for (int u = 0; u < NU; ++u) {
+            float2 h[H];
+            h_of(h, k, u);
 #pragma unroll
-            for (int j = 0; j < H; ++j) {
-                const float2 v = mul2(h[j], w[j]);
-                most = max_nan(most, max_nan(fabsf(v.x), fabsf(v.y)));
+            for (int j = 0; j < H; ++j) acc = fma2(h[j], h[j], acc);
+            if (row_scale) {
+                float2 w[H];
+                unpack_words<WT, WORDS>(w, weight[u]);
+#pragma unroll
+                for (int j = 0; j < H; ++j) {
+                    const float2 v = mul2(h[j], w[j]);
+                    most[k] = max_nan(most[k], max_nan(fabsf(v.x), fabsf(v.y)));
+                }
+            }
+        }
+        squares[k] = acc.x + acc.y;
+    }
+    if (!row_scale) load_weight();
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        squares[k] = warp_total(squares[k]);
+        if (row_scale) most[k] = warp_most(most[k], 32);
+    }
+    if (team_warps > 1) {
+        float* mine_red = red + threadIdx.y * team_warps;
+        if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) { mine_red[2 * k * kTeamWarps + warp] = squares[k]; mine_red[(2 * k + 1) * kTeamWarps + warp] = most[k]; }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            squares[k] = mine_red[2 * k * kTeamWarps];
+            for (int w = 1; w < team_warps; ++w) squares[k] += mine_red[2 * k * kTeamWarps + w];
+            if (row_scale) {
+                most[k] = mine_red[(2 * k + 1) * kTeamWarps];
+                for (int w = 1; w < team_warps; ++w) most[k] = max_nan(most[k], mine_red[(2 * k + 1) * kTeamWarps + w]);
             }
         }
     }
-    if (!row_scale) load_weight();
-    float squares = acc.x + acc.y;
-    if (row_scale) join_team<true>(squares, most, team_warps, red, red_most);
-    else join_team<false>(squares, most, team_warps, red, red_most);
-    const float rstd = __frsqrt_rn(squares / (float)width + a.eps);
-    float scale = 0.0f, inverse = 0.0f;
-    if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
-    if (here && unit0 == 0 && lane == 0) {
-        a.rstd[row] = rstd;
-        if (row_scale) a.scales[row] = scale;
-    }
-    char* hr = static_cast<char*>(a.h) + row * a.width * RS;
-    char* yr = static_cast<char*>(a.y) + row * a.width * (a.scales ? 1 : XS);
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        const int c = L::column(unit0 + u, lane, 0);
-        float2 h[H], w[H];
-        unpack_words<WT, WORDS>(w, weight[u]);
-        h_of(h, u);
-        if (a.r) store_unit<RT, L, true>(hr, h, unit0 + u, lane, in);
-#pragma unroll
-        for (int j = 0; j < H; ++j) h[j] = mul2(mul2(h[j], both(rstd)), w[j]);
-        if (!a.scales) {
-            store_unit<XT, L, true>(yr, h, unit0 + u, lane, in);
-            continue;
+    for (int k = 0; k < R; ++k) {
+        const int64_t row = row0 + k;
+        if (R > 1 && row >= rows) break;
+        const int in = row < rows ? width : 0;
+        const float rstd = rsqrtf(squares[k] * a.inv_width + a.eps);
+        float scale = 0.0f, inverse = 0.0f;
+        if (row_scale) group_scale(magnitude_bits(most[k] * rstd), &scale, &inverse);
+        if (threadIdx.x == 0 && in) {
+            a.rstd[row] = rstd;
+            if (row_scale) a.scales[row] = scale;
         }
-        if (!row_scale) {                            // 128 columns: a warp or half of one
-            float m = 0.0f;
+        char* hr = static_cast<char*>(a.h) + (row * width + c0) * RS;
+        char* yr = static_cast<char*>(a.y) + (row * width + c0) * (a.scales ? 1 : XS);
 #pragma unroll
-            for (int j = 0; j < H; ++j) m = max_nan(m, max_nan(fabsf(h[j].x), fabsf(h[j].y)));
-            m = warp_most(c < in ? m : 0.0f, L::GROUP_LANES);        // zeros are NaN by now where rstd is infinite or NaN
-            group_scale(magnitude_bits(m), &scale, &inverse);
-            if (lane % L::GROUP_LANES == 0 && c < in) a.scales[row * a.groups + c / 128] = scale;
+        for (int u = 0; u < NU; ++u) {
+            const bool inside = c0 + u * L::UNIT < in;
+            float2 h[H], w[H];
+            unpack_words<WT, WORDS>(w, weight[u]);
+            h_of(h, k, u);
+            if (a.r && inside) store_pairs<RT, H>(hr + u * (L::UNIT * RS), h);
+#pragma unroll
+            for (int j = 0; j < H; ++j) h[j] = mul2(mul2(h[j], both(rstd)), w[j]);
+            if (!a.scales) {
+                if (inside) store_pairs<XT, H>(yr + u * (L::UNIT * XS), h);
+                continue;
+            }
+            if (!row_scale) {                        // 128 columns: a warp or half of one
+                float m = 0.0f;
+#pragma unroll
+                for (int j = 0; j < H; ++j) m = max_nan(m, max_nan(fabsf(h[j].x), fabsf(h[j].y)));
+                m = warp_most(inside ? m : 0.0f, L::GROUP_LANES);                 // zeros are NaN by now where rstd is infinite or NaN
+                group_scale(magnitude_bits(m), &scale, &inverse);
+                if (lane % L::GROUP_LANES == 0 && inside) a.scales[row * a.groups + (c0 + u * L::UNIT) / 128] = scale;
+            }
+#pragma unroll
+            for (int j = 0; j < H; ++j) h[j] = mul2(h[j], both(inverse));
+            if (inside) store_e4m3<H>(yr + u * L::UNIT, h);
         }
-#pragma unroll
-        for (int j = 0; j < H; ++j) h[j] = mul2(h[j], both(inverse));
-        store_unit_e4m3<L, true>(reinterpret_cast<uint8_t*>(yr), h, unit0 + u, lane, in);
     }
 }
 
@@ -441,7 +485,7 @@ k_rms_shifted(const RmsArgs a, int64_t rows, int team_warps, int x_room, int r_r
             if (row_scale) most = max_nan(most, fabsf(h * w[u][j]));
         }
     join_team<true>(squares, most, team_warps, red, red_most);
-    const float rstd = __frsqrt_rn(squares / (float)width + a.eps);
+    const float rstd = rsqrtf(squares * a.inv_width + a.eps);
     float scale = 0.0f, inverse = 0.0f;
     if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
     if (here && unit0 == 0 && lane == 0) {
@@ -494,7 +538,7 @@ k_rms_rows(const RmsArgs a)
         const float h = h_of(c);
         acc = fmaf(h, h, acc);
     }
-    const float rstd = __frsqrt_rn(block_total(acc, red) / (float)a.width + a.eps);
+    const float rstd = rsqrtf(block_total(acc, red) * a.inv_width + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
     if (!a.scales) {
         for (int64_t c = threadIdx.x; c < a.width; c += kRmsThreads) {
@@ -753,6 +797,8 @@ Team team_for(int64_t units, int nu)
     return t;
 }
 
+constexpr int kManyRows = 8 * 148;
+
 // The kernel of a shape; false: too wide for it.  Elements a lane: so many that about eight 16-byte pieces of x and residual are in flight
 // (bfloat16 with a residual at 16 / 32 / 64 elements: 45.7 / 44.5 / 51 us on 8192x4096, binary32 at 16 / 32: 82.6 / 84.0 us).
 template <int XT, int RT, int WT>
@@ -766,12 +812,18 @@ struct RmsLaunch {
         return launch(k_rms_narrow<XT, RT, WT, TL>, dim3((unsigned)((rows + each - 1) / each)), 128, 0, stream, false, a, rows);
     }
 
-    template <int NU>
+    template <int NU, int R>
     static bool staged(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
     {
         const Team t = team_for(units, NU);
-        const size_t shared = (size_t)t.threads * NU * 16 * (a.r ? 1 + RS / XS : 1);
-        return t.threads && with_shared<k_rms_staged<XT, RT, WT, NU>>(t, shared, rows, stream, e, a, rows, t.warps);
+        const size_t shared = (size_t)t.threads * R * NU * 16 * (a.r ? 1 + RS / XS : 1);
+        return t.threads && with_shared<k_rms_staged<XT, RT, WT, NU, R>>(dim3(t.warps * 32, t.rows), (rows + t.rows * R - 1) / (t.rows * R), shared, stream, e, a, rows);
+    }
+    // two rows a team where that still leaves every SM four CTAs
+    template <int NU>
+    static bool staged(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
+    {
+        return rows >= (int64_t)kManyRows * team_for(units, NU).rows ? staged<NU, 2>(a, rows, units, stream, e) : staged<NU, 1>(a, rows, units, stream, e);
     }
 
     template <int NU>
@@ -779,18 +831,18 @@ struct RmsLaunch {
     {
         const Team t = team_for(units, NU);
         const int x_room = (int)((a.width * XS + 15 + 15) / 16 * 16), r_room = a.r ? (int)((a.width * RS + 15 + 15) / 16 * 16) : 0;
-        return t.threads && with_shared<k_rms_shifted<XT, RT, WT, NU>>(t, (size_t)t.rows * (x_room + r_room), rows, stream, e, a, rows, t.warps, x_room, r_room);
+        return t.threads && with_shared<k_rms_shifted<XT, RT, WT, NU>>(dim3(t.threads), (rows + t.rows - 1) / t.rows, (size_t)t.rows * (x_room + r_room), stream, e, a, rows, t.warps, x_room, r_room);
     }
 
     // KERNEL with as much shared memory as it asks for, within what a CTA can have
     template <auto KERNEL, class... Args>
-    static bool with_shared(const Team& t, size_t shared, int64_t rows, cudaStream_t stream, cudaError_t* e, const Args&... args)
+    static bool with_shared(dim3 block, int64_t grid, size_t shared, cudaStream_t stream, cudaError_t* e, const Args&... args)
     {
         static Resident resident[kMostDevices];
         int ctas = 0;
         if (shared > kMostShared) return false;
         *e = resident_ctas(resident, reinterpret_cast<const void*>(KERNEL), kTeamWarps * 32, kMostShared, &ctas);
-        if (*e == cudaSuccess) *e = launch(KERNEL, dim3((unsigned)((rows + t.rows - 1) / t.rows)), t.threads, shared, stream, false, args...);
+        if (*e == cudaSuccess) *e = launch(KERNEL, dim3((unsigned)grid), block, shared, stream, false, args...);
         return true;
     }
 
@@ -808,8 +860,7 @@ struct RmsLaunch {
             return true;
         }
         if (units == 2) return staged<2>(a, rows, units, stream, e);
-        if ((a.r || units <= 4) && staged<4>(a, rows, units, stream, e)) return true;
-        return staged<8>(a, rows, units, stream, e) || staged<16>(a, rows, units, stream, e);
+        return staged<4>(a, rows, units, stream, e) || staged<8, 1>(a, rows, units, stream, e) || staged<16, 1>(a, rows, units, stream, e);
     }
 };
 
@@ -909,7 +960,7 @@ apms_status apms_rms_norm(const apms_rms_norm_args* args, void* cuda_stream)
     a.x = g.x; a.r = g.residual; a.w = g.weight; a.h = g.h; a.y = g.y; a.scales = g.scales; a.rstd = g.rstd;
     a.group = g.group ? g.group : g.width;
     a.groups = (g.width + a.group - 1) / a.group;
-    a.x_type = g.x_type; a.r_type = g.residual_type; a.w_type = g.weight_type; a.eps = g.eps;
+    a.x_type = g.x_type; a.r_type = g.residual_type; a.w_type = g.weight_type; a.eps = g.eps; a.inv_width = 1.0f / (float)g.width;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     const bool vector = rows_of_16(a.x, a.x_stride, a.width, a.x_type) && rows_of_16(a.r, a.r_stride, a.width, a.r_type) && rows_of_16(a.w, 0, a.width, a.x_type) &&
                         rows_of_16(a.h, a.width, a.width, a.x_type) && (a.scales ? ((uintptr_t)a.y & 7u) == 0 && a.width % 8 == 0 : rows_of_16(a.y, a.width, a.width, a.x_type));
