@@ -281,44 +281,35 @@ k_rms_narrow(const RmsArgs a, int64_t rows)
 // SM: with the row in registers (binary32 beside the weight) 16384x4096 bfloat16 to 8 bits took 103 us, so 74 us; a CTA ends with its
 // row or rows, the next CTAs' copies cover the latency of its sum (persistent CTAs with a ring of rows: 87 us).
 // The row's 8-bit scale comes from max |h weight|, which the first reading can take: |y| is that times rstd, up to one rounding.
-// R rows a team where there are plenty: their sums meet at one barrier, and what a thread does once - indexes, the weight - serves all.
-template <int XT, int RT, int WT, int NU, int R>
+// RES: with a residual.  Two rows a team, to share the indexes and the weight, were slower (45.1 against 47.0 us): fewer CTAs.
+template <int XT, int RT, int WT, bool RES, int NU>
 __global__ void __launch_bounds__(kTeamWarps * 32)
 k_rms_staged(const RmsArgs a, int64_t rows)
 {
     using L = Lanes<XT, true>;
-    constexpr int E = L::E, H = E / 2, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2, WS = WT == APMS_GRAD_F32 ? 4 : 2, DR = E * RS / 16, WORDS = E * WS / 4;
+    constexpr int E = L::E, H = E / 2, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2, WS = WT == APMS_GRAD_F32 ? 4 : 2;
+    constexpr int DR = RES ? E * RS / 16 : 0, WORDS = E * WS / 4;
     extern __shared__ __align__(16) char staged[];
-    __shared__ float red[2 * R * kTeamWarps];
+    __shared__ float red[2 * kTeamWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team_warps = blockDim.x >> 5;
     const int c0 = warp * (NU * L::UNIT) + lane * E, width = (int)a.width;        // unit u of this lane begins at c0 + u UNIT
-    const int64_t row0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * R;
-    const int threads = blockDim.x * blockDim.y, piece = 16 * threads, per_unit = piece * (a.r ? 1 + DR : 1);
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int in = row < rows ? width : 0;           // a team without a row loads nothing and stays for the barrier
+    const int piece = 16 * blockDim.x * blockDim.y, per_unit = piece * (1 + DR);
     const uint32_t mine = (uint32_t)__cvta_generic_to_shared(staged) + 16 * (threadIdx.y * blockDim.x + threadIdx.x);      // a unit's pieces: x, then the residual's
-    const char* xp = static_cast<const char*>(a.x) + row0 * a.x_stride * XS + c0 * XS;
-    const char* rp = static_cast<const char*>(a.r) + row0 * a.r_stride * RS + c0 * RS;
+    const char* xp = static_cast<const char*>(a.x) + row * a.x_stride * XS + c0 * XS;
+    const char* rp = static_cast<const char*>(a.r) + row * a.r_stride * RS + c0 * RS;
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-        const int in = row0 + k < rows ? width : 0;                               // a missing row is zeros
+    for (int u = 0; u < NU; ++u) {
+        const uint32_t to = mine + u * per_unit;
+        if (c0 + u * L::UNIT < in) {
+            copy16_async(to, xp + u * (L::UNIT * XS));
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const uint32_t to = mine + (k * NU + u) * per_unit;
-            if (c0 + u * L::UNIT < in) {
-                copy16_async(to, xp + u * (L::UNIT * XS));
-                if (a.r) {
+            for (int j = 0; j < DR; ++j) copy16_async(to + (1 + j) * piece, rp + u * (L::UNIT * RS) + 16 * j);
+        } else {                                     // zeros, so that the sums need not ask
 #pragma unroll
-                    for (int j = 0; j < DR; ++j) copy16_async(to + (1 + j) * piece, rp + u * (L::UNIT * RS) + 16 * j);
-                }
-            } else {                                                              // zeros, so that the sums need not ask
-                put_zeros(to);
-                if (a.r) {
-#pragma unroll
-                    for (int j = 0; j < DR; ++j) put_zeros(to + (1 + j) * piece);
-                }
-            }
+            for (int j = 0; j < 1 + DR; ++j) put_zeros(to + j * piece);
         }
-        xp += a.x_stride * XS;
-        rp += a.r_stride * RS;
     }
     commit_copies();
     uint32_t weight[NU][WORDS];
@@ -327,18 +318,18 @@ k_rms_staged(const RmsArgs a, int64_t rows)
         for (int u = 0; u < NU; ++u) {
 #pragma unroll
             for (int k = 0; k < WORDS; ++k) weight[u][k] = 0;
-            if (c0 + u * L::UNIT < width) {
+            if (c0 + u * L::UNIT < in) {
 #pragma unroll
                 for (int k = 0; k < WORDS; k += 4) load16(weight[u] + k, static_cast<const char*>(a.w) + c0 * WS + u * (L::UNIT * WS) + 4 * k);
             }
         }
     };
-    auto h_of = [&](float2* h, int k, int u) {
-        const uint32_t from = mine + (k * NU + u) * per_unit;
-        uint32_t w[E * RS / 4 > 4 ? E * RS / 4 : 4];
+    auto h_of = [&](float2* h, int u) {
+        const uint32_t from = mine + u * per_unit;
+        uint32_t w[8];
         load_shared16(w, from);
         unpack_words<XT, E * XS / 4>(h, w);
-        if (a.r) {
+        if (RES) {
             float2 r[H];
 #pragma unroll
             for (int j = 0; j < DR; ++j) load_shared16(w + 4 * j, from + (1 + j) * piece);
@@ -348,93 +339,90 @@ k_rms_staged(const RmsArgs a, int64_t rows)
         }
     };
     const bool row_scale = a.scales && a.group == a.width;
-    if (row_scale) load_weight();                    // otherwise while the sums are under way
-    wait_for_copies<0>();
-    float squares[R], most[R];
+    float2 acc = both(0.0f);
+    float most = 0.0f;
+    if (row_scale) {
+        load_weight();
+        wait_for_copies<0>();
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-        float2 acc = both(0.0f);
-        most[k] = 0.0f;
+        for (int u = 0; u < NU; ++u) {
+            float2 h[H], w[H];
+            h_of(h, u);
+            unpack_words<WT, WORDS>(w, weight[u]);
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                acc = fma2(h[j], h[j], acc);
+                const float2 v = mul2(h[j], w[j]);
+                most = max_nan(most, max_nan(fabsf(v.x), fabsf(v.y)));
+            }
+        }
+    } else {
+        wait_for_copies<0>();
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             float2 h[H];
-            h_of(h, k, u);
+            h_of(h, u);
 #pragma unroll
             for (int j = 0; j < H; ++j) acc = fma2(h[j], h[j], acc);
-            if (row_scale) {
-                float2 w[H];
-                unpack_words<WT, WORDS>(w, weight[u]);
-#pragma unroll
-                for (int j = 0; j < H; ++j) {
-                    const float2 v = mul2(h[j], w[j]);
-                    most[k] = max_nan(most[k], max_nan(fabsf(v.x), fabsf(v.y)));
-                }
-            }
         }
-        squares[k] = acc.x + acc.y;
+        load_weight();                               // while the sums are under way
     }
-    if (!row_scale) load_weight();
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-        squares[k] = warp_total(squares[k]);
-        if (row_scale) most[k] = warp_most(most[k], 32);
-    }
+    float squares = warp_total(acc.x + acc.y);
+    if (row_scale) most = warp_most(most, 32);
     if (team_warps > 1) {
-        float* mine_red = red + threadIdx.y * team_warps;
-        if (lane == 0) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) { mine_red[2 * k * kTeamWarps + warp] = squares[k]; mine_red[(2 * k + 1) * kTeamWarps + warp] = most[k]; }
-        }
+        float* team = red + threadIdx.y * team_warps;
+        if (lane == 0) { team[warp] = squares; team[kTeamWarps + warp] = most; }
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            squares[k] = mine_red[2 * k * kTeamWarps];
-            for (int w = 1; w < team_warps; ++w) squares[k] += mine_red[2 * k * kTeamWarps + w];
-            if (row_scale) {
-                most[k] = mine_red[(2 * k + 1) * kTeamWarps];
-                for (int w = 1; w < team_warps; ++w) most[k] = max_nan(most[k], mine_red[(2 * k + 1) * kTeamWarps + w]);
-            }
+        squares = team[0];
+        for (int w = 1; w < team_warps; ++w) squares += team[w];
+        if (row_scale) {
+            most = team[kTeamWarps];
+            for (int w = 1; w < team_warps; ++w) most = max_nan(most, team[kTeamWarps + w]);
         }
     }
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-        const int64_t row = row0 + k;
-        if (R > 1 && row >= rows) break;
-        const int in = row < rows ? width : 0;
-        const float rstd = rsqrtf(squares[k] * a.inv_width + a.eps);
-        float scale = 0.0f, inverse = 0.0f;
-        if (row_scale) group_scale(magnitude_bits(most[k] * rstd), &scale, &inverse);
-        if (threadIdx.x == 0 && in) {
-            a.rstd[row] = rstd;
-            if (row_scale) a.scales[row] = scale;
-        }
-        char* hr = static_cast<char*>(a.h) + (row * width + c0) * RS;
-        char* yr = static_cast<char*>(a.y) + (row * width + c0) * (a.scales ? 1 : XS);
+    const float rstd = rsqrtf(squares * a.inv_width + a.eps);
+    float scale = 0.0f, inverse = 0.0f;
+    if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
+    if (threadIdx.x == 0 && in) {
+        a.rstd[row] = rstd;
+        if (row_scale) a.scales[row] = scale;
+    }
+    char* hr = static_cast<char*>(a.h) + (row * width + c0) * RS;
+    char* yr = static_cast<char*>(a.y) + (row * width + c0) * (a.scales ? 1 : XS);
+    if (!a.scales) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
-            const bool inside = c0 + u * L::UNIT < in;
             float2 h[H], w[H];
             unpack_words<WT, WORDS>(w, weight[u]);
-            h_of(h, k, u);
-            if (a.r && inside) store_pairs<RT, H>(hr + u * (L::UNIT * RS), h);
+            h_of(h, u);
+            const bool inside = c0 + u * L::UNIT < in;
+            if (RES && inside) store_pairs<RT, H>(hr + u * (L::UNIT * RS), h);
 #pragma unroll
             for (int j = 0; j < H; ++j) h[j] = mul2(mul2(h[j], both(rstd)), w[j]);
-            if (!a.scales) {
-                if (inside) store_pairs<XT, H>(yr + u * (L::UNIT * XS), h);
-                continue;
-            }
-            if (!row_scale) {                        // 128 columns: a warp or half of one
-                float m = 0.0f;
-#pragma unroll
-                for (int j = 0; j < H; ++j) m = max_nan(m, max_nan(fabsf(h[j].x), fabsf(h[j].y)));
-                m = warp_most(inside ? m : 0.0f, L::GROUP_LANES);                 // zeros are NaN by now where rstd is infinite or NaN
-                group_scale(magnitude_bits(m), &scale, &inverse);
-                if (lane % L::GROUP_LANES == 0 && inside) a.scales[row * a.groups + (c0 + u * L::UNIT) / 128] = scale;
-            }
-#pragma unroll
-            for (int j = 0; j < H; ++j) h[j] = mul2(h[j], both(inverse));
-            if (inside) store_e4m3<H>(yr + u * L::UNIT, h);
+            if (inside) store_pairs<XT, H>(yr + u * (L::UNIT * XS), h);
         }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        const bool inside = c0 + u * L::UNIT < in;
+        float2 h[H], w[H];
+        unpack_words<WT, WORDS>(w, weight[u]);
+        h_of(h, u);
+        if (RES && inside) store_pairs<RT, H>(hr + u * (L::UNIT * RS), h);
+#pragma unroll
+        for (int j = 0; j < H; ++j) h[j] = mul2(mul2(h[j], both(rstd)), w[j]);
+        if (!row_scale) {                            // 128 columns: a warp or half of one
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < H; ++j) m = max_nan(m, max_nan(fabsf(h[j].x), fabsf(h[j].y)));
+            m = warp_most(inside ? m : 0.0f, L::GROUP_LANES);                     // zeros are NaN by now where rstd is infinite or NaN
+            group_scale(magnitude_bits(m), &scale, &inverse);
+            if (lane % L::GROUP_LANES == 0 && inside) a.scales[row * a.groups + (c0 + u * L::UNIT) / 128] = scale;
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) h[j] = mul2(h[j], both(inverse));
+        if (inside) store_e4m3<H>(yr + u * L::UNIT, h);
     }
 }
 
@@ -797,8 +785,6 @@ Team team_for(int64_t units, int nu)
     return t;
 }
 
-constexpr int kManyRows = 8 * 148;
-
 // The kernel of a shape; false: too wide for it.  Elements a lane: so many that about eight 16-byte pieces of x and residual are in flight
 // (bfloat16 with a residual at 16 / 32 / 64 elements: 45.7 / 44.5 / 51 us on 8192x4096, binary32 at 16 / 32: 82.6 / 84.0 us).
 template <int XT, int RT, int WT>
@@ -812,18 +798,15 @@ struct RmsLaunch {
         return launch(k_rms_narrow<XT, RT, WT, TL>, dim3((unsigned)((rows + each - 1) / each)), 128, 0, stream, false, a, rows);
     }
 
-    template <int NU, int R>
-    static bool staged(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
-    {
-        const Team t = team_for(units, NU);
-        const size_t shared = (size_t)t.threads * R * NU * 16 * (a.r ? 1 + RS / XS : 1);
-        return t.threads && with_shared<k_rms_staged<XT, RT, WT, NU, R>>(dim3(t.warps * 32, t.rows), (rows + t.rows * R - 1) / (t.rows * R), shared, stream, e, a, rows);
-    }
-    // two rows a team where that still leaves every SM four CTAs
     template <int NU>
     static bool staged(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
     {
-        return rows >= (int64_t)kManyRows * team_for(units, NU).rows ? staged<NU, 2>(a, rows, units, stream, e) : staged<NU, 1>(a, rows, units, stream, e);
+        const Team t = team_for(units, NU);
+        const dim3 block(t.warps * 32, t.rows);
+        const size_t x_bytes = (size_t)t.threads * NU * 16, grid = (rows + t.rows - 1) / std::max(1, t.rows);
+        if (!t.threads) return false;
+        return a.r ? with_shared<k_rms_staged<XT, RT, WT, true, NU>>(block, grid, x_bytes * (1 + RS / XS), stream, e, a, rows)
+                   : with_shared<k_rms_staged<XT, RT, WT, false, NU>>(block, grid, x_bytes, stream, e, a, rows);
     }
 
     template <int NU>
@@ -860,7 +843,7 @@ struct RmsLaunch {
             return true;
         }
         if (units == 2) return staged<2>(a, rows, units, stream, e);
-        return staged<4>(a, rows, units, stream, e) || staged<8, 1>(a, rows, units, stream, e) || staged<16, 1>(a, rows, units, stream, e);
+        return staged<4>(a, rows, units, stream, e) || staged<8>(a, rows, units, stream, e) || staged<16>(a, rows, units, stream, e);
     }
 };
 
