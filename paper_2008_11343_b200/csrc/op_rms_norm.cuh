@@ -137,22 +137,6 @@ __device__ __forceinline__ void store_unit(char* row, const float2* f, int unit,
 
 constexpr int kTeamWarps = 16;                   // a row's at most: with 32 elements a lane, rows of up to 16,384
 
-// Combines a value of each of a team's warps (a row's); TEAM warps of consecutive index.  smem: one T per warp of the CTA.  Every
-// thread of the CTA calls it.
-template <class T, class Op>
-__device__ __forceinline__ T over_team(T v, T* smem, int team_warps, Op op)
-{
-    if (team_warps == 1) return v;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) smem[warp] = v;
-    __syncthreads();
-    const int first = warp / team_warps * team_warps;
-    v = lane < team_warps ? smem[first + lane] : T(0);
-#pragma unroll
-    for (int o = kTeamWarps; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
-
 // 16 bytes from global to shared memory without a register; both 16-byte aligned.  A thread copies what it reads itself,
 // so its own wait is all the order that is needed.
 __device__ __forceinline__ void copy16_async(const char* to_shared, const char* from)
@@ -170,17 +154,6 @@ __device__ __forceinline__ void load_shared16(uint32_t* w, uint32_t shared)
 }
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
-
-// E elements of TYPE, in pairs, from the 16-byte pieces at p, `stride` bytes apart.
-template <int TYPE, int E>
-__device__ __forceinline__ void unpack_pieces(float2* f, const char* p, int stride)
-{
-    constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2, WORDS = E * ES / 4;
-    uint32_t w[WORDS];
-#pragma unroll
-    for (int k = 0; k < WORDS; k += 4) load16(w + k, p + k / 4 * stride);
-    unpack_words<TYPE, WORDS>(f, w);
-}
 
 // copies `bytes` (1 to 16) of the 16, the rest become zeros
 __device__ __forceinline__ void copy16_async(char* to_shared, const char* from, int bytes)
@@ -563,107 +536,137 @@ struct RmsBackArgs {
     void *dx, *dr, *dw;
     float* partial;
     int dy_type, h_type, w_type;
+    float inv_width;
 };
 
 // A CTA walks over rows, a team of warps each, and keeps its columns' share of dweight in registers; `partial` gets one row of shares per CTA.
-// The rows' operands come through a ring of STAGES rows in shared memory, each thread copying its own pieces
-// ahead (cp.async: neither registers nor a producer), because one row a CTA in flight at a time would not cover HBM's latency.
-// Rows that are not whole 16-byte pieces are loaded directly.
+// The rows' operands come through a ring of STAGES rows in shared memory, copied ahead (cp.async: neither registers nor a
+// producer), because one row a CTA in flight at a time would not cover HBM's latency.
+// VECTOR: rows of whole 16-byte pieces; each thread copies what it reads itself, so a row costs one barrier, its sum's.
+// Otherwise the pieces a row touches are copied as they lie, by the team together, and read one element at a time: a barrier more a row.
 template <int XT, int HT, bool VECTOR, int NU>
 struct BackShape {
     using L = Lanes<XT, VECTOR>;
     static constexpr int XS = XT == APMS_GRAD_F32 ? 4 : 2, HS = HT == APMS_GRAD_F32 ? 4 : 2;
-    static constexpr int P_DY = VECTOR ? NU * L::E * XS / 16 : 0, P_H = VECTOR ? NU * L::E * HS / 16 : 0, PIECES = P_DY + 2 * P_H;
-    static constexpr int STAGES = PIECES <= 6 ? 4 : PIECES <= 8 ? 3 : PIECES <= 12 ? 2 : 1;      // at most 400 bytes a thread
-    static constexpr int LANE_ELEMENTS = NU * L::E;
-    static constexpr int BYTES_A_THREAD = STAGES * PIECES * 16 > LANE_ELEMENTS * 4 ? STAGES * PIECES * 16 : LANE_ELEMENTS * 4;
+    static constexpr int P_DY = NU * L::E * XS / 16, P_H = NU * L::E * HS / 16, PIECES = P_DY + 2 * P_H;
+    static constexpr int STAGES = !VECTOR ? 3 : PIECES <= 6 ? 4 : PIECES <= 8 ? 3 : PIECES <= 12 ? 2 : 1;      // at most 400 bytes a thread
 };
 
-template <int XT, int HT, bool VECTOR, int NU, int THREADS>
+template <int XT, int HT, int WT, bool CARRY, bool VECTOR, int NU, int THREADS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS)
-k_rms_back_team(const RmsBackArgs a, int team_warps)
+k_rms_back_team(const RmsBackArgs a, int team_warps, int dy_room, int h_room)
 {
     using S = BackShape<XT, HT, VECTOR, NU>;
     using L = typename S::L;
-    constexpr int E = L::E, STAGES = S::STAGES, PIECE = 16 * THREADS;
+    constexpr int E = L::E, H = E / 2, STAGES = S::STAGES, PIECE = 16 * THREADS, XS = S::XS, HS = S::HS, DX = E * XS / 16, DH = E * HS / 16;
     extern __shared__ __align__(16) char ring[];
-    __shared__ float red[2][2 * kTeamWarps];         // a spare warp looks behind the last team's
+    __shared__ float red[2][kTeamWarps];
     allow_next_kernel();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
-    const int teams = THREADS / 32 / team_warps, width = (int)a.width;
+    const int teams = THREADS / 32 / team_warps, width = (int)a.width, c0 = L::column(unit0, lane, 0);
     const bool spare = team >= teams;                // warps behind the last whole team
-    char* mine = ring + threadIdx.x * 16;
-    const int64_t step = (int64_t)gridDim.x * teams;
-    const int64_t row0 = (int64_t)blockIdx.x * teams, row_mine = spare ? a.rows : row0 + team;
+    const int own = spare ? 0 : width, t = threadIdx.x - team * team_warps * 32;
+    const int stage_bytes = VECTOR ? S::PIECES * PIECE : teams * (dy_room + 2 * h_room);
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    char* const room = ring + team * (dy_room + 2 * h_room);
+    const int64_t step = (int64_t)gridDim.x * teams, row0 = (int64_t)blockIdx.x * teams;
 
-    auto fetch = [&](int64_t row, int stage) {
-        if (VECTOR && row < a.rows) {
-            char* to = mine + stage * (S::PIECES * PIECE);
-            const char* dy = static_cast<const char*>(a.dy) + row * a.dy_stride * S::XS;
-            const char* h = static_cast<const char*>(a.h) + row * a.h_stride * S::HS;
-            const char* dh = static_cast<const char*>(a.dh) + row * a.dh_stride * S::HS;
+    // The next row to fetch, and where its operands begin.
+    int64_t ahead = spare ? a.rows : row0 + team;
+    const char* f_dy = static_cast<const char*>(a.dy) + ahead * a.dy_stride * XS + (VECTOR ? c0 * XS : 0);
+    const char* f_h = static_cast<const char*>(a.h) + ahead * a.h_stride * HS + (VECTOR ? c0 * HS : 0);
+    const char* f_dh = static_cast<const char*>(a.dh) + ahead * a.dh_stride * HS + (VECTOR ? c0 * HS : 0);
+    auto fetch = [&](int stage) {
+        if (ahead < a.rows) {
+            if (VECTOR) {
 #pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                const int c = L::column(unit0 + u, lane, 0);
-                if (c >= width) continue;
-                constexpr int DX = S::P_DY / NU, DH = S::P_H / NU;
+                for (int u = 0; u < NU; ++u) {
+                    if (c0 + u * L::UNIT >= width) continue;
+                    const uint32_t to = mine + stage * stage_bytes;
 #pragma unroll
-                for (int k = 0; k < DX; ++k) copy16_async(to + (u * DX + k) * PIECE, dy + (int64_t)c * S::XS + 16 * k);
+                    for (int k = 0; k < DX; ++k) copy16_async(to + (u * DX + k) * PIECE, f_dy + u * (L::UNIT * XS) + 16 * k);
 #pragma unroll
-                for (int k = 0; k < DH; ++k) copy16_async(to + (S::P_DY + u * DH + k) * PIECE, h + (int64_t)c * S::HS + 16 * k);
-                if (a.dh) {
+                    for (int k = 0; k < DH; ++k) copy16_async(to + (S::P_DY + u * DH + k) * PIECE, f_h + u * (L::UNIT * HS) + 16 * k);
+                    if (CARRY) {
 #pragma unroll
-                    for (int k = 0; k < DH; ++k) copy16_async(to + (S::P_DY + S::P_H + u * DH + k) * PIECE, dh + (int64_t)c * S::HS + 16 * k);
+                        for (int k = 0; k < DH; ++k) copy16_async(to + (S::P_DY + S::P_H + u * DH + k) * PIECE, f_dh + u * (L::UNIT * HS) + 16 * k);
+                    }
                 }
+            } else {
+                char* to = room + stage * stage_bytes;
+                stage_shifted<XS>(to, f_dy, width, t, team_warps * 32);
+                stage_shifted<HS>(to + dy_room, f_h, width, t, team_warps * 32);
+                if (CARRY) stage_shifted<HS>(to + dy_room + h_room, f_dh, width, t, team_warps * 32);
             }
         }
-        if (VECTOR) commit_copies();
+        commit_copies();
+        ahead += step;
+        f_dy += step * a.dy_stride * XS;
+        f_h += step * a.h_stride * HS;
+        if (CARRY) f_dh += step * a.dh_stride * HS;
     };
+    // E elements of one operand of a unit: TYPE, `piece` its first piece of the thread (VECTOR), or the room and the row's address
+    auto operand = [&](auto type, float2* f, int stage, int piece, int room_at, const char* row, int u) {
+        constexpr int TYPE = decltype(type)::value, WORDS = E * (TYPE == APMS_GRAD_F32 ? 4 : 2) / 4;
+        if (VECTOR) {
+            uint32_t w[WORDS];
+#pragma unroll
+            for (int k = 0; k < WORDS; k += 4) load_shared16(w + k, mine + stage * stage_bytes + (piece + u * (WORDS / 4) + k / 4) * PIECE);
+            unpack_words<TYPE, WORDS>(f, w);
+        } else {
+            const char* from = room + stage * stage_bytes + room_at + ((uintptr_t)row & 15);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const int c = L::column(unit0 + u, lane, j);
+                const float v = c < width ? load_element(from, c, TYPE) : 0.0f;
+                if (j & 1) f[j / 2].y = v; else f[j / 2].x = v;
+            }
+        }
+    };
+    using TypeX = std::integral_constant<int, XT>;
+    using TypeH = std::integral_constant<int, HT>;
 
-    constexpr int H = E / 2;                         // pairs a unit
     float2 w[NU][H], dw[NU][H];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-        if (a.w_type == APMS_GRAD_F32) load_unit<APMS_GRAD_F32, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, spare ? 0 : width);
-        else load_unit<XT, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, spare ? 0 : width);
+        load_unit<WT, L, VECTOR>(w[u], static_cast<const char*>(a.w), unit0 + u, lane, own);
 #pragma unroll
         for (int j = 0; j < H; ++j) dw[u][j] = both(0.0f);
-        if (VECTOR && L::column(unit0 + u, lane, 0) >= width) {        // nothing is ever copied there: zeros for good
-            for (int s = 0; s < STAGES; ++s)
-                for (int k = 0; k < S::PIECES; ++k) {
-                    const int of = k < S::P_DY ? k * NU / (S::P_DY + !VECTOR) : (k - S::P_DY) % (S::P_H + !VECTOR) * NU / (S::P_H + !VECTOR);
-                    if (of == u) *reinterpret_cast<uint4*>(mine + (s * S::PIECES + k) * PIECE) = make_uint4(0, 0, 0, 0);
-                }
-        }
     }
+    if (VECTOR && c0 + (NU - 1) * L::UNIT >= own)    // where nothing is ever copied there are zeros for good
+        for (int u = 0; u < NU; ++u)
+            for (int s = 0; s < STAGES && c0 + u * L::UNIT >= own; ++s) {
+                for (int k = 0; k < DX; ++k) put_zeros(mine + s * stage_bytes + (u * DX + k) * PIECE);
+                for (int k = 0; k < DH; ++k) {
+                    put_zeros(mine + s * stage_bytes + (S::P_DY + u * DH + k) * PIECE);
+                    put_zeros(mine + s * stage_bytes + (S::P_DY + S::P_H + u * DH + k) * PIECE);
+                }
+            }
+    int64_t row = ahead;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(row_mine + s * step, s);
-    float rstd = row_mine < a.rows ? a.rstd[row_mine] : 0.0f;
-    int stage = 0, flip = 0;
-    for (int64_t base = row0; base < a.rows; base += step) {           // the same number of rounds for all of the CTA's teams
-        const int64_t row = row_mine + (base - row0);
+    for (int s = 0; s < STAGES - 1; ++s) fetch(s);
+    float rstd = row < a.rows ? a.rstd[row] : 0.0f;
+    int stage = 0, free_stage = STAGES - 1, flip = 0;
+    for (int64_t base = row0; base < a.rows; base += step, row += step) {        // the same number of rounds for all of the CTA's teams
         const bool here = row < a.rows;
         const float next_rstd = row + step < a.rows ? a.rstd[row + step] : 0.0f;
-        if (STAGES == 1) fetch(row, 0); else fetch(row + (STAGES - 1) * step, (stage + STAGES - 1) % STAGES);
-        if (VECTOR) wait_for_copies<STAGES - 1>();
-        const char* from = mine + stage * (S::PIECES * PIECE);
+        if (VECTOR) {
+            fetch(STAGES == 1 ? 0 : free_stage);
+            wait_for_copies<STAGES - 1>();
+        } else {                                     // the row is whole once every thread's copies are; the stage behind it has been read by then
+            wait_for_copies<STAGES - 2 < 0 ? 0 : STAGES - 2>();
+            __syncthreads();
+            fetch(free_stage);
+        }
+        const char* dyr = static_cast<const char*>(a.dy) + row * a.dy_stride * XS;
+        const char* hr = static_cast<const char*>(a.h) + row * a.h_stride * HS;
         float2 dy[NU][H], xh[NU][H];
         float2 acc = both(0.0f);
         if (here) {
-            const char* dyr = static_cast<const char*>(a.dy) + row * a.dy_stride * S::XS;
-            const char* hr = static_cast<const char*>(a.h) + row * a.h_stride * S::HS;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
-                if (VECTOR) {
-                    unpack_pieces<XT, E>(dy[u], from + u * (S::P_DY / NU) * PIECE, PIECE);
-                    unpack_pieces<HT, E>(xh[u], from + (S::P_DY + u * (S::P_H / NU)) * PIECE, PIECE);
-                } else {
-                    load_unit<XT, L, VECTOR>(dy[u], dyr, unit0 + u, lane, width);
-                    load_unit<HT, L, VECTOR>(xh[u], hr, unit0 + u, lane, width);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < NU; ++u)
+                operand(TypeX(), dy[u], stage, 0, 0, dyr, u);
+                operand(TypeH(), xh[u], stage, S::P_DY, dy_room, hr, u);
 #pragma unroll
                 for (int j = 0; j < H; ++j) {
                     xh[u][j] = mul2(xh[u][j], both(rstd));
@@ -671,32 +674,41 @@ k_rms_back_team(const RmsBackArgs a, int team_warps)
                     dy[u][j] = mul2(w[u][j], dy[u][j]);                // a = w dy from here on
                     acc = fma2(dy[u][j], xh[u][j], acc);
                 }
+            }
         }
-        const float mean = over_team(warp_total(acc.x + acc.y), red[flip], team_warps, [](float p, float q) { return p + q; }) / (float)width;
-        flip ^= 1;                                                     // one barrier a row: the next row's sums go elsewhere
+        float mean = warp_total(acc.x + acc.y);
+        if (team_warps > 1) {
+            if (lane == 0) red[flip][warp] = mean;
+            __syncthreads();
+            const float* sums = red[flip] + (spare ? 0 : team * team_warps);
+            mean = sums[0];
+            for (int k = 1; k < team_warps; ++k) mean += sums[k];
+            flip ^= 1;                                                 // one barrier a sum: the next row's go elsewhere
+        }
         if (here) {
+            const float2 minus = both(-mean * a.inv_width), by = both(rstd);
+            char* dxp = static_cast<char*>(a.dx) + row * width * XS;
+            char* drp = static_cast<char*>(a.dr) + row * width * HS;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 float2 dh[H];
-                if (a.dh) {
-                    if (VECTOR) unpack_pieces<HT, E>(dh, from + (S::P_DY + S::P_H + u * (S::P_H / NU)) * PIECE, PIECE);
-                    else load_unit<HT, L, VECTOR>(dh, static_cast<const char*>(a.dh) + row * a.dh_stride * S::HS, unit0 + u, lane, width);
-                }
+                if (CARRY) operand(TypeH(), dh, stage, S::P_DY + S::P_H, dy_room + h_room, static_cast<const char*>(a.dh) + row * a.dh_stride * HS, u);
 #pragma unroll
                 for (int j = 0; j < H; ++j) {
-                    dy[u][j] = mul2(fma2(xh[u][j], both(-mean), dy[u][j]), both(rstd));
-                    if (a.dh) dy[u][j] = add2(dy[u][j], dh[j]);
+                    const float2 inner = fma2(xh[u][j], minus, dy[u][j]);
+                    dy[u][j] = CARRY ? fma2(inner, by, dh[j]) : mul2(inner, by);
                 }
-                store_unit<XT, L, VECTOR>(static_cast<char*>(a.dx) + row * a.width * S::XS, dy[u], unit0 + u, lane, width);
-                if (a.dr) store_unit<HT, L, VECTOR>(static_cast<char*>(a.dr) + row * a.width * S::HS, dy[u], unit0 + u, lane, width);
+                store_unit<XT, L, VECTOR>(dxp, dy[u], unit0 + u, lane, width);
+                if (a.dr) store_unit<HT, L, VECTOR>(drp, dy[u], unit0 + u, lane, width);
             }
         }
         rstd = next_rstd;
-        stage = STAGES == 1 ? 0 : (stage + 1) % STAGES;
+        free_stage = stage;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
 
     // the CTA's shares: its teams' in order
-    if (VECTOR) wait_for_copies<0>();
+    wait_for_copies<0>();
     __syncthreads();
     float* shares = reinterpret_cast<float*>(ring);
 #pragma unroll
@@ -704,12 +716,12 @@ k_rms_back_team(const RmsBackArgs a, int team_warps)
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             const int c = L::column(unit0 + u, lane, j);
-            if (!spare && c < width) shares[team * width + c] = j & 1 ? dw[u][j / 2].y : dw[u][j / 2].x;
+            if (c < own) shares[team * width + c] = j & 1 ? dw[u][j / 2].y : dw[u][j / 2].x;
         }
     __syncthreads();
     for (int c = threadIdx.x; c < width; c += THREADS) {
         float s = shares[c];
-        for (int t = 1; t < teams; ++t) s += shares[t * width + c];
+        for (int k = 1; k < teams; ++k) s += shares[k * width + c];
         a.partial[(int64_t)blockIdx.x * width + c] = s;
     }
 }
@@ -863,45 +875,59 @@ bool launch_rms(const RmsArgs& a, int64_t rows, bool vector, cudaStream_t stream
 
 constexpr int kMostShares = 512;
 
-template <int XT, int HT, bool VECTOR, int NU, int THREADS>
-cudaError_t launch_back(const RmsBackArgs& a, int team_warps, cudaStream_t stream)
+template <int XT, int HT, int WT, bool CARRY, bool VECTOR, int NU, int THREADS>
+bool launch_back(const RmsBackArgs& a, int team_warps, cudaStream_t stream, cudaError_t* e)
 {
     using S = BackShape<XT, HT, VECTOR, NU>;
-    constexpr size_t shared = (size_t)S::BYTES_A_THREAD * THREADS;
-    auto kernel = k_rms_back_team<XT, HT, VECTOR, NU, THREADS>;
+    const int teams = THREADS / 32 / team_warps;
+    const int dy_room = (int)((a.width * S::XS + 15 + 15) / 16 * 16), h_room = (int)((a.width * S::HS + 15 + 15) / 16 * 16);
+    const size_t operands = VECTOR ? (size_t)S::STAGES * S::PIECES * 16 * THREADS : (size_t)S::STAGES * teams * (dy_room + 2 * h_room);
+    const size_t shared = std::max(operands, (size_t)teams * a.width * sizeof(float));         // the ring, then the teams' shares
+    if (shared > kMostShared) return false;
+    auto kernel = k_rms_back_team<XT, HT, WT, CARRY, VECTOR, NU, THREADS>;
     static Resident resident[kMostDevices];          // asked once per kernel and device
     int ctas = 0;
-    cudaError_t e = resident_ctas(resident, reinterpret_cast<const void*>(kernel), THREADS, shared, &ctas);
-    if (e != cudaSuccess) return e;
-    const int teams = THREADS / 32 / team_warps;
+    *e = resident_ctas(resident, reinterpret_cast<const void*>(kernel), THREADS, VECTOR ? shared : kMostShared / (512 / THREADS), &ctas);
+    if (*e != cudaSuccess) return true;
+    if (!VECTOR) *e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared);
     const int grid = (int)std::min<int64_t>((a.rows + teams - 1) / teams, std::min(kMostShares, ctas));
-    e = launch(kernel, dim3((unsigned)grid), THREADS, shared, stream, false, a, team_warps);
-    if (e != cudaSuccess) return e;
-    return launch(k_rms_back_shares, dim3((unsigned)((a.width + 31) / 32)), 1024, 0, stream, true, a, grid);
+    if (*e == cudaSuccess) *e = launch(kernel, dim3((unsigned)grid), THREADS, shared, stream, false, a, team_warps, dy_room, h_room);
+    if (*e == cudaSuccess) *e = launch(k_rms_back_shares, dim3((unsigned)((a.width + 31) / 32)), 1024, 0, stream, true, a, grid);
+    return true;
 }
 
 // Lane elements: 16 for rows that 8 warps hold so, then 16 warps with 16 and with 32; 8 for the narrowest rows.
-template <int XT, int HT, bool VECTOR>
+template <int XT, int HT, int WT, bool CARRY, bool VECTOR>
 bool launch_back_width(const RmsBackArgs& a, cudaStream_t stream, cudaError_t* e)
 {
     using L = Lanes<XT, VECTOR>;
     constexpr int N8 = 8 / L::E, N16 = 16 / L::E, N32 = 32 / L::E;
     const int64_t warps8 = (a.width + 32 * 8 - 1) / (32 * 8), warps16 = (a.width + 32 * 16 - 1) / (32 * 16), warps32 = (a.width + 32 * 32 - 1) / (32 * 32);
-    if (warps8 == 1) *e = launch_back<XT, HT, VECTOR, N8, 256>(a, 1, stream);
-    else if (warps16 <= 8) *e = launch_back<XT, HT, VECTOR, N16, 256>(a, (int)warps16, stream);
-    else if (warps16 <= 16) *e = launch_back<XT, HT, VECTOR, N16, 512>(a, (int)warps16, stream);
-    else if (warps32 <= 16) *e = launch_back<XT, HT, VECTOR, N32, 512>(a, (int)warps32, stream);
-    else return false;
-    return true;
+    if (warps8 == 1) return launch_back<XT, HT, WT, CARRY, VECTOR, N8, 256>(a, 1, stream, e);
+    if (warps16 <= 8 && launch_back<XT, HT, WT, CARRY, VECTOR, N16, 256>(a, (int)warps16, stream, e)) return true;
+    if (warps16 <= 16 && launch_back<XT, HT, WT, CARRY, VECTOR, N16, 512>(a, (int)warps16, stream, e)) return true;
+    return warps32 <= 16 && launch_back<XT, HT, WT, CARRY, VECTOR, N32, 512>(a, (int)warps32, stream, e);
 }
 
-template <bool VECTOR>
-bool launch_back_rows(const RmsBackArgs& a, cudaStream_t stream, cudaError_t* e)
+template <int XT, int HT, int WT>
+bool launch_back_rows(const RmsBackArgs& a, bool vector, cudaStream_t stream, cudaError_t* e)
 {
-    const bool wide = a.h_type == APMS_GRAD_F32;
-    if (a.dy_type == APMS_GRAD_F32) return launch_back_width<APMS_GRAD_F32, APMS_GRAD_F32, VECTOR>(a, stream, e);
-    if (a.dy_type == APMS_GRAD_BF16) return wide ? launch_back_width<APMS_GRAD_BF16, APMS_GRAD_F32, VECTOR>(a, stream, e) : launch_back_width<APMS_GRAD_BF16, APMS_GRAD_BF16, VECTOR>(a, stream, e);
-    return wide ? launch_back_width<APMS_GRAD_F16, APMS_GRAD_F32, VECTOR>(a, stream, e) : launch_back_width<APMS_GRAD_F16, APMS_GRAD_F16, VECTOR>(a, stream, e);
+    if (a.dh) return vector ? launch_back_width<XT, HT, WT, true, true>(a, stream, e) : launch_back_width<XT, HT, WT, true, false>(a, stream, e);
+    return vector ? launch_back_width<XT, HT, WT, false, true>(a, stream, e) : launch_back_width<XT, HT, WT, false, false>(a, stream, e);
+}
+
+template <int XT>
+bool launch_back_types(const RmsBackArgs& a, bool vector, cudaStream_t stream, cudaError_t* e)
+{
+    if (a.h_type == XT) return a.w_type == XT ? launch_back_rows<XT, XT, XT>(a, vector, stream, e) : launch_back_rows<XT, XT, APMS_GRAD_F32>(a, vector, stream, e);
+    return a.w_type == XT ? launch_back_rows<XT, APMS_GRAD_F32, XT>(a, vector, stream, e) : launch_back_rows<XT, APMS_GRAD_F32, APMS_GRAD_F32>(a, vector, stream, e);
+}
+
+bool launch_rms_back(const RmsBackArgs& a, bool vector, cudaStream_t stream, cudaError_t* e)
+{
+    if (a.dy_type == APMS_GRAD_F32) return launch_back_rows<APMS_GRAD_F32, APMS_GRAD_F32, APMS_GRAD_F32>(a, vector, stream, e);
+    if (a.dy_type == APMS_GRAD_BF16) return launch_back_types<APMS_GRAD_BF16>(a, vector, stream, e);
+    return launch_back_types<APMS_GRAD_F16>(a, vector, stream, e);
 }
 
 // Every row begins on a 16-byte boundary and holds whole 16-byte pieces.
@@ -981,14 +1007,14 @@ apms_status apms_rms_norm_backward(const apms_rms_norm_backward_args* args, void
     a.rows = g.rows; a.width = g.width; a.dy_stride = g.dy_stride; a.h_stride = g.h_stride; a.dh_stride = g.dh_stride;
     a.dy = g.dy; a.h = g.h; a.w = g.weight; a.dh = g.dh; a.rstd = g.rstd; a.dx = g.dx; a.dr = g.dresidual; a.dw = g.dweight;
     a.partial = (float*)g.workspace_dev;
-    a.dy_type = g.dy_type; a.h_type = g.h_type; a.w_type = g.weight_type;
+    a.dy_type = g.dy_type; a.h_type = g.h_type; a.w_type = g.weight_type; a.inv_width = 1.0f / (float)g.width;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
     const bool vector = rows_of_16(a.dy, a.dy_stride, a.width, a.dy_type) && rows_of_16(a.h, a.h_stride, a.width, a.dy_type) && rows_of_16(a.dh, a.dh_stride, a.width, a.dy_type) &&
                         rows_of_16(a.w, 0, a.width, a.dy_type) && rows_of_16(a.dx, a.width, a.width, a.dy_type) && rows_of_16(a.dr, a.width, a.width, a.dy_type);
     if (!g.rows) {
         e = launch(k_rms_back_shares, dim3((unsigned)((a.width + 31) / 32)), 1024, 0, stream, false, a, 0);
-    } else if (!(vector ? launch_back_rows<true>(a, stream, &e) : launch_back_rows<false>(a, stream, &e))) {
+    } else if (!launch_rms_back(a, vector, stream, &e)) {
         e = launch(k_rms_back_rows, dim3((unsigned)g.rows), kRmsThreads, 0, stream, false, a);
         const unsigned columns = (unsigned)((g.width + kRmsThreads - 1) / kRmsThreads);
         if (e == cudaSuccess) e = launch(k_rms_back_weight, dim3(columns, kStrips), kRmsThreads, 0, stream, false, a);
