@@ -580,14 +580,14 @@ apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float 
  *
  * Per row of `width` elements:  h = x + residual (h = x without one),
  *   rstd = 1 / sqrt(mean(h^2) + eps),  y = h * rstd * weight.
- * All in binary32 from the unrounded h; every output is rounded once, from binary32.
+ * All in binary32 from the unrounded h; every output is rounded once, from binary32 (rstd is within 2 units in the last place).
  * x: x_type, rows x_stride elements apart; residual: x_type or binary32, or NULL; weight: `width` elements of x_type or
  * binary32; h: written (contiguous rows, residual_type) if there is a residual, ignored otherwise; rstd: `rows` floats,
  * written.  y: contiguous rows, of x_type - or, where scales is not NULL, e4m3 bytes: per group of `group`
  * consecutive elements of a row (group = 0: the whole row; 128: the last group of a row may be shorter),
  *   a = max |y|,  scale = a / 448,  q = e4m3(y * (448 / a)), nearest even,
- * scales: rows x ceil(width / group) floats.  A group whose a is below 2^-100 has scale 0 and q = 0; a NaN or
- * an infinity in a group shows in its scale.  Inputs need only be aligned to their element size. */
+ * scales: rows x ceil(width / group) floats (a row's a may be formed as max |h * weight| * rstd).  A group whose a is below
+ * 2^-100 has scale 0 and q = 0; a NaN or an infinity in a group shows in its scale.  Inputs need only be aligned to their element size. */
 typedef struct {
     int64_t rows, width;
     const void* x;        int64_t x_stride;        apms_grad_type x_type;
