@@ -195,16 +195,16 @@ k_one_norm(const __grid_constant__ ListMemory m, const __grid_constant__ NormOut
     __shared__ double red[kOneThreads / 32];
     constexpr int FEW = 32;
     allow_next_kernel();
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, mine_first = lane * 32 + (threadIdx.x >> 5);        // consecutive tensors go to different warps
     int2 mine = make_int2(0, 0);                     // tiles of this thread's first tensor
-    if (threadIdx.x < m.count) mine = make_int2(m.tensors[threadIdx.x].tile0, m.tensors[threadIdx.x].tiles);
+    if (mine_first < m.count) mine = make_int2(m.tensors[mine_first].tile0, m.tensors[mine_first].tiles);
     wait_for_last_kernel();
 #pragma unroll 8
     for (int k = threadIdx.x; k < tiles; k += kOneThreads) sums[k] = m.tile_sum[k];
     __syncthreads();
     double total = 0.0;
     for (int t0 = 0; t0 < m.count; t0 += kOneThreads) {
-        const int t = t0 + threadIdx.x;
+        const int t = t0 + mine_first;
         if (t0) mine = t < m.count ? make_int2(m.tensors[t].tile0, m.tensors[t].tiles) : make_int2(0, 0);
         double s = 0.0;
         if (mine.y <= FEW)

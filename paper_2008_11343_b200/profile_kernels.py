@@ -105,6 +105,64 @@ def _cases(args):
     }
 
 
+def _operator_cases():
+    """Kernels of the operators beside the step: name -> function making (call, algorithmic bytes of the whole call)."""
+    import torch
+
+    from . import operators as O
+
+    def tensor(rows, width, dtype=torch.bfloat16):
+        return torch.empty(rows, width, device="cuda", dtype=dtype).normal_()
+
+    def gradients(clip, big=8):
+        sizes = [4 << 20] * big + [1 << 20] * 32 + [1024] * 64                   # big = 8: 67 M elements
+        grads = [torch.empty(n, device="cuda").normal_() for n in sizes]
+        tensors, d = O.TensorList(grads), sum(sizes)
+        flat = torch.empty(d, device="cuda")
+        if clip:
+            return lambda: tensors.clip_grads(grads, 1.0, out=flat), 8 * d
+        return lambda: tensors.grad_norm(grads), 4 * d
+
+    def forward(rows, width, dtype=torch.bfloat16, group=None):
+        x, r, w = tensor(rows, width, dtype), tensor(rows, width, dtype), tensor(1, width, dtype)[0]
+        out = dtype.itemsize if group is None else 1
+        if group is None:
+            return lambda: O.rms_norm_forward(x, w, r), rows * width * (3 * dtype.itemsize + out)
+        return lambda: O.rms_norm_fp8(x, w, r, group=group), rows * width * (3 * dtype.itemsize + out)
+
+    def backward(rows, width):
+        dy, h, dh, w = (tensor(rows, width) for _ in range(4))
+        rstd = torch.rand(rows, device="cuda")
+        return lambda: O.rms_norm_backward(dy, h, w[0], rstd, dh), 8 * rows * width
+
+    return {
+        "k_tile_squares": lambda: gradients(False), "k_list_norm": lambda: gradients(False), "k_one_norm": lambda: gradients(False, 4), "k_scale_tiles": lambda: gradients(True),
+        "k_rms_staged": lambda: forward(8192, 4096), "k_rms_staged_row_scale": lambda: forward(8192, 4096, group=0),
+        "k_rms_staged_column_scales": lambda: forward(8192, 4096, group=128), "k_rms_staged_f32": lambda: forward(8192, 4096, torch.float32),
+        "k_rms_narrow": lambda: forward(200_000, 128), "k_rms_shifted": lambda: forward(8192, 4095),
+        "k_rms_back_team": lambda: backward(8192, 4096), "k_rms_back_team_shifted": lambda: backward(8192, 4095), "k_rms_back_shares": lambda: backward(8192, 4096),
+    }
+
+
+def _run_operator(args, make) -> int:
+    import torch
+
+    call, nbytes = make()
+    for _ in range(3):
+        call()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    torch.cuda.synchronize()
+    e0.record()
+    for _ in range(args.launches):
+        call()
+    e1.record()
+    torch.cuda.synchronize()
+    ms = e0.elapsed_time(e1) / args.launches
+    print(json.dumps({"kernel": args.kernel, "launches": args.launches, "algorithmic_bytes_per_call": nbytes, "ms_per_call": ms,
+                      "timed": "events around the whole call", "algorithmic_gbs": nbytes / (ms * 1e-3) / 1e9}))
+    return 0
+
+
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--kernel", required=True)
@@ -118,9 +176,11 @@ def main(argv=None) -> int:
     from . import binding as B
     from . import workloads as wl
 
-    cases = _cases(args)
+    cases, operators = _cases(args), _operator_cases()
+    if args.kernel in operators:
+        return _run_operator(args, operators[args.kernel])
     if args.kernel not in cases:
-        print("unknown kernel; one of: " + " ".join(sorted(cases)), file=sys.stderr)
+        print("unknown kernel; one of: " + " ".join(sorted(cases) + sorted(operators)), file=sys.stderr)
         return 2
     case = cases[args.kernel]
     e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
