@@ -182,20 +182,43 @@ __device__ __forceinline__ const char* stage_shifted(char* room, const char* p, 
     return room + shift;
 }
 
-// What a row's team found in its first reading, over the team (all its threads get it): sum of squares, and with TAKE_MOST the largest magnitude.
-// Every thread of the CTA calls it.
-template <bool TAKE_MOST>
-__device__ __forceinline__ void join_team(float& squares, float& most, int team_warps, float* red, float* red_most)
+// What the warps of a row (blockDim.x threads, a row per threadIdx.y) found in its first reading, over the row, in every thread: the sum of squares, and the
+// largest magnitude where it is wanted.  Every thread of the CTA calls it.  smem: 2 kTeamWarps floats.
+__device__ __forceinline__ void join_team(float& squares, float& most, bool take_most, float* smem)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team_warps = blockDim.x >> 5;
     squares = warp_total(squares);
-    if (TAKE_MOST) most = warp_most(most, 32);
+    if (take_most) most = warp_most(most, 32);
     if (team_warps == 1) return;
-    if (lane == 0) { red[warp] = squares; red_most[warp] = most; }
+    float* team = smem + threadIdx.y * team_warps;
+    if (lane == 0) { team[warp] = squares; team[kTeamWarps + warp] = most; }
     __syncthreads();
-    const int at = warp / team_warps * team_warps + lane;
-    squares = warp_total(lane < team_warps ? red[at] : 0.0f);
-    if (TAKE_MOST) most = warp_most(lane < team_warps ? red_most[at] : 0.0f, 32);
+    squares = team[0];
+    for (int w = 1; w < team_warps; ++w) squares += team[w];
+    if (take_most) {
+        most = team[kTeamWarps];
+        for (int w = 1; w < team_warps; ++w) most = max_nan(most, team[kTeamWarps + w]);
+    }
+}
+
+// One element in shared memory.
+template <int TYPE>
+__device__ __forceinline__ float load_shared_element(uint32_t shared)
+{
+    if (TYPE == APMS_GRAD_F32) {
+        float v;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(shared) : "memory");
+        return v;
+    }
+    unsigned short v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(shared) : "memory");
+    return unpack16<TYPE == APMS_GRAD_F32 ? APMS_GRAD_BF16 : TYPE>(v).x;
+}
+template <int ES>
+__device__ __forceinline__ void put_zero_element(uint32_t shared)
+{
+    if (ES == 4) asm volatile("st.shared.u32 [%0], %1;" :: "r"(shared), "r"(0) : "memory");
+    else asm volatile("st.shared.u16 [%0], %1;" :: "r"(shared), "h"((unsigned short)0) : "memory");
 }
 
 // Narrow rows (up to 256 elements of 16 bits, 128 of 32), whole 16-byte pieces: TL lanes a row and R rows a lane, in registers, the weight loaded once for
@@ -270,7 +293,7 @@ k_rms_staged(const RmsArgs a, int64_t rows)
     constexpr int DR = RES ? E * RS / 16 : 0, WORDS = E * WS / 4;
     extern __shared__ __align__(16) char staged[];
     __shared__ float red[2 * kTeamWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team_warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = warp * (NU * L::UNIT) + lane * E, width = (int)a.width;        // unit u of this lane begins at c0 + u UNIT
     const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const int in = row < rows ? width : 0;           // a team without a row loads nothing and stays for the barrier
@@ -346,19 +369,8 @@ k_rms_staged(const RmsArgs a, int64_t rows)
         }
         load_weight();                               // while the sums are under way
     }
-    float squares = warp_total(acc.x + acc.y);
-    if (row_scale) most = warp_most(most, 32);
-    if (team_warps > 1) {
-        float* team = red + threadIdx.y * team_warps;
-        if (lane == 0) { team[warp] = squares; team[kTeamWarps + warp] = most; }
-        __syncthreads();
-        squares = team[0];
-        for (int w = 1; w < team_warps; ++w) squares += team[w];
-        if (row_scale) {
-            most = team[kTeamWarps];
-            for (int w = 1; w < team_warps; ++w) most = max_nan(most, team[kTeamWarps + w]);
-        }
-    }
+    float squares = acc.x + acc.y;
+    join_team(squares, most, row_scale, red);
     const float rstd = rsqrtf(squares * a.inv_width + a.eps);
     float scale = 0.0f, inverse = 0.0f;
     if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
@@ -408,82 +420,105 @@ k_rms_staged(const RmsArgs a, int64_t rows)
 // Rows that do not start on 16-byte boundaries or hold a ragged number of bytes, through shared memory too: the 16-byte pieces that a row touches are
 // copied as they lie (its first bytes, up to a boundary, by plain loads: what is before them may not be the caller's), and
 // its elements read one by one from there, 32 lanes' consecutive.  Bound by those 2-byte accesses: 8192 x 1001 bfloat16 24 us = 2.7 TB/s
-// (2-byte loads from global memory: 28 us).
-template <int XT, int RT, int WT, int NU>
+// (2-byte loads from global memory: 28 us), 4000 x 8191 82 us = 3.2 TB/s.
+template <int XT, int RT, int WT, bool RES, int NU>
 __global__ void __launch_bounds__(kTeamWarps * 32)
-k_rms_shifted(const RmsArgs a, int64_t rows, int team_warps, int x_room, int r_room)
+k_rms_shifted(const RmsArgs a, int64_t rows, int x_room, int r_room)
 {
     using L = Lanes<XT, false>;
-    constexpr int E = L::E, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2;
+    constexpr int E = L::E, XS = XT == APMS_GRAD_F32 ? 4 : 2, RS = RT == APMS_GRAD_F32 ? 4 : 2, WS = WT == APMS_GRAD_F32 ? 4 : 2;
     extern __shared__ __align__(16) char staged[];
-    __shared__ float red[kTeamWarps], red_most[kTeamWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / team_warps, unit0 = (warp - team * team_warps) * NU;
-    const int width = (int)a.width, t = threadIdx.x - team * team_warps * 32, threads = team_warps * 32;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / 32 / team_warps) + team;
-    const bool here = row < rows;
-    const int in = here ? width : 0;
-    char* room = staged + team * (x_room + r_room);
-    const char* xs = stage_shifted<XS>(room, static_cast<const char*>(a.x) + row * a.x_stride * XS, in, t, threads);
-    const char* rs = a.r ? stage_shifted<RS>(room + x_room, static_cast<const char*>(a.r) + row * a.r_stride * RS, in, t, threads) : nullptr;
+    __shared__ float red[2 * kTeamWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team_warps = blockDim.x >> 5, width = (int)a.width;
+    const int c0 = warp * (NU * L::UNIT) + lane, padded = team_warps * (NU * L::UNIT);        // element j of unit u of this lane: column c0 + 128 u + 32 j
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int in = row < rows ? width : 0, left = in - c0;
+    char* room = staged + threadIdx.y * (x_room + r_room);
+    const char* xs = stage_shifted<XS>(room, static_cast<const char*>(a.x) + row * a.x_stride * XS, in, threadIdx.x, blockDim.x);
+    const char* rs = RES ? stage_shifted<RS>(room + x_room, static_cast<const char*>(a.r) + row * a.r_stride * RS, in, threadIdx.x, blockDim.x) : xs;
     commit_copies();
     float w[NU][E];
+    const char* wp = static_cast<const char*>(a.w) + (int64_t)c0 * WS;
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const int c = L::column(unit0 + u, lane, j);
-            w[u][j] = c < in ? load_element(a.w, c, WT) : 0.0f;
-        }
+        for (int j = 0; j < E; ++j) w[u][j] = u * L::UNIT + 32 * j < left ? load_element(wp + (u * L::UNIT + 32 * j) * WS, 0, WT) : 0.0f;
     const bool row_scale = a.scales && a.group == a.width;
     wait_for_copies<0>();
+    for (int c = in + threadIdx.x; c < padded; c += blockDim.x) {       // zeros behind the row, so that the sums need not ask
+        put_zero_element<XS>((uint32_t)__cvta_generic_to_shared(xs) + c * XS);
+        if (RES) put_zero_element<RS>((uint32_t)__cvta_generic_to_shared(rs) + c * RS);
+    }
     __syncthreads();
-    auto h_of = [&](int c) {
-        const float h = load_element(xs, c, XT);
-        return a.r ? h + load_element(rs, c, RT) : h;
+    const uint32_t xa = (uint32_t)__cvta_generic_to_shared(xs) + c0 * XS, ra = (uint32_t)__cvta_generic_to_shared(rs) + c0 * RS;
+    auto h_of = [&](int k) {                         // of column c0 + k
+        const float h = load_shared_element<XT>(xa + k * XS);
+        return RES ? h + load_shared_element<RT>(ra + k * RS) : h;
     };
     float squares = 0.0f, most = 0.0f;
+    if (row_scale) {
 #pragma unroll
-    for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const int c = L::column(unit0 + u, lane, j);
-            const float h = c < in ? h_of(c) : 0.0f;
-            squares = fmaf(h, h, squares);
-            if (row_scale) most = max_nan(most, fabsf(h * w[u][j]));
-        }
-    join_team<true>(squares, most, team_warps, red, red_most);
+            for (int j = 0; j < E; ++j) {
+                const float h = h_of(u * L::UNIT + 32 * j);
+                squares = fmaf(h, h, squares);
+                most = max_nan(most, fabsf(h * w[u][j]));
+            }
+    } else {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float h = h_of(u * L::UNIT + 32 * j);
+                squares = fmaf(h, h, squares);
+            }
+    }
+    join_team(squares, most, row_scale, red);
     const float rstd = rsqrtf(squares * a.inv_width + a.eps);
     float scale = 0.0f, inverse = 0.0f;
     if (row_scale) group_scale(magnitude_bits(most * rstd), &scale, &inverse);
-    if (here && unit0 == 0 && lane == 0) {
+    if (threadIdx.x == 0 && in) {
         a.rstd[row] = rstd;
         if (row_scale) a.scales[row] = scale;
     }
-    char* hr = static_cast<char*>(a.h) + row * a.width * RS;
-    char* yr = static_cast<char*>(a.y) + row * a.width * (a.scales ? 1 : XS);
+    char* hp = static_cast<char*>(a.h) + (row * width + c0) * RS;
+    char* yp = static_cast<char*>(a.y) + (row * width + c0) * (a.scales ? 1 : XS);
+    if (!a.scales) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const int k = u * L::UNIT + 32 * j;
+                const float h = h_of(k);
+                if (k < left) {
+                    if (RES) store_element(hp + k * RS, 0, RT, h);
+                    store_element(yp + k * XS, 0, XT, h * rstd * w[u][j]);
+                }
+            }
+        return;
+    }
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         float y[E], m = 0.0f;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const int c = L::column(unit0 + u, lane, j);
-            const float h = c < in ? h_of(c) : 0.0f;
+            const int k = u * L::UNIT + 32 * j;
+            const float h = h_of(k);
             y[j] = h * rstd * w[u][j];
-            if (c < in) {
-                if (a.r) store_element(hr, c, RT, h);
-                if (!a.scales) store_element(yr, c, XT, y[j]);
-                m = max_nan(m, fabsf(y[j]));
+            if (k < left) {
+                if (RES) store_element(hp + k * RS, 0, RT, h);
+                m = max_nan(m, fabsf(y[j]));         // zeros behind the row are NaN by now where rstd is infinite or NaN
             }
         }
-        if (!a.scales) continue;
         if (!row_scale) {
             group_scale(magnitude_bits(warp_most(m, 32)), &scale, &inverse);
-            if (lane == 0 && (unit0 + u) * L::UNIT < in) a.scales[row * a.groups + unit0 + u] = scale;
+            if (lane == 0 && u * L::UNIT < left) a.scales[row * a.groups + (c0 + u * L::UNIT) / 128] = scale;
         }
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const int c = L::column(unit0 + u, lane, j);
-            if (c < in) reinterpret_cast<uint8_t*>(yr)[c] = __nv_cvt_float_to_fp8(y[j] * inverse, __NV_SATFINITE, __NV_E4M3);
+            const int k = u * L::UNIT + 32 * j;
+            if (k < left) yp[k] = (char)__nv_cvt_float_to_fp8(y[j] * inverse, __NV_SATFINITE, __NV_E4M3);
         }
     }
 }
@@ -622,11 +657,11 @@ k_rms_back_team(const RmsBackArgs a, int team_warps, int dy_room, int h_room)
             for (int k = 0; k < WORDS; k += 4) load_shared16(w + k, mine + stage * stage_bytes + (piece + u * (WORDS / 4) + k / 4) * PIECE);
             unpack_words<TYPE, WORDS>(f, w);
         } else {
-            const char* from = room + stage * stage_bytes + room_at + ((uintptr_t)row & 15);
+            constexpr int ES = TYPE == APMS_GRAD_F32 ? 4 : 2;
+            const uint32_t from = (uint32_t)__cvta_generic_to_shared(room) + stage * stage_bytes + room_at + (uint32_t)((uintptr_t)row & 15) + c0 * ES;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const int c = L::column(unit0 + u, lane, j);
-                const float v = c < width ? load_element(from, c, TYPE) : 0.0f;
+                const float v = u * L::UNIT + 32 * j < own - c0 ? load_shared_element<TYPE>(from + (u * L::UNIT + 32 * j) * ES) : 0.0f;
                 if (j & 1) f[j / 2].y = v; else f[j / 2].x = v;
             }
         }
@@ -833,8 +868,12 @@ struct RmsLaunch {
     static bool shifted(const RmsArgs& a, int64_t rows, int units, cudaStream_t stream, cudaError_t* e)
     {
         const Team t = team_for(units, NU);
-        const int x_room = (int)((a.width * XS + 15 + 15) / 16 * 16), r_room = a.r ? (int)((a.width * RS + 15 + 15) / 16 * 16) : 0;
-        return t.threads && with_shared<k_rms_shifted<XT, RT, WT, NU>>(dim3(t.threads), (rows + t.rows - 1) / t.rows, (size_t)t.rows * (x_room + r_room), stream, e, a, rows, t.warps, x_room, r_room);
+        if (!t.threads) return false;
+        const int padded = t.warps * NU * 128, x_room = padded * XS + 16, r_room = a.r ? padded * RS + 16 : 0;
+        const dim3 block(t.warps * 32, t.rows);
+        const size_t grid = (rows + t.rows - 1) / t.rows, shared = (size_t)t.rows * (x_room + r_room);
+        return a.r ? with_shared<k_rms_shifted<XT, RT, WT, true, NU>>(block, grid, shared, stream, e, a, rows, x_room, r_room)
+                   : with_shared<k_rms_shifted<XT, RT, WT, false, NU>>(block, grid, shared, stream, e, a, rows, x_room, r_room);
     }
 
     // KERNEL with as much shared memory as it asks for, within what a CTA can have
