@@ -38,6 +38,8 @@ class _EightBitNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy, dh):
+        if torch.is_grad_enabled():                                       # create_graph=True: nothing to differentiate again
+            raise RuntimeError("no second derivatives through the 8-bit norm")
         dx, dweight, dstream = operators.rms_norm_backward(dy.contiguous(), *ctx.saved_tensors, dh)
         return dx, dweight, dstream
 

@@ -78,6 +78,20 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None):
     return _load().rms_norm_backward(dy, h, weight, rstd, dh)
 
 
+class _RmsNormGradient(torch.autograd.Function):
+    """rms_norm_backward where a graph of the backward pass is being built (create_graph=True): the kernels leave nothing to
+    differentiate, so its own backward pass raises.  (torch's once_differentiable would return constants where dy needs no gradient,
+    though h and the weight do.)"""
+
+    @staticmethod
+    def forward(ctx, dy, h, weight, rstd, dh):
+        return rms_norm_backward(dy, h, weight, rstd, dh)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("rms_norm has first derivatives only: its second derivatives are not implemented")
+
+
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
@@ -92,10 +106,12 @@ class _RmsNorm(torch.autograd.Function):
         h, weight, rstd = ctx.saved_tensors
         if dy is None:                                       # only h was used: the norm contributes nothing
             return None if dh is None else dh.to(ctx.x_type), None, dh, None
-        dx, dweight, *dresidual = rms_norm_backward(dy, h, weight, rstd, dh)
+        gradient = _RmsNormGradient.apply if torch.is_grad_enabled() else rms_norm_backward
+        dx, dweight, *dresidual = gradient(dy, h, weight, rstd, dh)
         return dx, dweight, (dresidual[0] if dresidual else dx) if ctx.junction else None, None
 
 
 def rms_norm(x, weight, residual=None, eps: float = 1e-6):
-    """y = rms_norm(x, weight), or (y, h) = rms_norm(x, weight, residual) with h = x + residual; differentiable in all three."""
+    """y = rms_norm(x, weight), or (y, h) = rms_norm(x, weight, residual) with h = x + residual; differentiable in all three,
+    once: a second derivative raises RuntimeError."""
     return _RmsNorm.apply(x, weight, residual, eps)
