@@ -323,9 +323,8 @@ TensorList& list_of(PyObject* capsule)
 }
 
 // The tensors' addresses, once they are found to be laid out as the list's are.
-void take_addresses(TensorList& self, PyObject* tensors, bool written)
+void take_addresses(TensorList& self, const Sequence& ts, bool written)
 {
-    const Sequence ts(tensors);
     if (ts.size() != (Py_ssize_t)self.layout.size()) refuse("the list has ", self.layout.size(), " tensors, not ", ts.size());
     for (Py_ssize_t k = 0; k < ts.size(); ++k) {
         const at::Tensor& t = ts[k];
@@ -352,12 +351,19 @@ cudaStream_t enter(TensorList& self)
     return now.stream();
 }
 
+// Autograd's notice that a tensor was written: a graph that has saved it raises in its backward pass.  (Inference tensors have no version, and
+// no graph can save them.)
+void note_write(const at::Tensor& t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject* {
         if (n != 2) refuse("grad_norm takes 2 arguments");
         TensorList& self = list_of(args[0]);
-        take_addresses(self, args[1], false);
+        take_addresses(self, Sequence(args[1]), false);
         const c10::cuda::OptionalCUDAGuard on(self.device);
         at::Tensor norm = empty({}, at::kFloat, self.device), norms = empty({(int64_t)self.layout.size()}, at::kFloat, self.device);
         check(c_grad_norm(self.list, self.addresses.data(), (float*)norm.data_ptr(), (float*)norms.data_ptr(), enter(self)));
@@ -374,7 +380,8 @@ PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n)
         if (PyErr_Occurred()) throw Raised();
         void* flat = nullptr;
         apms_grad_type type = APMS_GRAD_F32;
-        take_addresses(self, args[1], args[3] == Py_None);
+        const Sequence ts(args[1]);
+        take_addresses(self, ts, args[3] == Py_None);
         if (args[3] != Py_None) {
             const at::Tensor& out = tensor(args[3], "out");
             if (out.device() != self.device || !out.is_contiguous() || out.numel() != self.numel) refuse("out must be ", self.numel, " contiguous elements on ", self.device);
@@ -384,6 +391,8 @@ PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n)
         const c10::cuda::OptionalCUDAGuard on(self.device);
         at::Tensor norm = empty({}, at::kFloat, self.device);
         check(c_clip_grads(self.list, self.addresses.data(), (float)max_norm, flat, type, (float*)norm.data_ptr(), enter(self)));
+        if (flat) note_write(tensor(args[3], "out"));
+        for (Py_ssize_t k = 0; !flat && k < ts.size(); ++k) note_write(ts[k]);
         return wrap(std::move(norm));
     });
 }
