@@ -558,6 +558,14 @@ size_t      apms_tensors_workspace_bytes(const apms_tensors* list);
 apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t bytes, void* cuda_stream);
 void        apms_tensors_destroy(apms_tensors* list);
 
+/* What a call writes of the workspace (sums, a ticket, the clip factor) can be put elsewhere: the calls after this one use
+ * scratch_dev (>= apms_tensors_scratch_bytes, 256-byte aligned; the ticket is zeroed on `cuda_stream`, without synchronising), or with NULL the
+ * workspace again.  The tables, which no call writes, stay where they are.  For calls captured into a CUDA graph, whose replays no
+ * stream order holds apart from the list's other calls: between two of these calls, each captured call in scratch memory that
+ * belongs to the graph.  The zeroing is captured with them, so one call follows it. */
+size_t      apms_tensors_scratch_bytes(const apms_tensors* list);
+apms_status apms_tensors_use_scratch(apms_tensors* list, void* scratch_dev, size_t bytes, void* cuda_stream);
+
 /* norm_dev[0] = ||g||_2 over all tensors, norms_dev[t] (NULL or `count` floats) = ||g_t||_2.  Squares are summed in
  * binary64, in an order fixed by the list alone; the roots are rounded once to binary32.  NaN and infinities
  * propagate.  tensors_dev: HOST array of `count` device addresses, each aligned to its element size

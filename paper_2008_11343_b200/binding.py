@@ -100,6 +100,8 @@ SIGNATURES = {
     "apms_tensors_workspace_bytes": (C.c_size_t, [C.c_void_p]),
     "apms_tensors_bind": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "apms_tensors_destroy": (None, [C.c_void_p]),
+    "apms_tensors_scratch_bytes": (C.c_size_t, [C.c_void_p]),
+    "apms_tensors_use_scratch": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "apms_grad_norm": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "apms_clip_grads": (C.c_int, [C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
     "apms_rms_norm": (C.c_int, [C.c_void_p, C.c_void_p]),
@@ -480,6 +482,14 @@ def apms_tensors_bind(h, workspace_ptr: int, nbytes: int, stream: int):
 
 def apms_tensors_destroy(h):
     load().apms_tensors_destroy(h)
+
+
+def apms_tensors_scratch_bytes(h) -> int:
+    return int(load().apms_tensors_scratch_bytes(h))
+
+
+def apms_tensors_use_scratch(h, scratch_ptr: Optional[int], nbytes: int, stream: int):
+    _check_thread(load().apms_tensors_use_scratch(h, scratch_ptr, nbytes, stream))
 
 
 def apms_grad_norm(h, tensor_ptrs, norm_ptr: int, norms_ptr: Optional[int], stream: int):

@@ -395,7 +395,15 @@ struct apms_tensors {
     int64_t total;
     ListMemory m;                        // m.tiles == nullptr: no workspace yet
 
-    // Byte offsets of the tables and sums in the workspace.
+    // Which kernels form the norm: the tiles' last CTA adds up / one CTA does / the groups' CTAs do, the last of them the rest.
+    enum class Route { alone, one, groups };
+    Route route() const
+    {
+        if (!tiles.empty() && tiles.size() <= (size_t)kAloneTiles && tensors.size() <= (size_t)kListPointers) return Route::alone;
+        return tiles.size() <= (size_t)kOneTiles ? Route::one : Route::groups;
+    }
+
+    // Byte offsets of the tables and, from tile_sum on, of what the calls write in the workspace.
     struct Places { size_t tensors, groups, tile_sum, group_sum, ticket, bytes; };
     Places places() const
     {
@@ -408,6 +416,15 @@ struct apms_tensors {
         p.ticket = p.group_sum + up(groups.size() * sizeof(double));     // and the factor behind it
         p.bytes = p.ticket + 256;
         return p;
+    }
+    // The calls' sums, ticket and factor at `p`, laid out as from tile_sum on.
+    void write_at(char* p)
+    {
+        const Places at = places();
+        m.tile_sum = (double*)p;
+        m.group_sum = (double*)(p + (at.group_sum - at.tile_sum));
+        m.ticket = (unsigned*)(p + (at.ticket - at.tile_sum));
+        m.factor = (float*)(m.ticket + 1);
     }
 };
 
@@ -478,13 +495,33 @@ apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t by
     ListMemory& m = list->m;
     m.tiles = (const TileRecord*)ws;
     m.tensors = (const TensorRecord*)(ws + at.tensors);
-    m.tile_sum = (double*)(ws + at.tile_sum);
-    m.group_sum = (double*)(ws + at.group_sum);
     m.group = (const GroupRecord*)(ws + at.groups);
-    m.ticket = (unsigned*)(ws + at.ticket);
-    m.factor = (float*)(m.ticket + 1);
     m.count = (int)list->tensors.size();
     m.groups = (int)list->groups.size();
+    list->write_at(ws + at.tile_sum);
+    return APMS_OK;
+}
+
+size_t apms_tensors_scratch_bytes(const apms_tensors* list)
+{
+    if (!list) return 0;
+    const apms_tensors::Places at = list->places();
+    return at.bytes - at.tile_sum;
+}
+
+apms_status apms_tensors_use_scratch(apms_tensors* list, void* scratch_dev, size_t bytes, void* cuda_stream)
+{
+    if (!list || !list->m.tiles) return operator_fail(APMS_ERR_BAD_STATE, "apms_tensors_use_scratch: the list has no workspace (apms_tensors_bind)");
+    if (!scratch_dev) {
+        list->write_at((char*)list->m.tiles + list->places().tile_sum);
+        return APMS_OK;
+    }
+    if ((uintptr_t)scratch_dev & 255u) return operator_fail(APMS_ERR_INVALID_ARG, "apms_tensors_use_scratch: the scratch memory must be 256-byte aligned");
+    if (bytes < apms_tensors_scratch_bytes(list)) return operator_fail(APMS_ERR_OOM, "apms_tensors_use_scratch: scratch memory smaller than apms_tensors_scratch_bytes()");
+    const apms_tensors::Places at = list->places();
+    if (list->route() != apms_tensors::Route::one)       // the ticket is all that has to be there before a call
+        OPERATOR_CUDA("apms_tensors_use_scratch", cudaMemsetAsync((char*)scratch_dev + (at.ticket - at.tile_sum), 0, sizeof(unsigned), (cudaStream_t)cuda_stream));
+    list->write_at((char*)scratch_dev);
     return APMS_OK;
 }
 
@@ -535,10 +572,11 @@ cudaError_t list_norm(const apms_tensors* list, const void* const* tensors_dev, 
 {
     const NormOut out = {norm, norms, max_norm};
     const int tiles = (int)list->tiles.size();
-    if (tiles && tiles <= kAloneTiles && list->tensors.size() <= kListPointers) return over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares<true>, out);
+    const apms_tensors::Route route = list->route();
+    if (route == apms_tensors::Route::alone) return over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares<true>, out);
     cudaError_t e = over_tiles(list, tensors_dev, stream, kNormThreads, false, k_tile_squares<false>, out);
     if (e != cudaSuccess) return e;
-    if (tiles <= kOneTiles) {
+    if (route == apms_tensors::Route::one) {
         static Resident resident[kMostDevices];
         int ctas = 0;
         e = resident_ctas(resident, reinterpret_cast<const void*>(k_one_norm), kOneThreads, kOneTiles * sizeof(double), &ctas);

@@ -7,6 +7,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/CUDAEvent.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -26,6 +27,8 @@ decltype(&apms_tensors_create) c_create;
 decltype(&apms_tensors_workspace_bytes) c_workspace_bytes;
 decltype(&apms_tensors_bind) c_bind;
 decltype(&apms_tensors_destroy) c_destroy;
+decltype(&apms_tensors_scratch_bytes) c_scratch_bytes;
+decltype(&apms_tensors_use_scratch) c_use_scratch;
 decltype(&apms_grad_norm) c_grad_norm;
 decltype(&apms_clip_grads) c_clip_grads;
 decltype(&apms_rms_norm) c_rms_norm;
@@ -119,6 +122,9 @@ int64_t width_of(const at::Tensor& x, const char* what)
 
 // at::empty without the dispatcher's share of its time
 at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type, const at::Device& device) { return at::Tensor(at::detail::empty_cuda(sizes, type, device, std::nullopt)); }
+
+// Whether the current stream's work is being captured into a graph.
+bool capturing() { return c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None; }
 
 PyObject* wrap(at::Tensor t) { return THPVariable_Wrap(std::move(t)); }
 
@@ -303,6 +309,7 @@ PyObject* list_create(PyObject*, PyObject* tensors)
         self->addresses.resize(numel.size());
         check(c_create(&self->list, (int)numel.size(), numel.data(), types.data(), cols.data(), strides.data()));
         const c10::cuda::OptionalCUDAGuard on(self->device);
+        if (capturing()) refuse("a TensorList is built before a graph's capture, not within it");
         self->stream = c10::cuda::getCurrentCUDAStream(self->device.index());
         const size_t bytes = c_workspace_bytes(self->list);
         self->workspace = empty({(int64_t)bytes}, at::kByte, self->device);
@@ -337,19 +344,35 @@ void take_addresses(TensorList& self, const Sequence& ts, bool written)
     }
 }
 
-// The current stream, after the list's last one where they differ (the list's memory is shared by its calls).
-cudaStream_t enter(TensorList& self)
-{
-    const c10::cuda::CUDAStream now = c10::cuda::getCurrentCUDAStream(self.device.index());
-    if (now != self.stream) {
-        at::cuda::CUDAEvent done;
-        done.record(self.stream);
-        done.block(now);
-        self.workspace.record_stream(now);
-        self.stream = now;
+// The stream of one call, and the memory it writes to on the way.  The list's own memory is shared by its calls, so one on another stream than the last
+// one's waits for that one.  A call that is being captured cannot wait for what is outside its graph, and no stream order holds the
+// graph's replays apart from the list's other calls: it works in memory of its own, which comes from the graph's pool.
+class Turn {
+public:
+    explicit Turn(TensorList& list) : list_(list)
+    {
+        const c10::cuda::CUDAStream now = c10::cuda::getCurrentCUDAStream(list.device.index());
+        stream = now.stream();
+        if (capturing()) {
+            const size_t bytes = c_scratch_bytes(list.list);
+            scratch_ = empty({(int64_t)bytes}, at::kByte, list.device);
+            check(c_use_scratch(list.list, scratch_.data_ptr(), bytes, stream));
+        } else if (now != list.stream) {
+            at::cuda::CUDAEvent done;
+            done.record(list.stream);
+            done.block(now);
+            list.workspace.record_stream(now);
+            list.stream = now;
+        }
     }
-    return now.stream();
-}
+    ~Turn() { if (scratch_.defined()) c_use_scratch(list_.list, nullptr, 0, nullptr); }
+    Turn(const Turn&) = delete;
+    cudaStream_t stream;
+
+private:
+    TensorList& list_;
+    at::Tensor scratch_;
+};
 
 // Autograd's notice that a tensor was written: a graph that has saved it raises in its backward pass.  (Inference tensors have no version, and
 // no graph can save them.)
@@ -366,7 +389,8 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n)
         take_addresses(self, Sequence(args[1]), false);
         const c10::cuda::OptionalCUDAGuard on(self.device);
         at::Tensor norm = empty({}, at::kFloat, self.device), norms = empty({(int64_t)self.layout.size()}, at::kFloat, self.device);
-        check(c_grad_norm(self.list, self.addresses.data(), (float*)norm.data_ptr(), (float*)norms.data_ptr(), enter(self)));
+        const Turn turn(self);
+        check(c_grad_norm(self.list, self.addresses.data(), (float*)norm.data_ptr(), (float*)norms.data_ptr(), turn.stream));
         return tuple_of({wrap(std::move(norm)), wrap(std::move(norms))});
     });
 }
@@ -390,7 +414,8 @@ PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n)
         }
         const c10::cuda::OptionalCUDAGuard on(self.device);
         at::Tensor norm = empty({}, at::kFloat, self.device);
-        check(c_clip_grads(self.list, self.addresses.data(), (float)max_norm, flat, type, (float*)norm.data_ptr(), enter(self)));
+        const Turn turn(self);
+        check(c_clip_grads(self.list, self.addresses.data(), (float)max_norm, flat, type, (float*)norm.data_ptr(), turn.stream));
         if (flat) note_write(tensor(args[3], "out"));
         for (Py_ssize_t k = 0; !flat && k < ts.size(); ++k) note_write(ts[k]);
         return wrap(std::move(norm));
@@ -412,6 +437,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
         c_workspace_bytes = (decltype(c_workspace_bytes))address("apms_tensors_workspace_bytes");
         c_bind = (decltype(c_bind))address("apms_tensors_bind");
         c_destroy = (decltype(c_destroy))address("apms_tensors_destroy");
+        c_scratch_bytes = (decltype(c_scratch_bytes))address("apms_tensors_scratch_bytes");
+        c_use_scratch = (decltype(c_use_scratch))address("apms_tensors_use_scratch");
         c_grad_norm = (decltype(c_grad_norm))address("apms_grad_norm");
         c_clip_grads = (decltype(c_clip_grads))address("apms_clip_grads");
         c_rms_norm = (decltype(c_rms_norm))address("apms_rms_norm");

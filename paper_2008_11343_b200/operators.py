@@ -42,7 +42,9 @@ class TensorList:
 
     Built once for a model's gradients; each call is given the tensors again (their addresses may change between calls, their
     sizes, types and strides may not).  A tensor is contiguous, or rows of consecutive elements a fixed distance apart (a column
-    slice of a matrix).  Calls on another stream than the list's last one wait for that one.  `numel` is the total of elements."""
+    slice of a matrix).  Calls on another stream than the list's last one wait for that one.  Calls may be captured into a CUDA graph
+    on any stream: each works in memory of the graph's own, so replays need no order among the list's other calls; they read the list's tables,
+    so the list has to live as long as the graph.  The list itself is built outside a capture.  `numel` is the total of elements."""
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
         self._list, self.numel = _load().list_create(tensors)
