@@ -548,6 +548,35 @@ int64_t spanned_bytes(const TensorRecord& r)
     return ((r.numel / r.cols - 1) * r.stride + r.cols) * (int64_t)element_size(r.type);
 }
 
+// A tensor's bytes: `rows` rows of `length` bytes, `stride` apart.
+struct ByteRows {
+    int64_t first, rows, length, stride;
+    int64_t end() const { return first + (rows - 1) * stride + length; }
+};
+ByteRows byte_rows(const TensorRecord& r, const void* p)
+{
+    const int64_t es = (int64_t)element_size(r.type);
+    return {(int64_t)(uintptr_t)p, r.numel / r.cols, r.cols * es, r.stride * es};
+}
+
+// Whether two tensors share a byte, exactly: column slices of one matrix interleave without sharing any.
+bool share_bytes(const ByteRows& a, const ByteRows& b)
+{
+    if (a.end() <= b.first || b.end() <= a.first) return false;
+    if (a.rows == 1 && b.rows == 1) return true;
+    if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) {       // row by row of the shorter one
+        const ByteRows& few = a.rows <= b.rows ? a : b;
+        for (int64_t k = 0; k < few.rows; ++k)
+            if (share_bytes({few.first + k * few.stride, 1, few.length, few.stride}, a.rows <= b.rows ? b : a)) return true;
+        return false;
+    }
+    // Row i of a and row j of b share a byte where k = i - j has  k S < d + b.length  and  k S > d - a.length;  k lies between 1 - b.rows and a.rows - 1.
+    const int64_t S = a.rows > 1 ? a.stride : b.stride, d = b.first - a.first;
+    auto floor_div = [S](int64_t v) { return v / S - (v % S < 0); };
+    const int64_t least = floor_div(d - a.length) + 1, most = floor_div(d + b.length - 1);
+    return std::max(least, 1 - b.rows) <= std::min(most, a.rows - 1);
+}
+
 // Launches `kernel(addresses, first tensor, first tile, memory, ...)` over the list's tiles, as many tensors at a time as a
 // launch's arguments hold addresses.  `early`: the first launch may begin while the kernel before it drains.
 template <class... Params, class... Args>
@@ -619,13 +648,16 @@ apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float 
         }
     } else {
         try {
-            // of a tensor in rows its first row only: column slices of one matrix interleave without sharing elements
-            std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+            std::vector<ByteRows> all, open;             // open: those that reach behind the first byte of the one at hand
             for (size_t t = 0; t < count; ++t)
-                if (list->tensors[t].numel) spans.push_back({(uintptr_t)tensors_dev[t], (uintptr_t)tensors_dev[t] + (uintptr_t)list->tensors[t].cols * element_size(list->tensors[t].type)});
-            std::sort(spans.begin(), spans.end());
-            for (size_t k = 1; k < spans.size(); ++k)
-                if (spans[k].first < spans[k - 1].second) return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: two tensors of the list overlap in memory; clip into a flat gradient instead");
+                if (list->tensors[t].numel) all.push_back(byte_rows(list->tensors[t], tensors_dev[t]));
+            std::sort(all.begin(), all.end(), [](const ByteRows& a, const ByteRows& b) { return a.first < b.first; });
+            for (const ByteRows& r : all) {
+                open.erase(std::remove_if(open.begin(), open.end(), [&](const ByteRows& o) { return o.end() <= r.first; }), open.end());
+                for (const ByteRows& o : open)
+                    if (share_bytes(o, r)) return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: two tensors of the list overlap in memory; clip into a flat gradient instead");
+                open.push_back(r);
+            }
         } catch (const std::bad_alloc&) {
             return operator_fail(APMS_ERR_OOM, "apms_clip_grads: host allocation failed");
         }
