@@ -48,12 +48,16 @@ template <class... Parts>
     throw Refused(s.str());
 }
 
-void check(apms_status st)
+[[noreturn]] void fail(apms_status st, const std::string& message)
 {
-    if (st == APMS_OK) return;
-    PyObject* e = PyObject_CallFunction(g_error, "is", (int)st, c_last_error(nullptr));
+    PyObject* e = PyObject_CallFunction(g_error, "is", (int)st, message.c_str());
     if (e) { PyErr_SetObject(g_error, e); Py_DECREF(e); }
     throw Raised();
+}
+
+void check(apms_status st)
+{
+    if (st != APMS_OK) fail(st, c_last_error(nullptr));
 }
 
 template <class Body>
@@ -236,6 +240,7 @@ struct Layout {
     int64_t numel;
     at::ScalarType type;
     std::vector<int64_t> sizes, strides;             // empty: contiguous
+    bool turned;                                     // one run of memory, its elements in another order than their indexes'
 };
 
 struct TensorList {
@@ -298,10 +303,11 @@ PyObject* list_create(PyObject*, PyObject* tensors)
         for (Py_ssize_t k = 0; k < ts.size(); ++k) {
             const at::Tensor& t = ts[k];
             if (t.device() != self->device) refuse("the tensors of a TensorList lie on one CUDA device: ", t.device(), " and ", self->device);
-            const auto r = row_layout(t);
+            const bool turned = !t.is_contiguous() && t.is_non_overlapping_and_dense();
+            const auto r = turned ? std::pair<int64_t, int64_t>(t.numel(), t.numel()) : row_layout(t);
             numel.push_back(t.numel()); cols.push_back(r.first); strides.push_back(r.second);
             types.push_back((apms_grad_type)type_of(t, "a tensor"));
-            Layout l = {t.numel(), t.scalar_type(), {}, {}};
+            Layout l = {t.numel(), t.scalar_type(), {}, {}, turned};
             if (!t.is_contiguous()) { l.sizes = t.sizes().vec(); l.strides = t.strides().vec(); }
             self->layout.push_back(std::move(l));
             self->numel += t.numel();
@@ -342,6 +348,21 @@ void take_addresses(TensorList& self, const Sequence& ts, bool written)
         if (t.device() != self.device) refuse("tensor ", k, " lies on ", t.device(), ", the list on ", self.device);
         self.addresses[k] = written ? t.data_ptr() : const_cast<void*>(t.const_data_ptr());
     }
+}
+
+// For the flat gradient, which has the elements in their indexes' order: copies in that order of the tensors that lie in another.
+std::vector<at::Tensor> in_order(TensorList& self, const Sequence& ts, const at::Tensor& out)
+{
+    std::vector<at::Tensor> copies;
+    const char *f0 = static_cast<const char*>(out.const_data_ptr()), *f1 = f0 + out.nbytes();
+    for (Py_ssize_t k = 0; k < ts.size(); ++k) {
+        if (!self.layout[k].turned) continue;
+        const char* p = static_cast<const char*>(self.addresses[k]);
+        if (p < f1 && f0 < p + ts[k].nbytes()) fail(APMS_ERR_INVALID_ARG, "clip_grads: tensor " + std::to_string(k) + " overlaps the flat gradient without being in its place there");
+        copies.push_back(ts[k].contiguous());
+        self.addresses[k] = const_cast<void*>(copies.back().const_data_ptr());
+    }
+    return copies;
 }
 
 // The stream of one call, and the memory it writes to on the way.  The list's own memory is shared by its calls, so one on another stream than the last
@@ -413,6 +434,7 @@ PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n)
             flat = self.numel ? out.data_ptr() : self.workspace.data_ptr();       // an empty tensor has no address, and nothing is written
         }
         const c10::cuda::OptionalCUDAGuard on(self.device);
+        const std::vector<at::Tensor> copies = flat ? in_order(self, ts, tensor(args[3], "out")) : std::vector<at::Tensor>();
         at::Tensor norm = empty({}, at::kFloat, self.device);
         const Turn turn(self);
         check(c_clip_grads(self.list, self.addresses.data(), (float)max_norm, flat, type, (float*)norm.data_ptr(), turn.stream));

@@ -41,10 +41,12 @@ class TensorList:
     """The sizes, types and layouts of a list of CUDA tensors of one device, and the memory its calls work in.
 
     Built once for a model's gradients; each call is given the tensors again (their addresses may change between calls, their
-    sizes, types and strides may not).  A tensor is contiguous, or rows of consecutive elements a fixed distance apart (a column
-    slice of a matrix).  Calls on another stream than the list's last one wait for that one.  Calls may be captured into a CUDA graph
-    on any stream: each works in memory of the graph's own, so replays need no order among the list's other calls; they read the list's tables,
-    so the list has to live as long as the graph.  The list itself is built outside a capture.  `numel` is the total of elements."""
+    sizes, types and strides may not).  A tensor is dense - contiguous, or with its elements in another order (transposed, channels
+    last) - or rows of consecutive elements a fixed distance apart (a column slice of a matrix).  `numel` is the total of elements.
+
+    Calls on another stream than the list's last one wait for that one.  Calls may be captured into a CUDA graph on any stream: each
+    works in memory of the graph's own, so replays need no order among the list's other calls; they read the list's tables, so the list
+    has to live as long as the graph.  The list itself is built outside a capture."""
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
         self._list, self.numel = _load().list_create(tensors)
@@ -56,7 +58,8 @@ class TensorList:
     def clip_grads(self, tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[torch.Tensor] = None):
         """Multiplies every element by min(1, max_norm / norm) and returns the norm before clipping (a float32 scalar).
         Without `out` in place; with it the tensors stay as they are and the clipped elements are written to `out`, one
-        after the other: a flat gradient of self.numel elements for Context.warmup_step / compressed_step."""
+        after the other, each tensor's in the order of their indexes (one whose memory has another order is copied on the way): a flat
+        gradient of self.numel elements for Context.warmup_step / compressed_step."""
         return _ext.clip_grads(self._list, tensors, max_norm, out)
 
 
