@@ -523,11 +523,13 @@ k_rms_shifted(const RmsArgs a, int64_t rows, int x_room, int r_room)
     }
 }
 
-// Rows that do not fit into a CTA's shared memory: one CTA per row, any stride and alignment, read again for each pass.
+// Rows that do not fit into a CTA's shared memory: one CTA per row, any stride and alignment, read again for each pass.  A thread adds
+// width / 256 squares one after the other, up to 65,536: in binary64, where such a chain costs nothing (binary32: rstd off by 234 units in the last place on
+// equal elements, 2^20 wide).
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_rows(const RmsArgs a)
 {
-    __shared__ float red[kRmsThreads / 32];
+    __shared__ double red[kRmsThreads / 32];
     __shared__ uint32_t most;
     const int64_t row = blockIdx.x;
     const int64_t x0 = row * a.x_stride, r0 = row * a.r_stride, o0 = row * a.width;
@@ -535,12 +537,12 @@ k_rms_rows(const RmsArgs a)
         float h = load_element(a.x, x0 + c, a.x_type);
         return a.r ? h + load_element(a.r, r0 + c, a.r_type) : h;
     };
-    float acc = 0.0f;
+    double acc = 0.0;
     for (int64_t c = threadIdx.x; c < a.width; c += kRmsThreads) {
-        const float h = h_of(c);
-        acc = fmaf(h, h, acc);
+        const double h = (double)h_of(c);
+        acc = fma(h, h, acc);
     }
-    const float rstd = rsqrtf(block_total(acc, red) * a.inv_width + a.eps);
+    const float rstd = rsqrtf((float)block_total(acc, red) * a.inv_width + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
     if (!a.scales) {
         for (int64_t c = threadIdx.x; c < a.width; c += kRmsThreads) {
@@ -794,15 +796,15 @@ k_rms_back_shares(const RmsBackArgs a, int count)
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_back_rows(const RmsBackArgs a)
 {
-    __shared__ float red[kRmsThreads / 32];
+    __shared__ double red[kRmsThreads / 32];
     const int64_t row = blockIdx.x;
     const float rstd = a.rstd[row];
-    float acc = 0.0f;
+    double acc = 0.0;                                // as in k_rms_rows: the chain is up to 65,536 long
     for (int64_t c = threadIdx.x; c < a.width; c += kRmsThreads) {
         const float xh = load_element(a.h, row * a.h_stride + c, a.h_type) * rstd;
-        acc = fmaf(load_element(a.w, c, a.w_type) * load_element(a.dy, row * a.dy_stride + c, a.dy_type), xh, acc);
+        acc = fma((double)(load_element(a.w, c, a.w_type) * load_element(a.dy, row * a.dy_stride + c, a.dy_type)), (double)xh, acc);
     }
-    const float mean = block_total(acc, red) / (float)a.width;
+    const float mean = (float)(block_total(acc, red) / (double)a.width);
     for (int64_t c = threadIdx.x; c < a.width; c += kRmsThreads) {
         const float xh = load_element(a.h, row * a.h_stride + c, a.h_type) * rstd;
         const float v = load_element(a.w, c, a.w_type) * load_element(a.dy, row * a.dy_stride + c, a.dy_type);
