@@ -144,10 +144,6 @@ constexpr int kTeamWarps = 16;                   // a row's at most: with 32 ele
 
 // 16 bytes from global to shared memory without a register; both 16-byte aligned.  A thread copies what it reads itself,
 // so its own wait is all the order that is needed.
-__device__ __forceinline__ void copy16_async(const char* to_shared, const char* from)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to_shared)), "l"(from) : "memory");
-}
 __device__ __forceinline__ void copy16_async(uint32_t to_shared, const char* from)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to_shared), "l"(from) : "memory");
@@ -862,8 +858,10 @@ struct RmsLaunch {
         const dim3 block(t.warps * 32, t.rows);
         const size_t x_bytes = (size_t)t.threads * NU * 16, grid = (rows + t.rows - 1) / std::max(1, t.rows);
         if (!t.threads) return false;
-        return a.r ? with_shared<k_rms_staged<XT, RT, WT, true, NU>>(block, grid, x_bytes * (1 + RS / XS), stream, e, a, rows)
-                   : with_shared<k_rms_staged<XT, RT, WT, false, NU>>(block, grid, x_bytes, stream, e, a, rows);
+        if constexpr (RT == XT) {                    // without a residual its type is x's
+            if (!a.r) return with_shared<k_rms_staged<XT, RT, WT, false, NU>>(block, grid, x_bytes, stream, e, a, rows);
+        }
+        return with_shared<k_rms_staged<XT, RT, WT, true, NU>>(block, grid, x_bytes * (1 + RS / XS), stream, e, a, rows);
     }
 
     template <int NU>
@@ -874,8 +872,10 @@ struct RmsLaunch {
         const int padded = t.warps * NU * 128, x_room = padded * XS + 16, r_room = a.r ? padded * RS + 16 : 0;
         const dim3 block(t.warps * 32, t.rows);
         const size_t grid = (rows + t.rows - 1) / t.rows, shared = (size_t)t.rows * (x_room + r_room);
-        return a.r ? with_shared<k_rms_shifted<XT, RT, WT, true, NU>>(block, grid, shared, stream, e, a, rows, x_room, r_room)
-                   : with_shared<k_rms_shifted<XT, RT, WT, false, NU>>(block, grid, shared, stream, e, a, rows, x_room, r_room);
+        if constexpr (RT == XT) {
+            if (!a.r) return with_shared<k_rms_shifted<XT, RT, WT, false, NU>>(block, grid, shared, stream, e, a, rows, x_room, r_room);
+        }
+        return with_shared<k_rms_shifted<XT, RT, WT, true, NU>>(block, grid, shared, stream, e, a, rows, x_room, r_room);
     }
 
     // KERNEL with as much shared memory as it asks for, within what a CTA can have
@@ -955,7 +955,11 @@ bool launch_back_width(const RmsBackArgs& a, cudaStream_t stream, cudaError_t* e
     if (warps8 == 1) return launch_back<XT, HT, WT, CARRY, VECTOR, N8, 256>(a, 1, stream, e);
     if (warps16 <= 8 && launch_back<XT, HT, WT, CARRY, VECTOR, N16, 256>(a, (int)warps16, stream, e)) return true;
     if (warps16 <= 16 && launch_back<XT, HT, WT, CARRY, VECTOR, N16, 512>(a, (int)warps16, stream, e)) return true;
-    return warps32 <= 16 && launch_back<XT, HT, WT, CARRY, VECTOR, N32, 512>(a, (int)warps32, stream, e);
+    // wider than 8192: three rows off the boundary fit into shared memory in 16 bits only
+    constexpr int XS = XT == APMS_GRAD_F32 ? 4 : 2, HS = HT == APMS_GRAD_F32 ? 4 : 2;
+    if constexpr (VECTOR || (size_t)BackShape<XT, HT, VECTOR, N32>::STAGES * (XS + 2 * HS) * 8192 <= kMostShared)
+        return warps32 <= 16 && launch_back<XT, HT, WT, CARRY, VECTOR, N32, 512>(a, (int)warps32, stream, e);
+    return false;
 }
 
 template <int XT, int HT, int WT>
