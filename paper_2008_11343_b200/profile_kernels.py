@@ -11,6 +11,7 @@ the bytes the launch has to move, so that the same command is useful without a p
 from __future__ import annotations
 
 import argparse
+import itertools
 import json
 import sys
 
@@ -114,33 +115,43 @@ def _operator_cases():
     def tensor(rows, width, dtype=torch.bfloat16):
         return torch.empty(rows, width, device="cuda", dtype=dtype).normal_()
 
-    def gradients(clip, big=8):
+    def gradients(clip, big=8, in_place=False):
         sizes = [4 << 20] * big + [1 << 20] * 32 + [1024] * 64                   # big = 8: 67 M elements
         grads = [torch.empty(n, device="cuda").normal_() for n in sizes]
         tensors, d = O.TensorList(grads), sum(sizes)
         flat = torch.empty(d, device="cuda")
+        if in_place:
+            calls = itertools.count()
+            return lambda: tensors.clip_grads(grads, 1e3 * 0.99 ** next(calls)), 8 * d       # each limit below the norm that the last one left
         if clip:
             return lambda: tensors.clip_grads(grads, 1.0, out=flat), 8 * d
         return lambda: tensors.grad_norm(grads), 4 * d
 
-    def forward(rows, width, dtype=torch.bfloat16, group=None):
-        x, r, w = tensor(rows, width, dtype), tensor(rows, width, dtype), tensor(1, width, dtype)[0]
-        out = dtype.itemsize if group is None else 1
+    def forward(rows, width, dtype=torch.bfloat16, group=None, stream=None):
+        stream = stream or dtype
+        x, r, w = tensor(rows, width, dtype), tensor(rows, width, stream), tensor(1, width, dtype)[0]
+        nbytes = rows * width * (dtype.itemsize + 2 * stream.itemsize + (dtype.itemsize if group is None else 1))
         if group is None:
-            return lambda: O.rms_norm_forward(x, w, r), rows * width * (3 * dtype.itemsize + out)
-        return lambda: O.rms_norm_fp8(x, w, r, group=group), rows * width * (3 * dtype.itemsize + out)
+            return lambda: O.rms_norm_forward(x, w, r), nbytes
+        return lambda: O.rms_norm_fp8(x, w, r, group=group), nbytes
 
-    def backward(rows, width):
-        dy, h, dh, w = (tensor(rows, width) for _ in range(4))
+    def backward(rows, width, dtype=torch.bfloat16, stream=None):
+        both = stream is not None                                                # dx in both types
+        stream = stream or dtype
+        dy, h, dh, w = tensor(rows, width, dtype), tensor(rows, width, stream), tensor(rows, width, stream), tensor(1, width, dtype)[0]
         rstd = torch.rand(rows, device="cuda")
-        return lambda: O.rms_norm_backward(dy, h, w[0], rstd, dh), 8 * rows * width
+        return lambda: O.rms_norm_backward(dy, h, w, rstd, dh), rows * width * (2 * dtype.itemsize + (3 if both else 2) * stream.itemsize)
 
     return {
         "k_tile_squares": lambda: gradients(False), "k_list_norm": lambda: gradients(False), "k_one_norm": lambda: gradients(False, 4), "k_scale_tiles": lambda: gradients(True),
+        "k_scale_tiles_in_place": lambda: gradients(True, in_place=True),
         "k_rms_staged": lambda: forward(8192, 4096), "k_rms_staged_row_scale": lambda: forward(8192, 4096, group=0),
         "k_rms_staged_column_scales": lambda: forward(8192, 4096, group=128), "k_rms_staged_f32": lambda: forward(8192, 4096, torch.float32),
+        "k_rms_staged_f32_stream": lambda: forward(8192, 4096, stream=torch.float32), "k_rms_rows": lambda: forward(512, 65_544, torch.float32),
         "k_rms_narrow": lambda: forward(200_000, 128), "k_rms_shifted": lambda: forward(8192, 4095),
-        "k_rms_back_team": lambda: backward(8192, 4096), "k_rms_back_team_shifted": lambda: backward(8192, 4095), "k_rms_back_shares": lambda: backward(8192, 4096),
+        "k_rms_back_team": lambda: backward(8192, 4096), "k_rms_back_team_shifted": lambda: backward(8192, 4095), "k_rms_back_team_f32": lambda: backward(8192, 4096, torch.float32),
+        "k_rms_back_team_f32_stream": lambda: backward(8192, 4096, stream=torch.float32), "k_rms_back_team_wide": lambda: backward(4096, 16_384), "k_rms_back_rows": lambda: backward(512, 65_544, torch.float32),
+        "k_rms_back_shares": lambda: backward(8192, 4096),
     }
 
 
