@@ -553,10 +553,10 @@ struct ByteRows {
     int64_t first, rows, length, stride;
     int64_t end() const { return first + (rows - 1) * stride + length; }
 };
-ByteRows byte_rows(const TensorRecord& r, const void* p)
+ByteRows byte_rows(const TensorRecord& r, uintptr_t p)
 {
     const int64_t es = (int64_t)element_size(r.type);
-    return {(int64_t)(uintptr_t)p, r.numel / r.cols, r.cols * es, r.stride * es};
+    return {(int64_t)p, r.contiguous ? 1 : r.numel / r.cols, r.cols * es, r.stride * es};
 }
 
 // Whether two tensors share a byte, exactly: column slices of one matrix interleave without sharing any.
@@ -575,6 +575,30 @@ bool share_bytes(const ByteRows& a, const ByteRows& b)
     auto floor_div = [S](int64_t v) { return v / S - (v % S < 0); };
     const int64_t least = floor_div(d - a.length) + 1, most = floor_div(d + b.length - 1);
     return std::max(least, 1 - b.rows) <= std::min(most, a.rows - 1);
+}
+
+// Whether no two tensors of `all` share a byte.  Slices of one matrix mostly lie side by side in its rows, which one pass over their
+// columns shows (300 of them: 45,000 pairs otherwise, 260 us); what that leaves open is asked pair by pair.
+bool lie_apart(const std::vector<ByteRows>& all)
+{
+    if (all.size() < 2) return true;
+    int64_t S = 0;
+    bool matrix = true;
+    for (const ByteRows& r : all)
+        if (r.rows > 1) { matrix = matrix && (!S || S == r.stride); S = r.stride; }
+    if (matrix && S) {
+        std::vector<std::pair<int64_t, int64_t>> columns;
+        columns.reserve(all.size());
+        for (const ByteRows& r : all) columns.push_back({r.first % S, r.length});
+        std::sort(columns.begin(), columns.end());
+        bool side_by_side = columns.back().first + columns.back().second <= columns.front().first + S;
+        for (size_t k = 1; k < columns.size(); ++k) side_by_side = side_by_side && columns[k - 1].first + columns[k - 1].second <= columns[k].first;
+        if (side_by_side) return true;
+    }
+    for (size_t k = 1; k < all.size(); ++k)
+        for (size_t j = 0; j < k; ++j)
+            if (share_bytes(all[j], all[k])) return false;
+    return true;
 }
 
 // Launches `kernel(addresses, first tensor, first tile, memory, ...)` over the list's tiles, as many tensors at a time as a
@@ -648,16 +672,24 @@ apms_status apms_clip_grads(apms_tensors* list, void* const* tensors_dev, float 
         }
     } else {
         try {
-            std::vector<ByteRows> all, open;             // open: those that reach behind the first byte of the one at hand
+            std::vector<std::pair<uintptr_t, size_t>> by_address;
+            by_address.reserve(count);
             for (size_t t = 0; t < count; ++t)
-                if (list->tensors[t].numel) all.push_back(byte_rows(list->tensors[t], tensors_dev[t]));
-            std::sort(all.begin(), all.end(), [](const ByteRows& a, const ByteRows& b) { return a.first < b.first; });
-            for (const ByteRows& r : all) {
-                open.erase(std::remove_if(open.begin(), open.end(), [&](const ByteRows& o) { return o.end() <= r.first; }), open.end());
-                for (const ByteRows& o : open)
-                    if (share_bytes(o, r)) return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: two tensors of the list overlap in memory; clip into a flat gradient instead");
-                open.push_back(r);
+                if (list->tensors[t].numel) by_address.push_back({(uintptr_t)tensors_dev[t], t});
+            if (!std::is_sorted(by_address.begin(), by_address.end())) std::sort(by_address.begin(), by_address.end());
+            std::vector<ByteRows> knot;                  // consecutive ones, each beginning before the end of those before it
+            int64_t reach = 0;
+            bool apart = true;
+            for (const auto& [address, t] : by_address) {
+                const ByteRows r = byte_rows(list->tensors[t], address);
+                if (r.first >= reach) {
+                    apart = apart && lie_apart(knot);
+                    knot.clear();
+                }
+                knot.push_back(r);
+                reach = std::max(reach, r.end());
             }
+            if (!apart || !lie_apart(knot)) return operator_fail(APMS_ERR_INVALID_ARG, "apms_clip_grads: two tensors of the list overlap in memory; clip into a flat gradient instead");
         } catch (const std::bad_alloc&) {
             return operator_fail(APMS_ERR_OOM, "apms_clip_grads: host allocation failed");
         }
