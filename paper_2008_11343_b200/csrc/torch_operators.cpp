@@ -247,6 +247,7 @@ struct TensorList {
     apms_tensors* list = nullptr;
     std::vector<Layout> layout;
     std::vector<void*> addresses;                    // of the running call
+    std::vector<at::TensorImpl*> written;            // ... and the tensors that it writes in place
     int64_t numel = 0;
     at::Device device{at::kCUDA, 0};
     at::Tensor workspace;
@@ -339,6 +340,7 @@ TensorList& list_of(PyObject* capsule)
 void take_addresses(TensorList& self, const Sequence& ts, bool written)
 {
     if (ts.size() != (Py_ssize_t)self.layout.size()) refuse("the list has ", self.layout.size(), " tensors, not ", ts.size());
+    self.written.clear();
     for (Py_ssize_t k = 0; k < ts.size(); ++k) {
         const at::Tensor& t = ts[k];
         const Layout& l = self.layout[k];
@@ -347,6 +349,7 @@ void take_addresses(TensorList& self, const Sequence& ts, bool written)
             refuse("tensor ", k, " has other strides than the list's: ", t.strides());
         if (t.device() != self.device) refuse("tensor ", k, " lies on ", t.device(), ", the list on ", self.device);
         self.addresses[k] = written ? t.data_ptr() : const_cast<void*>(t.const_data_ptr());
+        if (written) self.written.push_back(t.unsafeGetTensorImpl());
     }
 }
 
@@ -397,9 +400,9 @@ private:
 
 // Autograd's notice that a tensor was written: a graph that has saved it raises in its backward pass.  (Inference tensors have no version, and
 // no graph can save them.)
-void note_write(const at::Tensor& t)
+void note_write(at::TensorImpl* t)
 {
-    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    if (!t->is_inference()) t->bump_version();
 }
 
 PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n)
@@ -438,8 +441,8 @@ PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n)
         at::Tensor norm = empty({}, at::kFloat, self.device);
         const Turn turn(self);
         check(c_clip_grads(self.list, self.addresses.data(), (float)max_norm, flat, type, (float*)norm.data_ptr(), turn.stream));
-        if (flat) note_write(tensor(args[3], "out"));
-        for (Py_ssize_t k = 0; !flat && k < ts.size(); ++k) note_write(ts[k]);
+        if (flat) note_write(tensor(args[3], "out").unsafeGetTensorImpl());
+        for (at::TensorImpl* t : self.written) note_write(t);
         return wrap(std::move(norm));
     });
 }
