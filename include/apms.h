@@ -558,11 +558,12 @@ size_t      apms_tensors_workspace_bytes(const apms_tensors* list);
 apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t bytes, void* cuda_stream);
 void        apms_tensors_destroy(apms_tensors* list);
 
-/* What a call writes of the workspace (sums, a ticket, the clip factor) can be put elsewhere: the calls after this one use
- * scratch_dev (>= apms_tensors_scratch_bytes, 256-byte aligned; the ticket is zeroed on `cuda_stream`, without synchronising), or with NULL the
- * workspace again.  The tables, which no call writes, stay where they are.  For calls captured into a CUDA graph, whose replays no
- * stream order holds apart from the list's other calls: between two of these calls, each captured call in scratch memory that
- * belongs to the graph.  The zeroing is captured with them, so one call follows it. */
+/* What a call writes of the workspace (sums, the clip factor) can be put elsewhere: the ONE call after this one uses
+ * scratch_dev (>= apms_tensors_scratch_bytes, 256-byte aligned) and a ticket of its own, then NULL gives the workspace back.
+ * For a call captured into a CUDA graph, whose replays no stream order holds apart from the list's other calls, in
+ * scratch memory that belongs to the graph.  The graph reads the list's tables and uses the ticket: it must not be replayed after
+ * the workspace is freed or bound again.  The list has 1023 tickets for such calls; from then on a ticket is cleared on `cuda_stream` before
+ * each.  Nothing synchronises. */
 size_t      apms_tensors_scratch_bytes(const apms_tensors* list);
 apms_status apms_tensors_use_scratch(apms_tensors* list, void* scratch_dev, size_t bytes, void* cuda_stream);
 

@@ -18,6 +18,7 @@ constexpr int kTotalThreads = 512;
 constexpr int kAloneTiles = kNormThreads;      // lists this short (4 MB): the CTA that finishes last adds up, a launch less (a call on six small
                                          // tensors 9.8 -> 8.2 us; on the GPU the ticket costs what the second kernel did)
 constexpr int kOneTiles = 8192, kOneThreads = 1024;      // lists this short: one CTA adds up, from shared memory
+constexpr int kTickets = 1024;           // of a list: one for its plain calls, one for each captured call (4 KB)
 constexpr int kListPointers = 500;       // tensors' addresses in a launch's arguments
 
 struct __align__(16) TileRecord {
@@ -403,29 +404,33 @@ struct apms_tensors {
         return tiles.size() <= (size_t)kOneTiles ? Route::one : Route::groups;
     }
 
-    // Byte offsets of the tables and, from tile_sum on, of what the calls write in the workspace.
-    struct Places { size_t tensors, groups, tile_sum, group_sum, ticket, bytes; };
+    // Byte offsets of the tables, the tickets and, from tile_sum on, of what a call writes before it reads it in the workspace.
+    struct Places { size_t tensors, groups, tickets, tile_sum, group_sum, last, bytes; };
     Places places() const
     {
         auto up = [](size_t v) { return (v + 255) / 256 * 256; };
         Places p;
         p.tensors = up(tiles.size() * sizeof(TileRecord));
         p.groups = p.tensors + up(tensors.size() * sizeof(TensorRecord));
-        p.tile_sum = p.groups + up(groups.size() * sizeof(GroupRecord));
+        p.tickets = p.groups + up(groups.size() * sizeof(GroupRecord));
+        p.tile_sum = p.tickets + kTickets * sizeof(unsigned);
         p.group_sum = p.tile_sum + up(tiles.size() * sizeof(double));
-        p.ticket = p.group_sum + up(groups.size() * sizeof(double));     // and the factor behind it
-        p.bytes = p.ticket + 256;
+        p.last = p.group_sum + up(groups.size() * sizeof(double));       // the factor, and a ticket beside it
+        p.bytes = p.last + 256;
         return p;
     }
-    // The calls' sums, ticket and factor at `p`, laid out as from tile_sum on.
-    void write_at(char* p)
+    int tickets_taken = 1;               // the first is the plain calls'
+
+    // The calls' sums and factor at `p`, laid out as from tile_sum on, and their ticket.
+    void write_at(char* p, unsigned* ticket)
     {
         const Places at = places();
         m.tile_sum = (double*)p;
         m.group_sum = (double*)(p + (at.group_sum - at.tile_sum));
-        m.ticket = (unsigned*)(p + (at.ticket - at.tile_sum));
-        m.factor = (float*)(m.ticket + 1);
+        m.factor = (float*)(p + (at.last - at.tile_sum));
+        m.ticket = ticket;
     }
+    unsigned* tickets() const { return (unsigned*)((char*)m.tiles + places().tickets); }
 };
 
 extern "C" {
@@ -490,7 +495,7 @@ apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t by
     OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws, list->tiles.data(), list->tiles.size() * sizeof(TileRecord), cudaMemcpyHostToDevice, stream));
     OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws + at.tensors, list->tensors.data(), list->tensors.size() * sizeof(TensorRecord), cudaMemcpyHostToDevice, stream));
     OPERATOR_CUDA("apms_tensors_bind", cudaMemcpyAsync(ws + at.groups, list->groups.data(), list->groups.size() * sizeof(GroupRecord), cudaMemcpyHostToDevice, stream));
-    OPERATOR_CUDA("apms_tensors_bind", cudaMemsetAsync(ws + at.ticket, 0, at.bytes - at.ticket, stream));
+    OPERATOR_CUDA("apms_tensors_bind", cudaMemsetAsync(ws + at.tickets, 0, kTickets * sizeof(unsigned), stream));
     OPERATOR_CUDA("apms_tensors_bind", cudaStreamSynchronize(stream));
     ListMemory& m = list->m;
     m.tiles = (const TileRecord*)ws;
@@ -498,7 +503,8 @@ apms_status apms_tensors_bind(apms_tensors* list, void* workspace_dev, size_t by
     m.group = (const GroupRecord*)(ws + at.groups);
     m.count = (int)list->tensors.size();
     m.groups = (int)list->groups.size();
-    list->write_at(ws + at.tile_sum);
+    list->tickets_taken = 1;
+    list->write_at(ws + at.tile_sum, list->tickets());
     return APMS_OK;
 }
 
@@ -513,15 +519,24 @@ apms_status apms_tensors_use_scratch(apms_tensors* list, void* scratch_dev, size
 {
     if (!list || !list->m.tiles) return operator_fail(APMS_ERR_BAD_STATE, "apms_tensors_use_scratch: the list has no workspace (apms_tensors_bind)");
     if (!scratch_dev) {
-        list->write_at((char*)list->m.tiles + list->places().tile_sum);
+        list->write_at((char*)list->m.tiles + list->places().tile_sum, list->tickets());
         return APMS_OK;
     }
     if ((uintptr_t)scratch_dev & 255u) return operator_fail(APMS_ERR_INVALID_ARG, "apms_tensors_use_scratch: the scratch memory must be 256-byte aligned");
     if (bytes < apms_tensors_scratch_bytes(list)) return operator_fail(APMS_ERR_OOM, "apms_tensors_use_scratch: scratch memory smaller than apms_tensors_scratch_bytes()");
     const apms_tensors::Places at = list->places();
-    if (list->route() != apms_tensors::Route::one)       // the ticket is all that has to be there before a call
-        OPERATOR_CUDA("apms_tensors_use_scratch", cudaMemsetAsync((char*)scratch_dev + (at.ticket - at.tile_sum), 0, sizeof(unsigned), (cudaStream_t)cuda_stream));
-    list->write_at((char*)scratch_dev);
+    unsigned* ticket = nullptr;
+    if (list->route() != apms_tensors::Route::one) {
+        // A ticket has to be zero before its call, which leaves it so.  The list's own are, so the call need not clear one (3.6 us more in a graph of
+        // a 5.6 us call); when they have run out, the one beside the factor is cleared on the stream.
+        if (list->tickets_taken < kTickets) {
+            ticket = list->tickets() + list->tickets_taken++;
+        } else {
+            ticket = (unsigned*)((char*)scratch_dev + (at.last - at.tile_sum)) + 1;
+            OPERATOR_CUDA("apms_tensors_use_scratch", cudaMemsetAsync(ticket, 0, sizeof(unsigned), (cudaStream_t)cuda_stream));
+        }
+    }
+    list->write_at((char*)scratch_dev, ticket);
     return APMS_OK;
 }
 

@@ -80,3 +80,25 @@ def test_a_list_is_built_outside():
         norm = tl.grad_norm(ts)[0]                                           # the capture is still sound
     graph.replay()
     assert torch.equal(norm, want)
+
+
+def test_more_captured_calls_than_a_list_has_tickets():
+    """1100 calls in graphs of 100, replayed on two streams at once: each call clips its own tensors to its own norm."""
+    sets = [[torch.full((n,), float(k + 1), device="cuda") for n in (900, 5)] for k in range(2)]
+    tl = O.TensorList(sets[0])
+    wants = [tl.grad_norm(ts)[0] for ts in sets]
+    graphs, norms = [], []
+    for k in range(11):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            norms.append([tl.grad_norm(sets[(k + j) % 2])[0] for j in range(100)])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for k, graph in enumerate(graphs):
+            with torch.cuda.stream(streams[k % 2]):
+                graph.replay()
+    torch.cuda.synchronize()
+    for k, got in enumerate(norms):
+        assert all(torch.equal(n, wants[(k + j) % 2]) for j, n in enumerate(got))
+    assert torch.equal(tl.grad_norm(sets[1])[0], wants[1])
