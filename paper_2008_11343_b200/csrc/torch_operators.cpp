@@ -249,6 +249,7 @@ struct TensorList {
     std::vector<void*> addresses;                    // of the running call
     std::vector<at::TensorImpl*> written;            // ... and the tensors that it writes in place
     int64_t numel = 0;
+    bool turned = false;                             // some tensor's layout is
     at::Device device{at::kCUDA, 0};
     at::Tensor workspace;
     c10::cuda::CUDAStream stream = c10::cuda::getDefaultCUDAStream(0);
@@ -312,6 +313,7 @@ PyObject* list_create(PyObject*, PyObject* tensors)
             if (!t.is_contiguous()) { l.sizes = t.sizes().vec(); l.strides = t.strides().vec(); }
             self->layout.push_back(std::move(l));
             self->numel += t.numel();
+            self->turned |= turned;
         }
         self->addresses.resize(numel.size());
         check(c_create(&self->list, (int)numel.size(), numel.data(), types.data(), cols.data(), strides.data()));
@@ -437,7 +439,7 @@ PyObject* clip_grads(PyObject*, PyObject* const* args, Py_ssize_t n)
             flat = self.numel ? out.data_ptr() : self.workspace.data_ptr();       // an empty tensor has no address, and nothing is written
         }
         const c10::cuda::OptionalCUDAGuard on(self.device);
-        const std::vector<at::Tensor> copies = flat ? in_order(self, ts, tensor(args[3], "out")) : std::vector<at::Tensor>();
+        const std::vector<at::Tensor> copies = flat && self.turned ? in_order(self, ts, tensor(args[3], "out")) : std::vector<at::Tensor>();
         at::Tensor norm = empty({}, at::kFloat, self.device);
         const Turn turn(self);
         check(c_clip_grads(self.list, self.addresses.data(), (float)max_norm, flat, type, (float*)norm.data_ptr(), turn.stream));
