@@ -616,7 +616,7 @@ apms_status apms_rms_norm(const apms_rms_norm_args* args, void* cuda_stream);
  * dh (NULL or rows of h_type, dh_stride apart) being the gradient that arrives on the residual stream (on the
  * output h).  dx is the gradient of x and of the residual alike: written to dx (dy_type, contiguous rows) and, where
  * dresidual is not NULL, to dresidual (h_type, contiguous rows) too.  h: dy_type or binary32.  dweight: `width`
- * elements of weight_type, summed in binary32 in an order fixed by the shape alone.
+ * elements of weight_type, summed in binary32 in an order fixed by the shape and the GPU's number of SMs.
  * workspace_dev: apms_rms_norm_backward_workspace_bytes(rows, width), 16-byte aligned. */
 typedef struct {
     int64_t rows, width;

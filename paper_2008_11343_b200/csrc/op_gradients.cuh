@@ -4,7 +4,7 @@
 //   S_t = sum_j g_tj^2 (binary64),  norm = sqrt(sum_t S_t),  c = norm <= max ? 1 : max / norm,  out = g * c
 //
 // The list is cut into tiles; a tile lies in one tensor and is one CTA.  Both readings are HBM streams, 2 operations per element: on a
-// list of 1.34 GB (392 tensors, binary32) the norm takes 192 us = 7.0 TB/s, clipping into the flat gradient 580 us = 6.9 TB/s over its two
+// list of 1.34 GB (391 tensors, binary32) the norm takes 192 us = 7.0 TB/s, clipping into the flat gradient 580 us = 6.9 TB/s over its two
 // readings and one writing; what bounds lists below some 100 MB is the launches and the ramp of one wave of CTAs (50 MB: 14 us).
 #pragma once
 

@@ -140,7 +140,7 @@ __device__ __forceinline__ void store_unit(char* row, const float2* f, int unit,
     }
 }
 
-constexpr int kTeamWarps = 16;                   // a row's at most: with 32 elements a lane, rows of up to 16,384
+constexpr int kTeamWarps = 16;                   // a row's at most
 
 // 16 bytes from global to shared memory without a register; both 16-byte aligned.  A thread copies what it reads itself,
 // so its own wait is all the order that is needed.
@@ -519,7 +519,8 @@ k_rms_shifted(const RmsArgs a, int64_t rows, int x_room, int r_room)
     }
 }
 
-// Rows that do not fit into a CTA's shared memory: one CTA per row, any stride and alignment, read again for each pass.  A thread adds
+// Rows that do not fit into a team's units or a CTA's shared memory (wider than 65,536 in 16 bits, 53,248 with a residual, 36,864 with a binary32 one, 32,768
+// in binary32, 26,624 with a residual; off the 16-byte boundary 32,768, and 26,624 in binary32 with a residual): one CTA per row, any stride and alignment, read again for each pass.  A thread adds
 // width / 256 squares one after the other, up to 65,536: in binary64, where such a chain costs nothing (binary32: rstd off by 234 units in the last place on
 // equal elements, 2^20 wide).
 __global__ void __launch_bounds__(kRmsThreads)
@@ -788,7 +789,8 @@ k_rms_back_shares(const RmsBackArgs a, int count)
     }
 }
 
-// Rows wider than a team's registers hold (16,384): read twice, once for dx and once for dweight.
+// Rows wider than a team's registers hold (16,384), or off the 16-byte boundary and wider than three stages of dy, h and dh in shared memory
+// (12,504 in 16 bits, 7504 with a binary32 stream, 6252 in binary32): read twice, once for dx and once for dweight.
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_back_rows(const RmsBackArgs a)
 {
