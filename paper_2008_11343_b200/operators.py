@@ -44,8 +44,8 @@ class TensorList:
     sizes, types and strides may not).  A tensor is dense - contiguous, or with its elements in another order (transposed, channels
     last) - or rows of consecutive elements a fixed distance apart (a column slice of a matrix).  `numel` is the total of elements.
 
-    Calls on another stream than the list's last one wait for that one.  Calls may be captured into a CUDA graph on any stream: each
-    works in memory of the graph's own, so replays need no order among the list's other calls; they read the list's tables, so the list
+    Calls on another stream than the list's last one wait for that one.  Calls may be captured by torch.cuda.graph on any stream: each
+    works in memory of the graph's pool, so replays need no order among the list's other calls; they read the list's tables, so the list
     has to live as long as the graph.  The list itself is built outside a capture."""
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
