@@ -521,7 +521,7 @@ k_rms_shifted(const RmsArgs a, int64_t rows, int x_room, int r_room)
 
 // Rows that do not fit into a team's units or a CTA's shared memory (wider than 65,536 in 16 bits, 53,248 with a residual, 36,864 with a binary32 one, 32,768
 // in binary32, 26,624 with a residual; off the 16-byte boundary 32,768, and 26,624 in binary32 with a residual): one CTA per row, any stride and alignment, read again for each pass.  A thread adds
-// width / 256 squares one after the other, up to 65,536: in binary64, where such a chain costs nothing (binary32: rstd off by 234 units in the last place on
+// width / 256 squares one after the other, up to 65,536: in binary64 (1 % of the time; binary32: rstd off by up to 356 units in the last place on
 // equal elements, 2^20 wide).
 __global__ void __launch_bounds__(kRmsThreads)
 k_rms_rows(const RmsArgs a)
