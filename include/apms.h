@@ -633,6 +633,110 @@ typedef struct {
 size_t      apms_rms_norm_backward_workspace_bytes(int64_t rows, int64_t width);
 apms_status apms_rms_norm_backward(const apms_rms_norm_backward_args* args, void* cuda_stream);
 
+/* --- embedding lookup with scaling, and its gradient ---------------------------------------
+ *
+ * out[i] = weight[tokens[i]] * scale, formed in binary32 and rounded once to out_type; a row of zeros where tokens[i] is not in
+ * [0, vocab).  tokens: `count` numbers of token_bytes (4 or 8) each; weight: vocab rows, weight_stride elements apart; out: contiguous rows.
+ * count * width <= APMS_EMBEDDING_MAX, width <= 2^19.  Addresses need only be aligned to their element size throughout. */
+#define APMS_EMBEDDING_MAX ((int64_t)1 << 40)
+typedef struct {
+    int64_t count, vocab, width;
+    const void* tokens;   int token_bytes;
+    const void* weight;   int64_t weight_stride;   apms_grad_type weight_type;
+    float       scale;
+    void*       out;      apms_grad_type out_type;
+} apms_embedding_args;
+apms_status apms_embedding(const apms_embedding_args* args, void* cuda_stream);
+
+/* dweight[v] = scale * (sum of dout[i] over the i with tokens[i] = v), 0 for a v that is no token: all vocab rows are written, contiguous.
+ * Summed in binary32, in an order fixed by count, vocab, width and the tokens; rounded once to dweight_type.  Tokens outside
+ * [0, vocab) contribute nothing.  dout: rows dout_stride >= 0 elements apart.  dweight must not overlap dout or tokens.
+ * workspace_dev: apms_embedding_backward_workspace_bytes(count, vocab, width), 256-byte aligned (not needed for count 0). */
+typedef struct {
+    int64_t count, vocab, width;
+    const void* tokens;   int token_bytes;
+    const void* dout;     int64_t dout_stride;     apms_grad_type dout_type;
+    float       scale;
+    void*       dweight;  apms_grad_type dweight_type;
+    void*       workspace_dev; size_t workspace_bytes;
+} apms_embedding_backward_args;
+size_t      apms_embedding_backward_workspace_bytes(int64_t count, int64_t vocab, int64_t width);
+apms_status apms_embedding_backward(const apms_embedding_backward_args* args, void* cuda_stream);
+
+/* --- dropout at a residual junction ---------------------------------------------------------
+ *
+ * h = residual + (kept ? x * s : 0) (no addition without a residual), formed in binary32 and rounded once to h_type.  The mask is not
+ * stored; it is a function of (seed, step, site, i), i being the element's index row * width + column: eight consecutive elements
+ * take one block of Philox 4x32 with 7 rounds, key = seed (low word first), counter = (i / 8, site, step's low word, step's high word), and
+ * element i the 16 bits number i mod 8 of its four words (low half of the first word first); it is kept where they are >= T = floor(65536 p + 1/2).
+ * s = 65536 / (65536 - T).  What is dropped counts as 0 whatever it is.  rng_dev: two 64-bit integers {seed, step} in device memory, read when the kernel
+ * runs, so that a captured call follows them; used_dev (NULL or two such) receives what was read.
+ * The gradient of x is the same call with dh in the place of x, no residual and the same numbers.
+ * x: rows x_stride apart; residual (NULL or of h_type): rows residual_stride apart; h: contiguous rows.  With a residual h_type is
+ * x_type or binary32; without one x_type, or any type if x is binary32.  rows * width <= APMS_DROPOUT_MAX. */
+#define APMS_DROPOUT_MAX ((int64_t)1 << 34)
+typedef struct {
+    int64_t rows, width;
+    const void* x;        int64_t x_stride;        apms_grad_type x_type;
+    const void* residual; int64_t residual_stride;
+    double      p;
+    const int64_t* rng_dev;
+    int64_t     site;                              /* in [0, 2^32): tells the calls of one step apart */
+    void*       h;        apms_grad_type h_type;
+    int64_t*    used_dev;
+} apms_dropout_args;
+apms_status apms_dropout(const apms_dropout_args* args, void* cuda_stream);
+
+/* --- gated linear recurrence, its single step and its backward pass -------------------------
+ *
+ * Per sequence and channel, with z_t = 1 / (1 + exp(gate_t)):   h_t = h_(t-1) + z_t (x_t - h_(t-1)),   h_(-1) = state (0 where it is NULL).
+ * States are held in binary32 from step to step; h (batch x steps x width, contiguous, of `type`) is rounded once.  gate = +infinity keeps a state,
+ * -infinity replaces it.  x and gate: elements of a step consecutive, steps and sequences *_step_stride and *_batch_stride >= 0 elements apart.
+ * state, last: batch x width floats; last receives the states behind the last step (with steps = 0: the first ones).
+ * starts (NULL, or apms_gated_scan_starts_bytes): what the backward pass needs of the forward pass. */
+typedef struct {
+    int64_t batch, steps, width;
+    const void* x;        int64_t x_batch_stride, x_step_stride;
+    const void* gate;     int64_t gate_batch_stride, gate_step_stride;
+    apms_grad_type type;
+    const float* state;
+    void*       h;
+    float*      last;
+    float*      starts;
+} apms_gated_scan_args;
+size_t      apms_gated_scan_starts_bytes(int64_t batch, int64_t steps, int64_t width);
+apms_status apms_gated_scan(const apms_gated_scan_args* args, void* cuda_stream);
+
+/* Gradients: with G_t = dh_t + a_(t+1) G_(t+1), a = 1 - z, and dlast (NULL: 0) in the place of a G behind the last step,
+ *   dx_t = z_t G_t,   dgate_t = G_t (h_(t-1) - x_t) a_t z_t,   dstate = a_0 G_0 (NULL: not written; dlast where steps = 0),
+ * the states being formed again from x, gate and starts.  dx, dgate: contiguous, of `type`. */
+typedef struct {
+    int64_t batch, steps, width;
+    const void* dh;       int64_t dh_batch_stride, dh_step_stride;
+    const void* x;        int64_t x_batch_stride, x_step_stride;
+    const void* gate;     int64_t gate_batch_stride, gate_step_stride;
+    apms_grad_type type;
+    const float* starts;
+    const float* dlast;
+    void*       dx;
+    void*       dgate;
+    float*      dstate;
+} apms_gated_scan_backward_args;
+apms_status apms_gated_scan_backward(const apms_gated_scan_backward_args* args, void* cuda_stream);
+
+/* One step of `batch` sequences: x and gate are batch rows, *_stride elements apart, of `type`; state and next batch x width floats (next may be
+ * state); h: batch x width, contiguous, of `type`. */
+typedef struct {
+    int64_t batch, width;
+    const void* x;        int64_t x_stride;
+    const void* gate;     int64_t gate_stride;
+    apms_grad_type type;
+    const float* state;
+    float*      next;
+    void*       h;
+} apms_gated_scan_step_args;
+apms_status apms_gated_scan_step(const apms_gated_scan_step_args* args, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

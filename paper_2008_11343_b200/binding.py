@@ -107,6 +107,14 @@ SIGNATURES = {
     "apms_rms_norm": (C.c_int, [C.c_void_p, C.c_void_p]),
     "apms_rms_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
     "apms_rms_norm_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_embedding": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_embedding_backward_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "apms_embedding_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_dropout": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_gated_scan_starts_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "apms_gated_scan": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_gated_scan_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_gated_scan_step": (C.c_int, [C.c_void_p, C.c_void_p]),
 }
 
 
@@ -128,6 +136,58 @@ class RmsNormBackwardArgs(C.Structure):
                 ("dh", C.c_void_p), ("dh_stride", C.c_int64),
                 ("dx", C.c_void_p), ("dresidual", C.c_void_p), ("dweight", C.c_void_p),
                 ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class EmbeddingArgs(C.Structure):
+    """Mirror of the C struct apms_embedding_args."""
+    _fields_ = [("count", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64),
+                ("tokens", C.c_void_p), ("token_bytes", C.c_int),
+                ("weight", C.c_void_p), ("weight_stride", C.c_int64), ("weight_type", C.c_int),
+                ("scale", C.c_float), ("out", C.c_void_p), ("out_type", C.c_int)]
+
+
+class EmbeddingBackwardArgs(C.Structure):
+    """Mirror of the C struct apms_embedding_backward_args."""
+    _fields_ = [("count", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64),
+                ("tokens", C.c_void_p), ("token_bytes", C.c_int),
+                ("dout", C.c_void_p), ("dout_stride", C.c_int64), ("dout_type", C.c_int),
+                ("scale", C.c_float), ("dweight", C.c_void_p), ("dweight_type", C.c_int),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class DropoutArgs(C.Structure):
+    """Mirror of the C struct apms_dropout_args."""
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("x_type", C.c_int),
+                ("residual", C.c_void_p), ("residual_stride", C.c_int64),
+                ("p", C.c_double), ("rng_dev", C.c_void_p), ("site", C.c_int64),
+                ("h", C.c_void_p), ("h_type", C.c_int), ("used_dev", C.c_void_p)]
+
+
+class GatedScanArgs(C.Structure):
+    """Mirror of the C struct apms_gated_scan_args."""
+    _fields_ = [("batch", C.c_int64), ("steps", C.c_int64), ("width", C.c_int64),
+                ("x", C.c_void_p), ("x_batch_stride", C.c_int64), ("x_step_stride", C.c_int64),
+                ("gate", C.c_void_p), ("gate_batch_stride", C.c_int64), ("gate_step_stride", C.c_int64),
+                ("type", C.c_int), ("state", C.c_void_p), ("h", C.c_void_p), ("last", C.c_void_p), ("starts", C.c_void_p)]
+
+
+class GatedScanBackwardArgs(C.Structure):
+    """Mirror of the C struct apms_gated_scan_backward_args."""
+    _fields_ = [("batch", C.c_int64), ("steps", C.c_int64), ("width", C.c_int64),
+                ("dh", C.c_void_p), ("dh_batch_stride", C.c_int64), ("dh_step_stride", C.c_int64),
+                ("x", C.c_void_p), ("x_batch_stride", C.c_int64), ("x_step_stride", C.c_int64),
+                ("gate", C.c_void_p), ("gate_batch_stride", C.c_int64), ("gate_step_stride", C.c_int64),
+                ("type", C.c_int), ("starts", C.c_void_p), ("dlast", C.c_void_p),
+                ("dx", C.c_void_p), ("dgate", C.c_void_p), ("dstate", C.c_void_p)]
+
+
+class GatedScanStepArgs(C.Structure):
+    """Mirror of the C struct apms_gated_scan_step_args."""
+    _fields_ = [("batch", C.c_int64), ("width", C.c_int64),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("gate", C.c_void_p), ("gate_stride", C.c_int64),
+                ("type", C.c_int), ("state", C.c_void_p), ("next", C.c_void_p), ("h", C.c_void_p)]
+
 
 _lib: Optional[C.CDLL] = None
 
@@ -515,6 +575,38 @@ def apms_rms_norm_backward_workspace_bytes(rows: int, width: int) -> int:
 
 def apms_rms_norm_backward(args: RmsNormBackwardArgs, stream: int):
     _check_thread(load().apms_rms_norm_backward(C.addressof(args), stream))
+
+
+def apms_embedding(args: EmbeddingArgs, stream: int):
+    _check_thread(load().apms_embedding(C.addressof(args), stream))
+
+
+def apms_embedding_backward_workspace_bytes(count: int, vocab: int, width: int) -> int:
+    return int(load().apms_embedding_backward_workspace_bytes(count, vocab, width))
+
+
+def apms_embedding_backward(args: EmbeddingBackwardArgs, stream: int):
+    _check_thread(load().apms_embedding_backward(C.addressof(args), stream))
+
+
+def apms_dropout(args: DropoutArgs, stream: int):
+    _check_thread(load().apms_dropout(C.addressof(args), stream))
+
+
+def apms_gated_scan_starts_bytes(batch: int, steps: int, width: int) -> int:
+    return int(load().apms_gated_scan_starts_bytes(batch, steps, width))
+
+
+def apms_gated_scan(args: GatedScanArgs, stream: int):
+    _check_thread(load().apms_gated_scan(C.addressof(args), stream))
+
+
+def apms_gated_scan_backward(args: GatedScanBackwardArgs, stream: int):
+    _check_thread(load().apms_gated_scan_backward(C.addressof(args), stream))
+
+
+def apms_gated_scan_step(args: GatedScanStepArgs, stream: int):
+    _check_thread(load().apms_gated_scan_step(C.addressof(args), stream))
 
 
 # --- convenience wrapper: handle + torch workspace + stream ---------------------------------

@@ -12,8 +12,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-# The translation units and what each includes: apms.cu the context and the kernels of the step, operators.cu the op_* files.
-UNITS = {"apms.cu": lambda f: not f.startswith("op"), "operators.cu": lambda f: f.startswith("op") or f == "errors.h"}
+# The translation units and what each includes: apms.cu the context and the kernels of the step, operators.cu the op_* files, layers.cu the layer* files.
+UNITS = {"apms.cu": lambda f: not f.startswith(("op", "layer")), "operators.cu": lambda f: f.startswith("op") or f == "errors.h",
+         "layers.cu": lambda f: f.startswith("layer") or f in ("op_common.cuh", "errors.h")}
 HDR = os.path.join(ROOT, "include", "apms.h")
 BUILD = os.path.join(HERE, "_build")                     # objects of the units
 LIB = os.path.join(HERE, "libapms.so")

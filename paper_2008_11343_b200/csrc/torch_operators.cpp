@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <memory>
@@ -34,6 +35,14 @@ decltype(&apms_clip_grads) c_clip_grads;
 decltype(&apms_rms_norm) c_rms_norm;
 decltype(&apms_rms_norm_backward_workspace_bytes) c_backward_bytes;
 decltype(&apms_rms_norm_backward) c_rms_norm_backward;
+decltype(&apms_embedding) c_embedding;
+decltype(&apms_embedding_backward_workspace_bytes) c_embedding_bytes;
+decltype(&apms_embedding_backward) c_embedding_backward;
+decltype(&apms_dropout) c_dropout;
+decltype(&apms_gated_scan_starts_bytes) c_starts_bytes;
+decltype(&apms_gated_scan) c_gated_scan;
+decltype(&apms_gated_scan_backward) c_gated_scan_backward;
+decltype(&apms_gated_scan_step) c_gated_scan_step;
 decltype(&apms_last_error) c_last_error;
 PyObject* g_error;
 
@@ -234,6 +243,281 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
+// ------------------------------------------------------------------------------------------ layers
+
+// Autograd's notice that a tensor was written: a graph that has saved it raises in its backward pass.  (Inference tensors have no version, and
+// no graph can save them.)
+void note_write(at::TensorImpl* t)
+{
+    if (!t->is_inference()) t->bump_version();
+}
+
+// None, or the element type that a torch.dtype names.
+at::ScalarType dtype_of(PyObject* o, at::ScalarType otherwise)
+{
+    if (o == Py_None) return otherwise;
+    if (!THPDtype_Check(o)) refuse("dtype must be a torch.dtype");
+    const at::ScalarType t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+    if (t != at::kFloat && t != at::kBFloat16 && t != at::kHalf) refuse("dtype is ", t, ": float32, bfloat16 or float16 is needed");
+    return t;
+}
+apms_grad_type type_of(at::ScalarType t) { return t == at::kFloat ? APMS_GRAD_F32 : t == at::kBFloat16 ? APMS_GRAD_BF16 : APMS_GRAD_F16; }
+
+// Tokens as consecutive numbers.
+at::Tensor tokens_of(PyObject* o, const at::Device& device)
+{
+    const at::Tensor& t = tensor(o, "tokens");
+    if (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt) refuse("tokens are ", t.scalar_type(), ": int64 or int32 is needed");
+    if (t.device() != device) refuse("tokens lie on ", t.device(), ", not on ", device);
+    return t.contiguous();
+}
+
+// embedding(tokens, weight, scale, dtype or None): out
+PyObject* embedding(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        if (n != 4) refuse("embedding takes 4 arguments");
+        const at::Tensor& weight = tensor(args[1], "weight");
+        const double scale = PyFloat_AsDouble(args[2]);
+        if (PyErr_Occurred()) throw Raised();
+        apms_embedding_args a = {};
+        a.width = width_of(weight, "weight");
+        if (weight.dim() != 2 || weight.size(0) == 0) refuse("weight must have the shape (vocabulary, width), not ", weight.sizes());
+        a.vocab = weight.size(0);
+        a.weight_type = (apms_grad_type)type_of(weight, "weight");
+        const at::ScalarType type = dtype_of(args[3], weight.scalar_type());
+        const c10::cuda::OptionalCUDAGuard on(weight.device());
+        const at::Tensor tokens = tokens_of(args[0], weight.device());
+        const Rows w = rows_of(weight, "weight", a.width, weight.device(), a.vocab);
+        std::vector<int64_t> shape(tokens.sizes().begin(), tokens.sizes().end());
+        shape.push_back(a.width);
+        at::Tensor out = empty(shape, type, weight.device());
+        a.count = tokens.numel(); a.tokens = tokens.const_data_ptr(); a.token_bytes = (int)tokens.element_size();
+        a.weight = w.p; a.weight_stride = w.stride; a.scale = (float)scale;
+        a.out = out.data_ptr(); a.out_type = type_of(type);
+        check(c_embedding(&a, c10::cuda::getCurrentCUDAStream(weight.get_device()).stream()));
+        return wrap(std::move(out));
+    });
+}
+
+// embedding_backward(dout, tokens, vocabulary, scale, dtype or None, out or None): dweight
+PyObject* embedding_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        if (n != 6) refuse("embedding_backward takes 6 arguments");
+        const at::Tensor& dout = tensor(args[0], "dout");
+        apms_embedding_backward_args a = {};
+        a.vocab = PyLong_AsLongLong(args[2]);
+        const double scale = PyErr_Occurred() ? 0.0 : PyFloat_AsDouble(args[3]);
+        if (PyErr_Occurred()) throw Raised();
+        a.width = width_of(dout, "dout");
+        if (a.vocab < 1) refuse("the vocabulary has at least one row, not ", a.vocab);
+        a.dout_type = (apms_grad_type)type_of(dout, "dout");
+        const c10::cuda::OptionalCUDAGuard on(dout.device());
+        const at::Tensor tokens = tokens_of(args[1], dout.device());
+        a.count = tokens.numel(); a.tokens = tokens.const_data_ptr(); a.token_bytes = (int)tokens.element_size();
+        if (dout.sizes().slice(0, dout.dim() - 1) != tokens.sizes()) refuse("dout of shape ", dout.sizes(), " does not fit tokens of shape ", tokens.sizes());
+        const Rows d = rows_of(dout, "dout", a.width, dout.device(), a.count);
+        a.dout = d.p; a.dout_stride = d.stride; a.scale = (float)scale;
+        at::Tensor out;
+        if (args[5] != Py_None) {
+            out = tensor(args[5], "out");
+            if (out.device() != dout.device() || !out.is_contiguous() || out.dim() != 2 || out.size(0) != a.vocab || out.size(1) != a.width)
+                refuse("out must be contiguous, of shape (", a.vocab, ", ", a.width, ") on ", dout.device(), ", not ", out.sizes());
+            const char *o0 = static_cast<const char*>(out.const_data_ptr()), *o1 = o0 + out.nbytes();
+            const char *t0 = static_cast<const char*>(a.tokens), *d0 = static_cast<const char*>(a.dout);
+            if (a.count && ((t0 < o1 && o0 < t0 + tokens.nbytes()) || (d0 < o1 && o0 < d0 + ((a.count - 1) * a.dout_stride + a.width) * (int64_t)dout.element_size())))
+                refuse("out shares memory with dout or tokens");
+            type_of(out, "out");
+            if (args[4] != Py_None && dtype_of(args[4], out.scalar_type()) != out.scalar_type()) refuse("out is ", out.scalar_type(), ", not of dtype");
+        } else {
+            out = empty({a.vocab, a.width}, dtype_of(args[4], dout.scalar_type()), dout.device());
+        }
+        a.dweight = out.data_ptr(); a.dweight_type = type_of(out.scalar_type());
+        a.workspace_bytes = c_embedding_bytes(a.count, a.vocab, a.width);
+        at::Tensor workspace = empty({(int64_t)a.workspace_bytes}, at::kByte, dout.device());
+        a.workspace_dev = workspace.data_ptr();
+        check(c_embedding_backward(&a, c10::cuda::getCurrentCUDAStream(dout.get_device()).stream()));
+        if (args[5] != Py_None) note_write(out.unsafeGetTensorImpl());
+        return wrap(std::move(out));
+    });
+}
+
+// dropout(x, p, rng, site, residual or None, dtype or None, keep): h, or with keep (h, the numbers used)
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        if (n != 7) refuse("dropout takes 7 arguments");
+        const at::Tensor& x = tensor(args[0], "x");
+        const at::Tensor& rng = tensor(args[2], "rng");
+        apms_dropout_args a = {};
+        a.p = PyFloat_AsDouble(args[1]);
+        a.site = PyErr_Occurred() ? 0 : PyLong_AsLongLong(args[3]);
+        const int keep = PyErr_Occurred() ? 0 : PyObject_IsTrue(args[6]);
+        if (PyErr_Occurred()) throw Raised();
+        a.width = width_of(x, "x");
+        a.rows = x.numel() / a.width;
+        a.x_type = (apms_grad_type)type_of(x, "x");
+        if (rng.scalar_type() != at::kLong || rng.numel() != 2 || !rng.is_contiguous() || rng.device() != x.device()) refuse("rng must be two contiguous int64 numbers (seed, step) on ", x.device());
+        const c10::cuda::OptionalCUDAGuard on(x.device());
+        const Rows xr = rows_of(x, "x", a.width, x.device(), a.rows);
+        a.x = xr.p; a.x_stride = xr.stride;
+        a.rng_dev = static_cast<const int64_t*>(rng.const_data_ptr());
+        at::ScalarType type = dtype_of(args[5], x.scalar_type());
+        Rows rr;
+        if (args[4] != Py_None) {
+            const at::Tensor& residual = tensor(args[4], "residual");
+            if (residual.sizes() != x.sizes() || (residual.scalar_type() != x.scalar_type() && residual.scalar_type() != at::kFloat))
+                refuse("residual must have x's shape ", x.sizes(), ", and its type or float32: ", residual.sizes(), ", ", residual.scalar_type());
+            rr = rows_of(residual, "residual", a.width, x.device(), a.rows);
+            a.residual = rr.p; a.residual_stride = rr.stride;
+            type = residual.scalar_type();
+        }
+        at::Tensor h = empty(x.sizes(), type, x.device()), used;
+        a.h = h.data_ptr(); a.h_type = type_of(type);
+        if (keep) {
+            used = empty({2}, at::kLong, x.device());
+            a.used_dev = static_cast<int64_t*>(used.data_ptr());
+        }
+        check(c_dropout(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
+        if (!keep) return wrap(std::move(h));
+        return tuple_of({wrap(std::move(h)), wrap(std::move(used))});
+    });
+}
+
+// A tensor (batch, steps, width) with consecutive channels, copied only where its last stride is not 1.
+struct Sequences {
+    at::Tensor kept;
+    const void* p;
+    int64_t batch, step;
+};
+Sequences sequences_of(const at::Tensor& t, const char* what, const at::Tensor& like)
+{
+    if (t.device() != like.device() || t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type())
+        refuse(what, " must have the shape ", like.sizes(), ", type ", like.scalar_type(), " and device ", like.device(), ": ", t.sizes(), ", ", t.scalar_type(), ", ", t.device());
+    Sequences s = {t.size(2) == 1 || t.stride(2) == 1 ? t : t.contiguous(), nullptr, 0, 0};
+    s.p = s.kept.const_data_ptr(); s.batch = s.kept.stride(0); s.step = s.kept.stride(1);
+    return s;
+}
+
+// A state (batch, width): contiguous float32.
+at::Tensor state_of(PyObject* o, const char* what, int64_t batch, int64_t width, const at::Device& device)
+{
+    const at::Tensor& t = tensor(o, what);
+    if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != batch || t.size(1) != width || t.device() != device)
+        refuse(what, " must be float32 of shape (", batch, ", ", width, ") on ", device, ": ", t.sizes(), ", ", t.scalar_type(), ", ", t.device());
+    return t.contiguous();
+}
+
+void check_sequences(const at::Tensor& x)
+{
+    if (!x.is_cuda()) refuse("x must be a CUDA tensor; there is no CPU path");
+    if (x.dim() != 3 || x.size(2) == 0) refuse("x must have the shape (batch, steps, width), not ", x.sizes());
+}
+
+// The rows of starts hold whole slabs of channels.
+std::vector<int64_t> starts_shape(const at::Tensor& x)
+{
+    const int64_t row = (int64_t)(c_starts_bytes(1, 1, x.size(2)) / sizeof(float)), bytes = (int64_t)c_starts_bytes(1, x.size(1), x.size(2));
+    return {x.size(0), row ? bytes / (int64_t)sizeof(float) / row : 0, row};
+}
+
+// gated_scan(x, gate, state or None, keep): (h, last, starts or None)
+PyObject* gated_scan(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        if (n != 4) refuse("gated_scan takes 4 arguments");
+        const at::Tensor& x = tensor(args[0], "x");
+        const int keep = PyObject_IsTrue(args[3]);
+        if (PyErr_Occurred()) throw Raised();
+        check_sequences(x);
+        apms_gated_scan_args a = {};
+        a.batch = x.size(0); a.steps = x.size(1); a.width = x.size(2);
+        a.type = (apms_grad_type)type_of(x, "x");
+        const c10::cuda::OptionalCUDAGuard on(x.device());
+        const Sequences xs = sequences_of(x, "x", x), gs = sequences_of(tensor(args[1], "gate"), "gate", x);
+        a.x = xs.p; a.x_batch_stride = xs.batch; a.x_step_stride = xs.step;
+        a.gate = gs.p; a.gate_batch_stride = gs.batch; a.gate_step_stride = gs.step;
+        at::Tensor state, starts;
+        if (args[2] != Py_None) {
+            state = state_of(args[2], "state", a.batch, a.width, x.device());
+            a.state = static_cast<const float*>(state.const_data_ptr());
+        }
+        at::Tensor h = empty(x.sizes(), x.scalar_type(), x.device()), last = empty({a.batch, a.width}, at::kFloat, x.device());
+        if (keep) {
+            starts = empty(starts_shape(x), at::kFloat, x.device());
+            a.starts = static_cast<float*>(starts.data_ptr());
+        }
+        a.h = h.data_ptr(); a.last = static_cast<float*>(last.data_ptr());
+        check(c_gated_scan(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
+        if (!keep) { Py_INCREF(Py_None); return tuple_of({wrap(std::move(h)), wrap(std::move(last)), Py_None}); }
+        return tuple_of({wrap(std::move(h)), wrap(std::move(last)), wrap(std::move(starts))});
+    });
+}
+
+// gated_scan_backward(dh, x, gate, starts, dlast or None): (dx, dgate, dstate)
+PyObject* gated_scan_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        if (n != 5) refuse("gated_scan_backward takes 5 arguments");
+        const at::Tensor& x = tensor(args[1], "x");
+        const at::Tensor& starts = tensor(args[3], "starts");
+        check_sequences(x);
+        apms_gated_scan_backward_args a = {};
+        a.batch = x.size(0); a.steps = x.size(1); a.width = x.size(2);
+        a.type = (apms_grad_type)type_of(x, "x");
+        const c10::cuda::OptionalCUDAGuard on(x.device());
+        const Sequences xs = sequences_of(x, "x", x), gs = sequences_of(tensor(args[2], "gate"), "gate", x), ds = sequences_of(tensor(args[0], "dh"), "dh", x);
+        a.x = xs.p; a.x_batch_stride = xs.batch; a.x_step_stride = xs.step;
+        a.gate = gs.p; a.gate_batch_stride = gs.batch; a.gate_step_stride = gs.step;
+        a.dh = ds.p; a.dh_batch_stride = ds.batch; a.dh_step_stride = ds.step;
+        if (starts.scalar_type() != at::kFloat || starts.device() != x.device() || !starts.is_contiguous() || starts.sizes() != at::IntArrayRef(starts_shape(x)))
+            refuse("starts must be what gated_scan_forward kept for x of shape ", x.sizes());
+        a.starts = static_cast<const float*>(starts.const_data_ptr());
+        at::Tensor dlast;
+        if (args[4] != Py_None) {
+            dlast = state_of(args[4], "dlast", a.batch, a.width, x.device());
+            a.dlast = static_cast<const float*>(dlast.const_data_ptr());
+        }
+        at::Tensor dx = empty(x.sizes(), x.scalar_type(), x.device()), dgate = empty(x.sizes(), x.scalar_type(), x.device()), dstate = empty({a.batch, a.width}, at::kFloat, x.device());
+        a.dx = dx.data_ptr(); a.dgate = dgate.data_ptr(); a.dstate = static_cast<float*>(dstate.data_ptr());
+        check(c_gated_scan_backward(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
+        return tuple_of({wrap(std::move(dx)), wrap(std::move(dgate)), wrap(std::move(dstate))});
+    });
+}
+
+// gated_scan_step(x, gate, state, out or None): h; the new states in out, or in state
+PyObject* gated_scan_step(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        if (n != 4) refuse("gated_scan_step takes 4 arguments");
+        const at::Tensor& x = tensor(args[0], "x");
+        const at::Tensor& gate = tensor(args[1], "gate");
+        const at::Tensor& state = tensor(args[2], "state");
+        const at::Tensor& next = args[3] == Py_None ? state : tensor(args[3], "out");
+        apms_gated_scan_step_args a = {};
+        a.width = width_of(x, "x");
+        if (x.dim() != 2) refuse("x must have the shape (batch, width), not ", x.sizes());
+        a.batch = x.size(0);
+        a.type = (apms_grad_type)type_of(x, "x");
+        if (gate.scalar_type() != x.scalar_type()) refuse("gate must have x's type ", x.scalar_type(), ", not ", gate.scalar_type());
+        for (const at::Tensor* t : {&state, &next})
+            if (t->scalar_type() != at::kFloat || t->sizes() != x.sizes() || !t->is_contiguous() || t->device() != x.device())
+                refuse("state and out must be contiguous float32 of shape ", x.sizes(), " on ", x.device());
+        const c10::cuda::OptionalCUDAGuard on(x.device());
+        const Rows xr = rows_of(x, "x", a.width, x.device(), a.batch), gr = rows_of(gate, "gate", a.width, x.device(), a.batch);
+        a.x = xr.p; a.x_stride = xr.stride; a.gate = gr.p; a.gate_stride = gr.stride;
+        at::Tensor h = empty(x.sizes(), x.scalar_type(), x.device());
+        a.state = static_cast<const float*>(state.const_data_ptr());
+        a.next = static_cast<float*>(next.data_ptr());
+        if (a.state != a.next && a.state < a.next + next.numel() && a.next < a.state + state.numel()) refuse("out shares part of state's memory");
+        a.h = h.data_ptr();
+        check(c_gated_scan_step(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
+        note_write(next.unsafeGetTensorImpl());
+        return wrap(std::move(h));
+    });
+}
+
 // ------------------------------------------------------------------------------------------ many tensors
 
 struct Layout {
@@ -400,13 +684,6 @@ private:
     at::Tensor scratch_;
 };
 
-// Autograd's notice that a tensor was written: a graph that has saved it raises in its backward pass.  (Inference tensors have no version, and
-// no graph can save them.)
-void note_write(at::TensorImpl* t)
-{
-    if (!t->is_inference()) t->bump_version();
-}
-
 PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject* {
@@ -471,6 +748,14 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
         c_rms_norm = (decltype(c_rms_norm))address("apms_rms_norm");
         c_backward_bytes = (decltype(c_backward_bytes))address("apms_rms_norm_backward_workspace_bytes");
         c_rms_norm_backward = (decltype(c_rms_norm_backward))address("apms_rms_norm_backward");
+        c_embedding = (decltype(c_embedding))address("apms_embedding");
+        c_embedding_bytes = (decltype(c_embedding_bytes))address("apms_embedding_backward_workspace_bytes");
+        c_embedding_backward = (decltype(c_embedding_backward))address("apms_embedding_backward");
+        c_dropout = (decltype(c_dropout))address("apms_dropout");
+        c_starts_bytes = (decltype(c_starts_bytes))address("apms_gated_scan_starts_bytes");
+        c_gated_scan = (decltype(c_gated_scan))address("apms_gated_scan");
+        c_gated_scan_backward = (decltype(c_gated_scan_backward))address("apms_gated_scan_backward");
+        c_gated_scan_step = (decltype(c_gated_scan_step))address("apms_gated_scan_step");
         c_last_error = (decltype(c_last_error))address("apms_last_error");
         Py_INCREF(args[0]);
         Py_XDECREF(g_error);
@@ -484,6 +769,12 @@ PyMethodDef methods[] = {
     {"bind", FASTCALL(bind)},
     {"rms_norm", FASTCALL(rms_norm)},
     {"rms_norm_backward", FASTCALL(rms_norm_backward)},
+    {"embedding", FASTCALL(embedding)},
+    {"embedding_backward", FASTCALL(embedding_backward)},
+    {"dropout", FASTCALL(dropout)},
+    {"gated_scan", FASTCALL(gated_scan)},
+    {"gated_scan_backward", FASTCALL(gated_scan_backward)},
+    {"gated_scan_step", FASTCALL(gated_scan_step)},
     {"row_layout", row_layout_of, METH_O, nullptr},
     {"list_create", list_create, METH_O, nullptr},
     {"grad_norm", FASTCALL(grad_norm)},

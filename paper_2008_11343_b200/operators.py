@@ -5,6 +5,10 @@ csrc/torch_operators.cpp).
                    binding.Context's step functions take
   rms_norm         root-mean-square norm at a residual junction, differentiable
   rms_norm_forward, rms_norm_fp8, rms_norm_backward    its parts; 8-bit output (e4m3) with scales
+  embedding        lookup of scaled rows, differentiable; embedding_forward, embedding_backward (into the flat gradient's place)
+  dropout          at a residual junction, its mask never stored, differentiable; dropout_forward, dropout_backward
+  gated_scan       the gated linear recurrence over sequences, differentiable; gated_scan_forward, gated_scan_backward, and
+                   gated_scan_step for one token
 
 Every call runs on torch's current stream and returns without a host synchronisation; there is no CPU path.  Arguments that do not
 fit raise ValueError, what the library refuses raises binding.ApmsError.
@@ -31,7 +35,7 @@ def _load():
             raise ImportError("_operators.so is not built; run `python -m paper_2008_11343_b200.build` (there is no fallback path)")
         from . import _operators
 
-        names = [n for n in B.SIGNATURES if n.startswith(("apms_tensors_", "apms_grad_", "apms_clip_", "apms_rms_"))] + ["apms_last_error"]
+        names = [n for n in B.SIGNATURES if n.startswith(("apms_tensors_", "apms_grad_", "apms_clip_", "apms_rms_", "apms_embedding", "apms_dropout", "apms_gated_"))] + ["apms_last_error"]
         _operators.bind(B.ApmsError, {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
         _ext = _operators
     return _ext
@@ -120,3 +124,132 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6):
     """y = rms_norm(x, weight), or (y, h) = rms_norm(x, weight, residual) with h = x + residual; differentiable in all three,
     once: a second derivative raises RuntimeError."""
     return _RmsNorm.apply(x, weight, residual, eps)
+
+
+class _FirstDerivative(torch.autograd.Function):
+    """call(*args) where a graph of the backward pass is being built (create_graph=True): its own backward pass raises."""
+
+    @staticmethod
+    def forward(ctx, name, call, *args):
+        ctx.name = name
+        return call(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"{ctx.name} has first derivatives only: its second derivatives are not implemented")
+
+
+def _derivative(name, call, *args):
+    return _FirstDerivative.apply(name, call, *args) if torch.is_grad_enabled() else call(*args)
+
+
+# ------------------------------------------------------------------------------------------ embedding
+
+def embedding_forward(tokens, weight, scale: float = 1.0, dtype: Optional[torch.dtype] = None):
+    """weight[tokens] * scale, in dtype (the weight's without one), of shape (*tokens.shape, width): formed in binary32, rounded once.  A token outside
+    [0, len(weight)) gives zeros.  tokens: int64 or int32; weight: (vocabulary, width), float32, bfloat16 or float16."""
+    return _load().embedding(tokens, weight, scale, dtype)
+
+
+def embedding_backward(dout, tokens, vocabulary: int, scale: float = 1.0, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None):
+    """The weight's gradient, (vocabulary, width): row v is scale times the sum of dout's rows at the tokens v, zeros where there are none.  Every
+    row is written, once, in dtype (dout's without one), or to `out`: contiguous, such as the weight's place in a flat gradient."""
+    return _load().embedding_backward(dout, tokens, vocabulary, scale, dtype, out)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, weight, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.rows, ctx.scale, ctx.dtype = weight.shape[0], scale, weight.dtype
+        return embedding_forward(tokens, weight, scale, dtype)
+
+    @staticmethod
+    def backward(ctx, dout):
+        return None, _derivative("embedding", embedding_backward, dout, ctx.saved_tensors[0], ctx.rows, ctx.scale, ctx.dtype), None, None
+
+
+def embedding(tokens, weight, scale: float = 1.0, dtype: Optional[torch.dtype] = None):
+    """embedding_forward, differentiable in the weight (once: a second derivative raises RuntimeError)."""
+    return _Embedding.apply(tokens, weight, scale, dtype)
+
+
+# ------------------------------------------------------------------------------------------ dropout
+
+def dropout_forward(x, p: float, rng, site: int = 0, residual=None):
+    """(h, used): h = residual + x / (1 - p) where the mask keeps x and residual (0 without one) where it does not.  rng: two int64 numbers (seed, step)
+    on x's device; the mask is a function of them, of `site` (which tells the calls of a step apart) and of the element's index alone.  They are read when
+    the kernel runs: add 1 to rng[1] once per step, in a captured graph too.  used: a copy of them, for dropout_backward.  p counts in steps of
+    2^-16, and 1 / (1 - p) is of the p so rounded.  residual: x's type or float32; h has the residual's type."""
+    return _load().dropout(x, p, rng, site, residual, None, True)
+
+
+def dropout_backward(dh, p: float, used, site: int = 0, dtype: Optional[torch.dtype] = None):
+    """The gradient of dropout_forward's x from that of h (the residual's is dh): dh / (1 - p) where the mask kept x, else 0, in dtype (dh's without one;
+    another than dh's from float32 only)."""
+    return _load().dropout(dh, p, used, site, None, dtype, False)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, rng, site, residual):
+        h, used = dropout_forward(x, p, rng, site, residual)
+        ctx.save_for_backward(used)
+        ctx.p, ctx.site, ctx.dtype, ctx.junction = p, site, x.dtype, residual is not None
+        return h
+
+    @staticmethod
+    def backward(ctx, dh):
+        dx = _derivative("dropout", dropout_backward, dh, ctx.p, ctx.saved_tensors[0], ctx.site, ctx.dtype) if ctx.needs_input_grad[0] else None
+        return dx, None, None, None, dh if ctx.junction else None
+
+
+def dropout(x, p: float, rng, site: int = 0, residual=None):
+    """dropout_forward's h, differentiable in x and residual (once: a second derivative in x raises RuntimeError)."""
+    return _Dropout.apply(x, p, rng, site, residual)
+
+
+# ------------------------------------------------------------------------------------------ gated linear recurrence
+
+def gated_scan_forward(x, gate, state=None, keep: bool = False):
+    """(h, last, starts): over the steps of x and gate, (batch, steps, width) of one type, h_t = h_(t-1) + sigmoid(-gate_t) (x_t - h_(t-1)) for every
+    channel, from `state` ((batch, width) float32; zeros without one).  States are binary32 from step to step; h has x's type, last is the state
+    behind the last step (float32).  starts: with keep what gated_scan_backward needs, else None.  A gate of +infinity keeps the state, one of -infinity
+    replaces it by x (where a packed sequence begins, say)."""
+    return _load().gated_scan(x, gate, state, keep)
+
+
+def gated_scan_backward(dh, x, gate, starts, dlast=None):
+    """(dx, dgate, dstate) from the gradients dh of h and dlast (float32; None: zero) of last."""
+    return _load().gated_scan_backward(dh, x, gate, starts, dlast)
+
+
+def gated_scan_step(x, gate, state, out=None):
+    """One token of every sequence: x and gate (batch, width); returns h and puts the new states into `out`, or into state itself."""
+    return _load().gated_scan_step(x, gate, state, out)
+
+
+class _GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, state):
+        keep = any(ctx.needs_input_grad)
+        h, last, starts = gated_scan_forward(x, gate, state, keep)
+        if keep:
+            ctx.save_for_backward(x, gate, starts)
+        ctx.set_materialize_grads(False)
+        return h, last
+
+    @staticmethod
+    def backward(ctx, dh, dlast):
+        x, gate, starts = ctx.saved_tensors
+        if dh is None and dlast is None:
+            return None, None, None
+        if dh is None:
+            dh = torch.zeros_like(x)
+        dx, dgate, dstate = _derivative("gated_scan", gated_scan_backward, dh, x, gate, starts, dlast)
+        return dx, dgate, dstate if ctx.needs_input_grad[2] else None
+
+
+def gated_scan(x, gate, state=None):
+    """(h, last) of gated_scan_forward, differentiable in all three (once: a second derivative raises RuntimeError)."""
+    return _GatedScan.apply(x, gate, state)
