@@ -692,8 +692,9 @@ apms_status apms_dropout(const apms_dropout_args* args, void* cuda_stream);
  * Per sequence and channel, with z_t = 1 / (1 + exp(gate_t)):   h_t = h_(t-1) + z_t (x_t - h_(t-1)),   h_(-1) = state (0 where it is NULL).
  * States are held in binary32 from step to step; h (batch x steps x width, contiguous, of `type`) is rounded once.  gate = +infinity keeps a state,
  * -infinity replaces it.  x and gate: elements of a step consecutive, steps and sequences *_step_stride and *_batch_stride >= 0 elements apart.
- * state, last: batch x width floats; last receives the states behind the last step (with steps = 0: the first ones).
- * starts (NULL, or apms_gated_scan_starts_bytes): what the backward pass needs of the forward pass. */
+ * steps <= 2^30, batch * width <= 2^31.  state, last: batch x width floats; last receives the states behind the last step (with steps = 0: the first ones).
+ * starts (NULL, or apms_gated_scan_starts_bytes, 16-byte aligned): what the backward pass needs of the forward pass.
+ * workspace_dev: apms_gated_scan_workspace_bytes, 16-byte aligned (0 bytes where sequences are not cut into segments), for both passes. */
 typedef struct {
     int64_t batch, steps, width;
     const void* x;        int64_t x_batch_stride, x_step_stride;
@@ -703,7 +704,9 @@ typedef struct {
     void*       h;
     float*      last;
     float*      starts;
+    void*       workspace_dev; size_t workspace_bytes;
 } apms_gated_scan_args;
+size_t      apms_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t width, apms_grad_type type);
 size_t      apms_gated_scan_starts_bytes(int64_t batch, int64_t steps, int64_t width);
 apms_status apms_gated_scan(const apms_gated_scan_args* args, void* cuda_stream);
 
@@ -721,6 +724,7 @@ typedef struct {
     void*       dx;
     void*       dgate;
     float*      dstate;
+    void*       workspace_dev; size_t workspace_bytes;
 } apms_gated_scan_backward_args;
 apms_status apms_gated_scan_backward(const apms_gated_scan_backward_args* args, void* cuda_stream);
 

@@ -111,6 +111,7 @@ SIGNATURES = {
     "apms_embedding_backward_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
     "apms_embedding_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
     "apms_dropout": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "apms_gated_scan_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64, C.c_int]),
     "apms_gated_scan_starts_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
     "apms_gated_scan": (C.c_int, [C.c_void_p, C.c_void_p]),
     "apms_gated_scan_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
@@ -169,7 +170,8 @@ class GatedScanArgs(C.Structure):
     _fields_ = [("batch", C.c_int64), ("steps", C.c_int64), ("width", C.c_int64),
                 ("x", C.c_void_p), ("x_batch_stride", C.c_int64), ("x_step_stride", C.c_int64),
                 ("gate", C.c_void_p), ("gate_batch_stride", C.c_int64), ("gate_step_stride", C.c_int64),
-                ("type", C.c_int), ("state", C.c_void_p), ("h", C.c_void_p), ("last", C.c_void_p), ("starts", C.c_void_p)]
+                ("type", C.c_int), ("state", C.c_void_p), ("h", C.c_void_p), ("last", C.c_void_p), ("starts", C.c_void_p),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 class GatedScanBackwardArgs(C.Structure):
@@ -179,7 +181,8 @@ class GatedScanBackwardArgs(C.Structure):
                 ("x", C.c_void_p), ("x_batch_stride", C.c_int64), ("x_step_stride", C.c_int64),
                 ("gate", C.c_void_p), ("gate_batch_stride", C.c_int64), ("gate_step_stride", C.c_int64),
                 ("type", C.c_int), ("starts", C.c_void_p), ("dlast", C.c_void_p),
-                ("dx", C.c_void_p), ("dgate", C.c_void_p), ("dstate", C.c_void_p)]
+                ("dx", C.c_void_p), ("dgate", C.c_void_p), ("dstate", C.c_void_p),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 class GatedScanStepArgs(C.Structure):
@@ -591,6 +594,10 @@ def apms_embedding_backward(args: EmbeddingBackwardArgs, stream: int):
 
 def apms_dropout(args: DropoutArgs, stream: int):
     _check_thread(load().apms_dropout(C.addressof(args), stream))
+
+
+def apms_gated_scan_workspace_bytes(batch: int, steps: int, width: int, type: int) -> int:
+    return int(load().apms_gated_scan_workspace_bytes(batch, steps, width, type))
 
 
 def apms_gated_scan_starts_bytes(batch: int, steps: int, width: int) -> int:

@@ -178,7 +178,7 @@ __device__ void embed_sort(const EmbedBackArgs& a, uint32_t (*counts)[kSortBins]
 
 // Zeros into the rows of [begin, end) that no token has.  Each CTA of a cluster looks at a share of the tokens; the rows' bits are joined through shared memory.
 template <int OT>
-__device__ void embed_clear(const EmbedBackArgs& a, int64_t begin, int64_t end, uint32_t* bits, bool vector)
+__device__ void embed_clear(const EmbedBackArgs& a, int64_t begin, int64_t end, uint32_t* bits, uint32_t* own, bool vector)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -192,19 +192,26 @@ __device__ void embed_clear(const EmbedBackArgs& a, int64_t begin, int64_t end, 
             if (r >= 0 && r < rows) atomicOr(bits + (r >> 5), 1u << (r & 31));
         }
         cluster_barrier();
-        for (int w = (int)rank * kSortWarps + warp; w < words; w += kSortCtas * kSortWarps) {        // 32 rows a warp
+        const int mine = (words - (int)rank + kSortCtas - 1) / kSortCtas;                             // every eighth word's rows
+        for (int k = threadIdx.x; k < mine; k += kSortThreads) {
             uint32_t taken = 0;
-            if (lane < kSortCtas) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(taken) : "r"(cluster_address(shared_address(bits + w), lane)));
-            taken = __reduce_or_sync(0xffffffffu, taken);
-            const int some = (int)min((int64_t)32, rows - (int64_t)w * 32);
-            for (int k = 0; k < some; ++k) {
-                if (taken >> k & 1) continue;
-                char* row = static_cast<char*>(a.dw) + (at + (int64_t)w * 32 + k) * a.width * kBytes<OT>;
-                if (vector) {
-                    for (int64_t c = lane * 16; c < a.width * kBytes<OT>; c += 512) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
-                } else {
-                    for (int64_t c = lane; c < a.width; c += 32) store1<OT>(row, c, 0.0f);
-                }
+            for (uint32_t r = 0; r < kSortCtas; ++r) {
+                uint32_t v;
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_address(shared_address(bits + rank + k * kSortCtas), r)));
+                taken |= v;
+            }
+            own[k] = taken;
+        }
+        __syncthreads();
+        const int64_t row_bytes = a.width * kBytes<OT>;
+        for (int i = warp; i < mine * 32; i += kSortWarps) {
+            const int64_t r = ((int64_t)rank + (i >> 5) * kSortCtas) * 32 + (i & 31);
+            if (r >= rows || (own[i >> 5] >> (i & 31) & 1)) continue;
+            char* row = static_cast<char*>(a.dw) + (at + r) * row_bytes;
+            if (vector) {
+                for (int64_t c = lane * 16; c < row_bytes; c += 512) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int64_t c = lane; c < a.width; c += 32) store1<OT>(row, c, 0.0f);
             }
         }
         cluster_barrier();
@@ -216,7 +223,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedBackArgs a, in
 {
     __shared__ union {
         struct { uint32_t counts[kSortWarps][kSortBins], total[kSortBins], base[kSortBins], warp_sums[kSortWarps]; } sort;
-        uint32_t bits[kClearRows / 32];
+        struct { uint32_t bits[kClearRows / 32], own[kClearRows / 32 / kSortCtas]; } clear;
     } s;
     allow_next_kernel();
     const int cluster = blockIdx.x / kSortCtas;
@@ -224,7 +231,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedBackArgs a, in
         embed_sort(a, s.sort.counts, s.sort.total, s.sort.base, s.sort.warp_sums);
     } else {
         const int64_t share = ((a.tokens.vocab + clearing - 1) / clearing + 31) / 32 * 32, begin = min(a.tokens.vocab, (cluster - 1) * share);
-        embed_clear<OT>(a, begin, min(a.tokens.vocab, begin + share), s.bits, vector);
+        embed_clear<OT>(a, begin, min(a.tokens.vocab, begin + share), s.clear.bits, s.clear.own, vector);
     }
 }
 

@@ -6,391 +6,629 @@ namespace {
 
 // Per channel, with z = sigmoid(-gate) and a = 1 - z = sigmoid(gate):  h_t = a_t h_(t-1) + z_t x_t, computed as h + z (x - h), which keeps a state that
 // has reached its input to the last bit however long it is held (a rounded a would forget 2^-24 of it every step).  A span of steps takes
-// h to h + (B - C h): B what the span makes of h = 0, C = 1 - the product of its a, formed as C + z (1 - C) for the same reason.
-// Backward, with G_t the gradient of h_t and k what arrives from later steps:  G = dh + k,  dx = z G,  dgate = G (h_(t-1) - x) a z,  k = a G.
+// h to h + (B + D h): B what the span makes of h = 0, D the product of its a less 1, formed as D - z D - z for the same reason.
+// Backward, with G_t the gradient of h_t and k what arrives from later steps:  G = dh + k,  dx = z G,  dgate = G (h_(t-1) - x) a z,  k = a G;  a span takes k to
+// B + A k.  The states come from `starts`, those that the forward pass had before every 8 steps, and x and gate again.
 //
-// A warp takes 128 bytes of channels (a slab: 64 16-bit or 32 binary32 ones) and a span of kSpan steps, so that a span's operands fit into
-// registers; kWarps warps lie one behind the other in time (in a short sequence fewer, and several slabs a CTA), and up to 16 CTAs of a
-// cluster behind one another too, where there are too few channels to fill the GPU: a round of the loop is kSpan * warps * CTAs steps.  Per round each warp forms its
-// span's (B, C); CTAs exchange the warps', clusters the CTAs' through one another's shared memory; then each warp runs its steps from its own first
-// state.  The rounds' operands come by asynchronous copies, `kStages` rounds ahead, each warp its own: no barrier is needed for them.  Inputs are read once and outputs
-// written once: bound by HBM.
-constexpr int kSpan = 16, kWarps = 8, kScanThreads = kWarps * 32, kStages = 2;
-constexpr int kRowBytes = 128, kSpanBytes = kSpan * kRowBytes;
-constexpr int kMostCluster = 16, kMostClusterBack = 8;
-constexpr int kStartsPad = 64;                                      // rows of starts: whole slabs of either type
+// A lane holds 8 bytes of channels (two pairs of 16-bit ones, one pair of binary32), a warp a slab of 256 bytes, over a span of 8 steps, whose operands fit into registers.
+// Eight warps lie one behind the other in time (in a short sequence fewer, and several slabs together): a round of the loop.  Per round each warp forms its span's (B, D),
+// the first one takes the state through them, and each runs its steps from its own first state.  An SM holds two such teams: two CTAs, or, where there are too few slabs
+// for that, the two halves of one CTA that take turns at a slab's rounds; one team forms its spans (bound by the exponentials and reciprocals) while the other one finishes.
+// Where there are fewer slabs than SMs, a sequence is cut into segments, whose (B, D) a kernel of its own forms first; each segment then begins with the state behind those
+// before it.  The operands come by asynchronous copies two rounds ahead, each warp its own.  Inputs are read once (before the last segment twice) and outputs written once.
+constexpr int kSpan = 8, kTeam = 8;                                 // steps; warps
+constexpr int kRowBytes = 256;
+constexpr int kStartsPad = 128;                                     // rows of starts: whole slabs of either type
+constexpr int kStages = 2;
 
+struct Rows { const void* p; int64_t batch, step; };                // bytes between sequences and steps
 struct ScanArgs {
-    int64_t batch, steps, width;
-    const void *x, *gate, *dh;
-    int64_t x_batch, x_step, gate_batch, gate_step, dh_batch, dh_step;
+    int64_t batch, width;
+    Rows x, gate, dh;
     const float *state, *dlast;
     void *h, *dx, *dgate;
     float *last, *starts, *dstate;
-    int64_t slabs, spans, starts_width;
-    int warps, rounds;                                              // warps in time; rounds of the loop
-    int pairs;                                                      // outputs can be written two 16-bit elements at a time
+    float4* segments;                                               // (B, D) of the segments' pieces: [sequence and slab][segment][piece][pair][lane]
+    int64_t slabs, starts_width;
+    int steps, spans, warps, parts, part_steps, pieces;             // warps in time of a team; segments, their steps, and what their (B, D) are formed in
+    int whole;                                                      // outputs can be written eight bytes at a time
 };
 
-// A warp's channels: one a lane in binary32, two in 16 bits; values as pairs, the second unused in binary32.
-template <int TYPE> constexpr int kLaneChannels = TYPE == APMS_GRAD_F32 ? 1 : 2;
+template <int TYPE> constexpr int kPairs = TYPE == APMS_GRAD_F32 ? 1 : 2;
+template <int TYPE> constexpr int kLaneChannels = 2 * kPairs<TYPE>;
 
 __device__ __forceinline__ float exp2_fast(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 __device__ __forceinline__ float reciprocal_fast(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float lower(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 constexpr float kLog2E = 1.44269504f;
 
-// z = 1 / (1 + exp(gate)).  For 16-bit types by the approximate exponential and reciprocal (about 2^-21 relative to z at |gate| = 10, beside their
-// 2^-9 and 2^-12); in binary32 by the library's.
+// z and, for the backward pass, -z and a z of a gate.  16-bit types take the approximate exponential and reciprocal (about 2^-19 relative to z at
+// |gate| = 16, beside their 2^-9 and 2^-12; a z below 2^-126 counts as 0), binary32 the library's.  Neither loses digits where z or a is small.
 template <int TYPE>
-__device__ __forceinline__ float taken(float gate)
+__device__ __forceinline__ float2 taken(float2 gate)
 {
-    if (TYPE == APMS_GRAD_F32) return 1.0f / (1.0f + expf(gate));
-    return reciprocal_fast(1.0f + exp2_fast(gate * kLog2E));
+    if constexpr (TYPE == APMS_GRAD_F32) {
+        return make_float2(1.0f / (1.0f + expf(gate.x)), 1.0f / (1.0f + expf(gate.y)));
+    } else {
+        const float2 e = mul2(gate, both(kLog2E)), d = add2(make_float2(exp2_fast(e.x), exp2_fast(e.y)), both(1.0f));
+        return make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
+    }
 }
-// The smaller of z and a, with the sign of the gate: both come from it without cancellation.
 template <int TYPE>
-__device__ __forceinline__ float smaller(float gate)
+__device__ __forceinline__ void minus_taken_and_slope(float2 gate, float2& nz, float2& az)
 {
-    const float m = fabsf(gate);
-    const float p = TYPE == APMS_GRAD_F32 ? expf(-m) / (1.0f + expf(-m)) : exp2_fast(-m * kLog2E) * reciprocal_fast(1.0f + exp2_fast(-m * kLog2E));
-    return copysignf(p, gate);
+    if constexpr (TYPE == APMS_GRAD_F32) {
+        const float2 z = taken<TYPE>(gate);
+        nz = make_float2(-z.x, -z.y);
+        az = mul2(taken<TYPE>(make_float2(-gate.x, -gate.y)), z);
+    } else {
+        float2 e = mul2(gate, both(kLog2E));
+        e = make_float2(exp2_fast(lower(e.x, 127.0f)), exp2_fast(lower(e.y, 127.0f)));           // finite, so that e z z is 0 where z is
+        const float2 d = fma2(e, both(-1.0f), both(-1.0f));
+        nz = make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
+        az = mul2(mul2(e, nz), nz);
+    }
 }
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, both(-1.0f), a); }  // exact product: rounded as a difference
 
 __device__ __forceinline__ void copy_async16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory"); }
 __device__ __forceinline__ void copy_async4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(to), "l"(from) : "memory"); }
 __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
 
-// `valid` rows of a slab to the warp's place in shared memory, 128 bytes apart.  UNIT: the bytes that rows are aligned to.
-template <int TYPE, int UNIT>
-__device__ __forceinline__ void fetch(uint32_t to, const void* rows, int64_t stride, int valid, int channels, int lane)
-{
-    constexpr int ES = kBytes<TYPE>;
-    const char* p = static_cast<const char*>(rows);
-    if constexpr (UNIT == 16) {
-        const int piece = lane & 7;
-#pragma unroll
-        for (int r = lane >> 3; r < kSpan; r += 4)
-            if (r < valid && piece * (16 / ES) < channels) copy_async16(to + r * kRowBytes + piece * 16, p + r * stride * ES + piece * 16);
-    } else if constexpr (UNIT == 4) {
-#pragma unroll
-        for (int r = 0; r < kSpan; ++r)
-            if (r < valid && lane * (4 / ES) < channels) copy_async4(to + r * kRowBytes + lane * 4, p + r * stride * ES + lane * 4);
-    } else {
-        const uint16_t* q = static_cast<const uint16_t*>(rows);
-#pragma unroll
-        for (int r = 0; r < kSpan; ++r) {
-            if (r >= valid || lane * 2 >= channels) break;
-            const uint32_t a = q[r * stride + lane * 2], b = lane * 2 + 1 < channels ? q[r * stride + lane * 2 + 1] : 0u;
-            asm volatile("st.shared.u32 [%0], %1;" :: "r"(to + r * kRowBytes + lane * 4), "r"(a | b << 16) : "memory");
-        }
-    }
-}
-
+__device__ __forceinline__ uint2 shared_words(uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; }
 __device__ __forceinline__ uint32_t shared_word(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
+
+// What a warp fetches of one input: a span's rows of a slab a time, to shared memory.  UNIT: the bytes that rows are aligned to.  Rows of 16-bit elements that are
+// aligned to nothing more are copied by the aligned words that hold them, and shifted where they are read (a plain load of every element, waited for: seven times as slow).
+template <int UNIT> constexpr int kPitch = kRowBytes + (UNIT == 2 ? 8 : 0);
+template <int UNIT> constexpr int kSpanBytes = kSpan * kPitch<UNIT>;
+template <int TYPE, int UNIT>
+struct Feed {
+    const char* p;                                                  // this lane's share of the next span
+    uint32_t low;                                                   // UNIT 2: address of the first row of the span that is read
+    __device__ __forceinline__ Feed(const Rows& r, int64_t sequence, int64_t column, int first, int lane)
+        : p(static_cast<const char*>(r.p) + sequence * r.batch + column * kBytes<TYPE> + first * r.step), low((uint32_t)(uintptr_t)p)
+    {
+        if (UNIT == 16) p += (lane >> 4) * r.step + (lane & 15) * 16;
+    }
+    __device__ __forceinline__ void fetch(uint32_t to, const Rows& r, int64_t round, int valid, int channels, int lane)
+    {
+        const char* q = p;
+        if constexpr (UNIT == 16) {
+            to += lane * 16;                                        // (lane >> 4) rows and (lane & 15) pieces
+            if ((lane & 15) * (16 / kBytes<TYPE>) < channels) {
+#pragma unroll
+                for (int s = 0; s < kSpan; s += 2) {
+                    if ((lane >> 4) + s < valid) copy_async16(to + s * kRowBytes, q);
+                    q += 2 * r.step;
+                }
+            }
+        } else {
+            const int bytes = channels * kBytes<TYPE> - lane * 4;   // from this lane's first word on
+#pragma unroll
+            for (int s = 0; s < kSpan; ++s) {
+                if (s >= valid) break;
+                const int shift = UNIT == 2 ? (int)((uintptr_t)q & 2) : 0;
+                const char* words = q - shift + lane * 4;
+                const uint32_t at = to + s * kPitch<UNIT> + lane * 4;
+                if (bytes + shift > 0) copy_async4(at, words);
+                if (bytes + shift > kRowBytes / 2) copy_async4(at + kRowBytes / 2, words + kRowBytes / 2);
+                if (UNIT == 2 && bytes + shift > kRowBytes) copy_async4(at + kRowBytes, words + kRowBytes);        // lane 0: the last element's word
+                q += r.step;
+            }
+        }
+        p += round;
+    }
+    // Lane `lane`'s words of row s; at: its place in the span's first row.
+    __device__ __forceinline__ uint2 words(uint32_t at, int s, const Rows& r) const
+    {
+        const uint2 w = shared_words(at + s * kPitch<UNIT>);
+        if constexpr (UNIT != 2) return w;
+        const uint32_t next = shared_word(at + s * kPitch<UNIT> + 8), shift = ((low + (uint32_t)(s * r.step)) & 2) * 8;
+        return make_uint2(__funnelshift_r(w.x, w.y, shift), __funnelshift_r(w.y, next, shift));
+    }
+    __device__ __forceinline__ void read(int64_t round) { low += (uint32_t)round; }                       // on to the next span
+    static __device__ __forceinline__ void zero(uint32_t at, int s, int lane)
+    {
+        asm volatile("st.shared.v2.u32 [%0], {%1, %1};" :: "r"(at + s * kPitch<UNIT>), "r"(0) : "memory");
+        if (UNIT == 2 && lane == 31) asm volatile("st.shared.u32 [%0], %1;" :: "r"(at + s * kPitch<UNIT> + 8), "r"(0) : "memory");
+    }
+};
+
 template <int TYPE>
-__device__ __forceinline__ float2 pair_at(uint32_t a)
+__device__ __forceinline__ float2 pair_of(uint2 w, int p)
 {
-    const uint32_t w = shared_word(a);
-    if constexpr (TYPE == APMS_GRAD_F32) return make_float2(__uint_as_float(w), 0.0f);
-    else return unpack16<TYPE>(w);
+    if constexpr (TYPE == APMS_GRAD_F32) return make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+    else return unpack16<TYPE>(p ? w.y : w.x);
 }
 
-// One arithmetic operation on a lane's channels.
-template <int TYPE> __device__ __forceinline__ float2 fma_(float2 a, float2 b, float2 c)
+// A lane's channels, rounded; WHOLE: all exist and can be written at once.
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ void store_lane(char* p, const float2* v, int mine)
 {
-    if constexpr (TYPE == APMS_GRAD_F32) return make_float2(fmaf(a.x, b.x, c.x), 0.0f);
-    else return fma2(a, b, c);
-}
-template <int TYPE> __device__ __forceinline__ float2 add_(float2 a, float2 b)
-{
-    if constexpr (TYPE == APMS_GRAD_F32) return make_float2(a.x + b.x, 0.0f);
-    else return add2(a, b);
-}
-template <int TYPE> __device__ __forceinline__ float2 sub_(float2 a, float2 b)
-{
-    if constexpr (TYPE == APMS_GRAD_F32) return make_float2(a.x - b.x, 0.0f);
-    else return fma2(b, both(-1.0f), a);
-}
-template <int TYPE> __device__ __forceinline__ float2 mul_(float2 a, float2 b)
-{
-    if constexpr (TYPE == APMS_GRAD_F32) return make_float2(a.x * b.x, 0.0f);
-    else return mul2(a, b);
-}
-__device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
-
-template <int TYPE>
-__device__ __forceinline__ void store_pair(void* p, int64_t at, float2 v, int mine, bool pairs)
-{
-    if constexpr (TYPE == APMS_GRAD_F32) {
-        static_cast<float*>(p)[at] = v.x;
-    } else if (pairs) {
-        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p) + at) = pack16<TYPE>(v);
+    if constexpr (WHOLE) {
+        *reinterpret_cast<uint2*>(p) = TYPE == APMS_GRAD_F32 ? make_uint2(__float_as_uint(v[0].x), __float_as_uint(v[0].y)) : make_uint2(pack16<TYPE>(v[0]), pack16<TYPE>(v[kPairs<TYPE> - 1]));
     } else {
-        store1<TYPE>(p, at, v.x);
-        if (mine > 1) store1<TYPE>(p, at + 1, v.y);
+#pragma unroll
+        for (int i = 0; i < kLaneChannels<TYPE>; ++i)
+            if (i < mine) store1<TYPE>(p, i, i & 1 ? v[i / 2].y : v[i / 2].x);
     }
 }
 
-// A span of steps as h -> B + (1 - C) h, for a lane's channels; in the backward pass k -> B + A k.
-struct Span { float2 b, c; };
-
-// Where a warp works: which sequence and slab, and what of a round.
+// Where a warp works: which sequence and slab, which segment.
 template <int TYPE>
 struct Place {
-    int lane, warp, in_time, rank, ctas, mine, channels;           // mine: of this lane's channels, those that exist (0: none); channels: of the slab
-    int64_t sequence, column;                                       // column: of the slab's first channel
+    int in_time, mine, channels, part;                              // mine: of this lane's channels, those that exist; channels: of the slab
+    int64_t slab, sequence, column, state_at;                       // column: of the slab's first channel; state_at: this lane's first element of a state
     bool live;
-    __device__ __forceinline__ explicit Place(const ScanArgs& a, int ctas_) : ctas(ctas_)
+    __device__ __forceinline__ Place(const ScanArgs& a, int warp)   // warp: of the team
     {
-        constexpr int WIDE = 32 * kLaneChannels<TYPE>;
-        lane = threadIdx.x & 31; warp = threadIdx.x >> 5;
+        constexpr int LC = kLaneChannels<TYPE>, WIDE = 32 * LC;
+        const int lane = threadIdx.x & 31;
         in_time = warp & (a.warps - 1);
-        rank = ctas > 1 ? (int)cluster_rank() : 0;
-        const int64_t slab = (int64_t)(blockIdx.x / ctas) * (kWarps / a.warps) + warp / a.warps;
+        part = blockIdx.y;
+        slab = (int64_t)blockIdx.x * (kTeam / a.warps) + warp / a.warps;
         live = slab < a.batch * a.slabs;
         sequence = live ? slab / a.slabs : 0;
         column = live ? (slab - sequence * a.slabs) * WIDE : 0;
         channels = live ? (int)min((int64_t)WIDE, a.width - column) : 0;
-        mine = max(0, min(kLaneChannels<TYPE>, channels - lane * kLaneChannels<TYPE>));
+        mine = max(0, min(LC, channels - lane * LC));
+        state_at = sequence * a.width + column + lane * LC;
     }
-    // The span of this warp in a round, counted from the first step or, backward, from the last.
-    __device__ __forceinline__ int64_t span(const ScanArgs& a, int round) const { return ((int64_t)round * ctas + rank) * a.warps + in_time; }
+    __device__ __forceinline__ void load_state(float2* v, const float* from) const
+    {
+#pragma unroll
+        for (int p = 0; p < kPairs<TYPE>; ++p) {
+            v[p].x = from && 2 * p < mine ? from[state_at + 2 * p] : 0.0f;
+            v[p].y = from && 2 * p + 1 < mine ? from[state_at + 2 * p + 1] : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void store_state(float* to, const float2* v) const
+    {
+#pragma unroll
+        for (int p = 0; p < kPairs<TYPE>; ++p) {
+            if (2 * p < mine) to[state_at + 2 * p] = v[p].x;
+            if (2 * p + 1 < mine) to[state_at + 2 * p + 1] = v[p].y;
+        }
+    }
+    // Where the (B, D) of this slab's piece s lies.
+    __device__ __forceinline__ float4* piece(const ScanArgs& a, int s) const { return a.segments + ((slab * a.parts * a.pieces + s) * kPairs<TYPE>) * 32 + (threadIdx.x & 31); }
 };
 
-// Joins the warps' spans of a round: `first` becomes what this warp's span begins with, `carry` (of the round's beginning) that of the next round's.
-// APPLY(span, state): the state behind a span; JOIN(earlier, later): both as one.
-template <class Apply, class Join>
-__device__ __forceinline__ void exchange(Span mine, float2& carry, float2& first, int round, int warps, int warp, int lane, int rank, int ctas,
-                                         float4 (*spans)[kWarps][32], float4* of_ctas, Apply apply, Join join)
+// One pair of channels over a span, and what it does to a state.
+struct Span { float2 b, c; };
+__device__ __forceinline__ Span span_of(const float4& v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
+struct Forward {
+    static __device__ __forceinline__ float2 apply(const Span& s, float2 h) { return add2(h, fma2(s.c, h, s.b)); }
+    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {add2(e.b, fma2(l.c, e.b, l.b)), add2(fma2(l.c, e.c, e.c), l.c)}; }
+};
+struct Backward {
+    static __device__ __forceinline__ float2 apply(const Span& s, float2 k) { return fma2(s.c, k, s.b); }
+    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {fma2(l.c, e.b, l.b), mul2(l.c, e.c)}; }
+};
+
+// Barriers of a team's warps: the spans are there (all wait), the states are there (the warps that join them only arrive); and of two teams' first warps: the carried state is.
+template <int THREADS> __device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "n"(THREADS) : "memory"); }
+template <int THREADS> __device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(THREADS) : "memory"); }
+constexpr int kFormed = 1, kJoined = 3, kCarried = 5;               // + the team
+
+// Takes the state through a round's spans.  here: [pair][warp][lane], a span's (b, c), which becomes (the state that it begins with, .), from the group's first warp on.
+template <int TYPE, class Way>
+__device__ __forceinline__ void join_spans(float2* carry, int warps, float4* here)
 {
-    float4 (*here)[32] = spans[ctas == 1 ? round & 1 : 0];        // a cluster's barrier keeps two rounds apart as well
-    here[warp][lane] = make_float4(mine.b.x, mine.b.y, mine.c.x, mine.c.y);
-    __syncthreads();
-    const int base = warp & ~(warps - 1);
-    auto at = [&](int w) { const float4 v = here[w][lane]; return Span{make_float2(v.x, v.y), make_float2(v.z, v.w)}; };
-    if (ctas == 1) {
-        float2 s = carry;
-        for (int w = 0; w < warps; ++w) {
-            if (base + w == warp) first = s;
-            s = apply(at(base + w), s);
+    constexpr int P = kPairs<TYPE>;
+    if (warps == kTeam) {
+#pragma unroll
+        for (int w0 = 0; w0 < kTeam; w0 += 4) {                     // loads first: four spans at a time
+            float4 v[4][P];
+#pragma unroll
+            for (int w = 0; w < 4 * P; ++w) v[w / P][w % P] = here[(w % P * kTeam + w0 + w / P) * 32];
+#pragma unroll
+            for (int w = 0; w < 4 * P; ++w) {
+                *reinterpret_cast<float2*>(here + (w % P * kTeam + w0 + w / P) * 32) = carry[w % P];
+                carry[w % P] = Way::apply(span_of(v[w / P][w % P]), carry[w % P]);
+            }
         }
-        carry = s;
-        return;
+    } else {
+        for (int w = 0; w < warps; ++w)
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const Span s = span_of(here[(p * kTeam + w) * 32]);
+                *reinterpret_cast<float2*>(here + (p * kTeam + w) * 32) = carry[p];
+                carry[p] = Way::apply(s, carry[p]);
+            }
     }
-    Span all = at(0), before = all;                                 // several CTAs: all their warps lie in time
-    for (int w = 1; w < kWarps; ++w) {
-        if (w == warp) before = all;
-        all = join(all, at(w));
-    }
-    float4* slots = of_ctas + (round & 1) * ctas * 32;              // two rounds apart: a CTA is past its reading when it comes to the next round's barrier
-    for (int r = warp; r < ctas; r += kWarps) {
-        const uint32_t to = cluster_address(shared_address(slots + rank * 32 + lane), (uint32_t)r);
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(to), "f"(all.b.x), "f"(all.b.y), "f"(all.c.x), "f"(all.c.y) : "memory");
-    }
-    cluster_barrier();
-    float2 s = carry;
-    for (int r = 0; r < ctas; ++r) {
-        if (r == rank) first = s;
-        const float4 v = slots[r * 32 + lane];
-        s = apply(Span{make_float2(v.x, v.y), make_float2(v.z, v.w)}, s);
-    }
-    carry = s;
-    if (warp) first = apply(before, first);
 }
 
-// Shared memory: the ring, the warps' spans (twice, or once and the CTAs' twice).  Two CTAs fit an SM, backward with clusters of up to 8.
-template <bool BACK> constexpr int kStageBytes = BACK ? 3 * kSpanBytes + 256 : 2 * kSpanBytes;
-template <bool BACK>
-constexpr size_t scan_shared(int ctas) { return (size_t)kStages * kWarps * kStageBytes<BACK> + (ctas == 1 ? 2 * kWarps : kWarps + 2 * ctas) * 32 * sizeof(float4); }
+// The state that a segment begins with: the first one through the `count` pieces before it, the first of which is `from`, the next ones `step` apart.
+template <int TYPE, class Way>
+__device__ __forceinline__ void through_pieces(float2* carry, const float4* from, int64_t step, int count)
+{
+    constexpr int P = kPairs<TYPE>;
+    for (int s0 = 0; s0 < count; s0 += 4) {
+        float4 v[4][P];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            if (s0 + s < count) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) v[s][p] = __ldcg(from + (s0 + s) * step + p * 32);
+            }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            if (s0 + s < count) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) carry[p] = Way::apply(span_of(v[s][p]), carry[p]);
+            }
+    }
+}
 
-template <int TYPE, int UNIT>
-__global__ void __launch_bounds__(kScanThreads, 2) k_scan(ScanArgs a, int ctas)
+// One round's join by the team's first warps in time: with two teams the carried state comes from and goes to the other one's.
+template <int TYPE, class Way, int TEAMS>
+__device__ __forceinline__ void join_round(float2* carry, int round, int rounds, int warps, float4* here, float2* carried)
+{
+    constexpr int P = kPairs<TYPE>;
+    const int lane = threadIdx.x & 31;
+    if (TEAMS == 2 && round) {
+        bar_sync<64>(kCarried + (round & 1));
+#pragma unroll
+        for (int p = 0; p < P; ++p) carry[p] = carried[p * 32 + lane];
+    }
+    join_spans<TYPE, Way>(carry, warps, here);
+    if (TEAMS == 2 && round + 1 < rounds) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) carried[p * 32 + lane] = carry[p];
+        bar_arrive<64>(kCarried + (~round & 1));
+    }
+}
+
+// A warp's span in, the state that it begins with out.
+template <int TYPE>
+__device__ __forceinline__ void put_span(const Span* mine, float4* at)
+{
+#pragma unroll
+    for (int p = 0; p < kPairs<TYPE>; ++p) at[p * kTeam * 32] = make_float4(mine[p].b.x, mine[p].b.y, mine[p].c.x, mine[p].c.y);
+}
+template <int TYPE>
+__device__ __forceinline__ void get_state(float2* state, const float4* at)
+{
+#pragma unroll
+    for (int p = 0; p < kPairs<TYPE>; ++p) state[p] = *reinterpret_cast<const float2*>(at + p * kTeam * 32);
+}
+
+// Shared memory: the rings, the teams' spans, the carried state.
+template <int UNIT, int TENSORS> constexpr int kStageBytes = TENSORS * kSpanBytes<UNIT>;
+template <int UNIT, int TENSORS>
+constexpr size_t scan_shared(int teams, int pairs) { return (size_t)teams * kTeam * kStages * kStageBytes<UNIT, TENSORS> + (size_t)pairs * 32 * (teams * kTeam * sizeof(float4) + sizeof(float2)); }
+
+// The (B, D) of a span from its gates and x, and a and z x of each step; VALID of its steps exist.
+template <int TYPE, int UNIT, bool WHOLE>
+__device__ __forceinline__ void form_span(Span* mine, float2 (*keep)[kPairs<TYPE>], float2 (*zx)[kPairs<TYPE>], const Feed<TYPE, UNIT>& x_feed, const Feed<TYPE, UNIT>& gate_feed, const ScanArgs& a,
+                                          uint32_t at, int valid)
+{
+    constexpr int P = kPairs<TYPE>;
+#pragma unroll
+    for (int p = 0; p < P; ++p) mine[p].b = mine[p].c = both(0.0f);
+#pragma unroll
+    for (int s = 0; s < kSpan; ++s) {
+        const uint2 g = gate_feed.words(at + kSpanBytes<UNIT>, s, a.gate), x = x_feed.words(at, s, a.x);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float2 z = taken<TYPE>(pair_of<TYPE>(g, p));
+            keep[s][p] = sub2(both(1.0f), z);
+            zx[s][p] = mul2(z, pair_of<TYPE>(x, p));
+            if (!WHOLE && s >= valid) { keep[s][p] = both(1.0f); z = zx[s][p] = both(0.0f); }            // behind the sequence the state stays
+            mine[p].b = fma2(keep[s][p], mine[p].b, zx[s][p]);
+            mine[p].c = fma2(keep[s][p], mine[p].c, z);
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) mine[p].c = make_float2(-mine[p].c.x, -mine[p].c.y);
+}
+
+template <int TYPE, int UNIT, int TEAMS>
+__global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan(ScanArgs a)
 {
     extern __shared__ float4 room[];
-    constexpr int LC = kLaneChannels<TYPE>;
-    constexpr int STAGE = kStageBytes<false>;
+    constexpr int P = kPairs<TYPE>, LC = kLaneChannels<TYPE>, STAGE = kStageBytes<UNIT, 2>;
+    const int warp = (threadIdx.x >> 5) % kTeam, team = threadIdx.x / (kTeam * 32), lane = threadIdx.x & 31;
     char* ring = reinterpret_cast<char*>(room);
-    float4 (*spans)[kWarps][32] = reinterpret_cast<float4 (*)[kWarps][32]>(ring + kStages * kWarps * STAGE);
-    float4* of_ctas = reinterpret_cast<float4*>(ring + kStages * kWarps * STAGE) + kWarps * 32;
-    const Place<TYPE> me(a, ctas);
-    const uint32_t my_ring = shared_address(ring) + me.warp * kStages * STAGE;
-    const int64_t channel = me.column + me.lane * LC;
-    const char* xs = static_cast<const char*>(a.x) + (me.sequence * a.x_batch + me.column) * kBytes<TYPE>;
-    const char* gs = static_cast<const char*>(a.gate) + (me.sequence * a.gate_batch + me.column) * kBytes<TYPE>;
-
-    auto steps_of = [&](int64_t span) { return me.live ? (int)max((int64_t)0, min((int64_t)kSpan, a.steps - span * kSpan)) : 0; };
-    auto issue = [&](int round) {
-        if (round < a.rounds) {
-            const int64_t t = me.span(a, round) * kSpan;
-            const int valid = steps_of(me.span(a, round));
-            const uint32_t to = my_ring + (round % kStages) * STAGE;
-            fetch<TYPE, UNIT>(to, xs + t * a.x_step * kBytes<TYPE>, a.x_step, valid, me.channels, me.lane);
-            fetch<TYPE, UNIT>(to + kSpanBytes, gs + t * a.gate_step * kBytes<TYPE>, a.gate_step, valid, me.channels, me.lane);
-        }
+    float4* here = reinterpret_cast<float4*>(ring + TEAMS * kTeam * kStages * STAGE);
+    float2* carried = reinterpret_cast<float2*>(here + TEAMS * P * kTeam * 32);
+    here += team * P * kTeam * 32 + warp * 32 + lane;
+    const Place<TYPE> me(a, warp);
+    const uint32_t my_ring = shared_address(ring) + (threadIdx.x >> 5) * kStages * STAGE;
+    const int begin = me.part * a.part_steps, steps = me.live ? min(a.steps, begin + a.part_steps) : 0, round_steps = a.warps * kSpan;
+    int t = begin + (team * a.warps + me.in_time) * kSpan, fetched = t;         // first step of the span that comes next, and of the one fetched next
+    Feed<TYPE, UNIT> x_feed(a.x, me.sequence, me.column, t, lane), gate_feed(a.gate, me.sequence, me.column, t, lane);
+    auto fetch = [&](uint32_t to) {
+        x_feed.fetch(to, a.x, TEAMS * round_steps * a.x.step, steps - fetched, me.channels, lane);
+        gate_feed.fetch(to + kSpanBytes<UNIT>, a.gate, TEAMS * round_steps * a.gate.step, steps - fetched, me.channels, lane);
+        fetched += TEAMS * round_steps;
         copies_issued();
     };
-    for (int r = 0; r < kStages; ++r) issue(r);
-    if (ctas > 1) cluster_barrier();                                // every CTA has begun: its shared memory may be written
-
-    float2 carry = make_float2(0.0f, 0.0f);
-    const int64_t state_at = me.sequence * a.width + channel;
-    if (a.state && me.mine > 0) {
-        carry.x = a.state[state_at];
-        if (me.mine > 1) carry.y = a.state[state_at + 1];
+#pragma unroll
+    for (int r = 0; r < kStages; ++r) fetch(my_ring + r * STAGE);
+    const int64_t row = a.width * kBytes<TYPE>;
+    char* out = static_cast<char*>(a.h) + ((me.sequence * a.steps + t) * a.width + me.column + lane * LC) * kBytes<TYPE>;
+    uint32_t stage = my_ring;
+    float2 carry[P];                                                // in the first warps in time
+    me.load_state(carry, a.state);
+    if (me.part && me.in_time == 0 && team == 0) {
+        wait_for_last_kernel();
+        through_pieces<TYPE, Forward>(carry, me.piece(a, 0), P * 32, me.part * a.pieces);
     }
-    for (int round = 0; round < a.rounds; ++round) {
-        const int64_t span = me.span(a, round);
-        const int valid = steps_of(span);
-        const uint32_t from = my_ring + (round % kStages) * STAGE + me.lane * 4;
+    const int rounds = (min(a.steps, begin + a.part_steps) - begin + round_steps - 1) / round_steps;
+    for (int round = team; round < rounds; round += TEAMS) {
+        const int valid = steps - t;                                // 8 or more: the whole span
+        const uint32_t from = stage + lane * 8;
         copies_done<kStages - 1>();
         __syncwarp();
-        float2 x[kSpan], z[kSpan];
-        Span mine = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-        for (int s = 0; s < kSpan; ++s) {
-            x[s] = pair_at<TYPE>(from + s * kRowBytes);
-            const float2 g = pair_at<TYPE>(from + kSpanBytes + s * kRowBytes);
-            z[s].x = taken<TYPE>(g.x);
-            z[s].y = LC > 1 ? taken<TYPE>(g.y) : 0.0f;
+        float2 keep[kSpan][P], zx[kSpan][P];
+        Span mine[P];
+        if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, keep, zx, x_feed, gate_feed, a, from, valid);
+        else form_span<TYPE, UNIT, false>(mine, keep, zx, x_feed, gate_feed, a, from, valid);
+        put_span<TYPE>(mine, here);
+        bar_sync<kTeam * 32>(kFormed + team);
+        if (me.in_time == 0) {
+            join_round<TYPE, Forward, TEAMS>(carry, round, rounds, a.warps, here, carried);
+            bar_arrive<kTeam * 32>(kJoined + team);
         }
-        if (valid < kSpan) {                                        // behind the sequence the state stays
+        x_feed.read(TEAMS * round_steps * a.x.step);
+        gate_feed.read(TEAMS * round_steps * a.gate.step);
+        fetch(stage);
+        stage = stage == my_ring ? my_ring + STAGE : my_ring;
+        if (me.in_time) bar_sync<kTeam * 32>(kJoined + team);
+        float2 h[P];
+        get_state<TYPE>(h, here);
+        if (valid > 0 && me.mine > 0) {
+            if (a.starts) {
+                float2* start = reinterpret_cast<float2*>(a.starts + (me.sequence * a.spans + t / kSpan) * a.starts_width + me.column + lane * LC);
+#pragma unroll
+                for (int p = 0; p < P; ++p) start[p] = h[p];
+            }
+            char* to = out;
+            auto run = [&](auto whole) {
+#pragma unroll
+                for (int s = 0; s < kSpan; ++s) {
+                    if (!whole.value && s >= valid) break;
+#pragma unroll
+                    for (int p = 0; p < P; ++p) h[p] = fma2(keep[s][p], h[p], zx[s][p]);
+                    store_lane<TYPE, whole.value>(to, h, me.mine);
+                    to += row;
+                }
+            };
+            if (valid >= kSpan && a.whole) run(std::true_type()); else run(std::false_type());
+        }
+        out += TEAMS * round_steps * row;
+        t += TEAMS * round_steps;
+    }
+    // The first warp that joined the last round has the state behind it.
+    if (me.part == a.parts - 1 && me.in_time == 0 && team == (rounds ? (rounds - 1) % TEAMS : 0)) me.store_state(a.last, carry);
+}
+
+template <int TYPE, int UNIT, int TEAMS>
+__global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(ScanArgs a)
+{
+    extern __shared__ float4 room[];
+    constexpr int P = kPairs<TYPE>, LC = kLaneChannels<TYPE>, STAGE = kStageBytes<UNIT, 3>;
+    const int warp = (threadIdx.x >> 5) % kTeam, team = threadIdx.x / (kTeam * 32), lane = threadIdx.x & 31;
+    char* ring = reinterpret_cast<char*>(room);
+    float4* here = reinterpret_cast<float4*>(ring + TEAMS * kTeam * kStages * STAGE);
+    float2* carried = reinterpret_cast<float2*>(here + TEAMS * P * kTeam * 32);
+    here += team * P * kTeam * 32 + warp * 32 + lane;
+    const Place<TYPE> me(a, warp);
+    const uint32_t my_ring = shared_address(ring) + (threadIdx.x >> 5) * kStages * STAGE;
+    const int begin = me.part * a.part_steps, end = min(a.steps, begin + a.part_steps), steps = me.live ? end : 0, round_steps = a.warps * kSpan;
+    // Rounds go backward in time, as do the spans of each: from the segment's last one.
+    int t = begin + ((end - begin + kSpan - 1) / kSpan - 1 - team * a.warps - me.in_time) * kSpan, fetched = t;      // first step of the span that comes next, and of the one fetched next
+    Feed<TYPE, UNIT> x_feed(a.x, me.sequence, me.column, t, lane), gate_feed(a.gate, me.sequence, me.column, t, lane), dh_feed(a.dh, me.sequence, me.column, t, lane);
+    auto valid_at = [&](int first) { return first < begin ? 0 : steps - first; };
+    auto fetch = [&](uint32_t to) {
+        const int valid = valid_at(fetched);
+        x_feed.fetch(to, a.x, -TEAMS * round_steps * a.x.step, valid, me.channels, lane);
+        gate_feed.fetch(to + kSpanBytes<UNIT>, a.gate, -TEAMS * round_steps * a.gate.step, valid, me.channels, lane);
+        dh_feed.fetch(to + 2 * kSpanBytes<UNIT>, a.dh, -TEAMS * round_steps * a.dh.step, valid, me.channels, lane);
+        fetched -= TEAMS * round_steps;
+        copies_issued();
+    };
+    const float* starts = a.starts + (me.sequence * a.spans + t / kSpan) * a.starts_width + me.column + lane * LC;
+    float2 start[P] = {};                                           // of the span that comes next
+    auto fetch_start = [&](int first) {
+        if (valid_at(first) > 0) {                                  // rows of starts hold whole slabs
+#pragma unroll
+            for (int p = 0; p < P; ++p) start[p] = reinterpret_cast<const float2*>(starts)[p];
+        }
+        starts -= TEAMS * a.warps * a.starts_width;
+    };
+#pragma unroll
+    for (int r = 0; r < kStages; ++r) fetch(my_ring + r * STAGE);
+    fetch_start(t);
+    const int64_t row = a.width * kBytes<TYPE>, out = ((me.sequence * a.steps + t + kSpan - 1) * a.width + me.column + lane * LC) * kBytes<TYPE>;
+    char *dx_out = static_cast<char*>(a.dx) + out, *dgate_out = static_cast<char*>(a.dgate) + out;       // of the span's last step
+    uint32_t stage = my_ring;
+    float2 carry[P];                                                // in the first warps in time
+    me.load_state(carry, a.dlast);
+    if (me.part < a.parts - 1 && me.in_time == 0 && team == 0) {
+        wait_for_last_kernel();
+        through_pieces<TYPE, Backward>(carry, me.piece(a, a.parts * a.pieces - 1), -P * 32, (a.parts - 1 - me.part) * a.pieces);
+    }
+    const int rounds = (end - begin + round_steps - 1) / round_steps;
+    for (int round = team; round < rounds; round += TEAMS) {
+        const int valid = valid_at(t);                              // 8 or more: the whole span
+        const uint32_t from = stage + lane * 8;
+        copies_done<kStages - 1>();
+        __syncwarp();
+        if (valid < kSpan) {                                        // behind the sequence nothing changes
 #pragma unroll
             for (int s = 0; s < kSpan; ++s)
-                if (s >= valid) x[s] = z[s] = make_float2(0.0f, 0.0f);
+                if (s >= valid) { x_feed.zero(from, s, lane); dh_feed.zero(from + 2 * kSpanBytes<UNIT>, s, lane); }
+            __syncwarp();
         }
+        float2 nz[kSpan][P], az[kSpan][P];
 #pragma unroll
         for (int s = 0; s < kSpan; ++s) {
-            mine.b = fma_<TYPE>(z[s], sub_<TYPE>(x[s], mine.b), mine.b);
-            mine.c = fma_<TYPE>(z[s], sub_<TYPE>(both(1.0f), mine.c), mine.c);
-        }
-        __syncwarp();                                               // all lanes have read the stage
-        issue(round + kStages);
-        float2 h;
-        exchange(mine, carry, h, round, a.warps, me.warp, me.lane, me.rank, ctas, spans, of_ctas,
-                 [](const Span& s, float2 v) { return add_<TYPE>(v, fma_<TYPE>(minus(s.c), v, s.b)); },
-                 [](const Span& e, const Span& l) {
-                     return Span{add_<TYPE>(e.b, fma_<TYPE>(minus(l.c), e.b, l.b)), fma_<TYPE>(l.c, sub_<TYPE>(both(1.0f), e.c), e.c)};
-                 });
-        if (valid && me.mine) {
-            if (a.starts) {
-                float* start = a.starts + (me.sequence * a.spans + span) * a.starts_width + channel;
-                start[0] = h.x;
-                if (LC > 1) start[1] = h.y;
-            }
-            const int64_t first = (me.sequence * a.steps + span * kSpan) * a.width + channel;
+            const uint2 g = gate_feed.words(from + kSpanBytes<UNIT>, s, a.gate);
 #pragma unroll
-            for (int s = 0; s < kSpan; ++s) {
-                if (s >= valid) break;
-                h = fma_<TYPE>(z[s], sub_<TYPE>(x[s], h), h);
-                store_pair<TYPE>(a.h, first + s * a.width, h, me.mine, a.pairs);
-            }
+            for (int p = 0; p < P; ++p) minus_taken_and_slope<TYPE>(pair_of<TYPE>(g, p), nz[s][p], az[s][p]);
         }
-    }
-    if (me.rank == 0 && me.in_time == 0 && me.mine > 0 && a.last) {
-        a.last[state_at] = carry.x;
-        if (me.mine > 1) a.last[state_at + 1] = carry.y;
-    }
-}
-
-template <int TYPE, int UNIT>
-__global__ void __launch_bounds__(kScanThreads, 2) k_scan_back(ScanArgs a, int ctas)
-{
-    extern __shared__ float4 room[];
-    constexpr int LC = kLaneChannels<TYPE>, STAGE = kStageBytes<true>;
-    char* ring = reinterpret_cast<char*>(room);
-    float4 (*spans)[kWarps][32] = reinterpret_cast<float4 (*)[kWarps][32]>(ring + kStages * kWarps * STAGE);
-    float4* of_ctas = reinterpret_cast<float4*>(ring + kStages * kWarps * STAGE) + kWarps * 32;
-    const Place<TYPE> me(a, ctas);
-    const uint32_t my_ring = shared_address(ring) + me.warp * kStages * STAGE;
-    const int64_t channel = me.column + me.lane * LC;
-    const char* xs = static_cast<const char*>(a.x) + (me.sequence * a.x_batch + me.column) * kBytes<TYPE>;
-    const char* gs = static_cast<const char*>(a.gate) + (me.sequence * a.gate_batch + me.column) * kBytes<TYPE>;
-    const char* ds = static_cast<const char*>(a.dh) + (me.sequence * a.dh_batch + me.column) * kBytes<TYPE>;
-    const float* starts = a.starts + me.sequence * a.spans * a.starts_width + channel;
-
-    // Rounds go backward in time: span counts from the last one.
-    auto span_of = [&](int round) { return a.spans - 1 - me.span(a, round); };
-    auto steps_of = [&](int64_t span) { return me.live && span >= 0 ? (int)min((int64_t)kSpan, a.steps - span * kSpan) : 0; };
-    auto issue = [&](int round) {
-        if (round < a.rounds) {
-            const int64_t span = span_of(round), t = span * kSpan;
-            const int valid = steps_of(span);
-            const uint32_t to = my_ring + (round % kStages) * STAGE;
-            fetch<TYPE, UNIT>(to, xs + t * a.x_step * kBytes<TYPE>, a.x_step, valid, me.channels, me.lane);
-            fetch<TYPE, UNIT>(to + kSpanBytes, gs + t * a.gate_step * kBytes<TYPE>, a.gate_step, valid, me.channels, me.lane);
-            fetch<TYPE, UNIT>(to + 2 * kSpanBytes, ds + t * a.dh_step * kBytes<TYPE>, a.dh_step, valid, me.channels, me.lane);
-            if (valid) {                                            // rows of starts hold whole slabs
-                const float* start = starts + span * a.starts_width;
-                copy_async4(to + 3 * kSpanBytes + me.lane * LC * 4, start);
-                if (LC > 1) copy_async4(to + 3 * kSpanBytes + me.lane * 8 + 4, start + 1);
-            }
-        }
-        copies_issued();
-    };
-    for (int r = 0; r < kStages; ++r) issue(r);
-    if (ctas > 1) cluster_barrier();                                // every CTA has begun: its shared memory may be written
-
-    float2 carry = make_float2(0.0f, 0.0f);
-    const int64_t state_at = me.sequence * a.width + channel;
-    if (a.dlast && me.mine > 0) {
-        carry.x = a.dlast[state_at];
-        if (me.mine > 1) carry.y = a.dlast[state_at + 1];
-    }
-    for (int round = 0; round < a.rounds; ++round) {
-        const int64_t span = span_of(round);
-        const int valid = steps_of(span);
-        const uint32_t stage = my_ring + (round % kStages) * STAGE, from = stage + me.lane * 4;
-        copies_done<kStages - 1>();
-        __syncwarp();
-        float2 p[kSpan];                                            // the smaller of z and a, with the gate's sign
+        if (valid < kSpan) {
 #pragma unroll
-        for (int s = 0; s < kSpan; ++s) {
-            const float2 g = pair_at<TYPE>(from + kSpanBytes + s * kRowBytes);
-            p[s].x = smaller<TYPE>(g.x);
-            p[s].y = LC > 1 ? smaller<TYPE>(g.y) : 0.0f;
+            for (int s = 0; s < kSpan; ++s)
+                if (s >= valid) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) nz[s][p] = az[s][p] = both(0.0f);
+                }
         }
-        auto z_of = [](float2 v) {
-            return make_float2(__float_as_int(v.x) < 0 ? 1.0f + v.x : v.x, LC > 1 ? (__float_as_int(v.y) < 0 ? 1.0f + v.y : v.y) : 0.0f);
-        };
-        Span mine = {make_float2(0.0f, 0.0f), both(1.0f)};
+        Span mine[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f)};
 #pragma unroll
         for (int s = kSpan - 1; s >= 0; --s) {
-            if (s >= valid) continue;
-            const float2 g = add_<TYPE>(pair_at<TYPE>(from + 2 * kSpanBytes + s * kRowBytes), mine.b), nz = minus(z_of(p[s]));
-            mine.b = fma_<TYPE>(nz, g, g);
-            mine.c = fma_<TYPE>(nz, mine.c, mine.c);
+            const uint2 w = dh_feed.words(from + 2 * kSpanBytes<UNIT>, s, a.dh);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const float2 g = add2(pair_of<TYPE>(w, p), mine[p].b);
+                mine[p].b = fma2(nz[s][p], g, g);
+                mine[p].c = fma2(nz[s][p], mine[p].c, mine[p].c);
+            }
         }
-        float2 k;
-        exchange(mine, carry, k, round, a.warps, me.warp, me.lane, me.rank, ctas, spans, of_ctas,
-                 [](const Span& s, float2 v) { return fma_<TYPE>(s.c, v, s.b); },
-                 [](const Span& e, const Span& l) { return Span{fma_<TYPE>(l.c, e.b, l.b), mul_<TYPE>(l.c, e.c)}; });
-        if (valid && me.mine) {
-            float2 h = LC > 1 ? make_float2(__uint_as_float(shared_word(stage + 3 * kSpanBytes + me.lane * 8)), __uint_as_float(shared_word(stage + 3 * kSpanBytes + me.lane * 8 + 4)))
-                              : make_float2(__uint_as_float(shared_word(stage + 3 * kSpanBytes + me.lane * 4)), 0.0f);
-            float2 d[kSpan];                                        // h_(t-1) - x_t
+        put_span<TYPE>(mine, here);
+        bar_sync<kTeam * 32>(kFormed + team);
+        if (me.in_time == 0) {
+            join_round<TYPE, Backward, TEAMS>(carry, round, rounds, a.warps, here, carried);
+            bar_arrive<kTeam * 32>(kJoined + team);
+        }
 #pragma unroll
-            for (int s = 0; s < kSpan; ++s) {
-                d[s] = sub_<TYPE>(h, pair_at<TYPE>(from + s * kRowBytes));
-                h = fma_<TYPE>(minus(z_of(p[s])), d[s], h);
-            }
-            const int64_t first = (me.sequence * a.steps + span * kSpan) * a.width + channel;
+        for (int s = 0; s < kSpan; ++s) {                           // az becomes (h_(t-1) - x_t) a z
+            const uint2 w = x_feed.words(from, s, a.x);
 #pragma unroll
-            for (int s = kSpan - 1; s >= 0; --s) {
-                if (s >= valid) continue;
-                const float2 g = add_<TYPE>(pair_at<TYPE>(from + 2 * kSpanBytes + s * kRowBytes), k), z = z_of(p[s]);
-                const float2 q = make_float2(fabsf(p[s].x), fabsf(p[s].y)), az = fma_<TYPE>(minus(q), q, q);
-                store_pair<TYPE>(a.dx, first + s * a.width, mul_<TYPE>(z, g), me.mine, a.pairs);
-                store_pair<TYPE>(a.dgate, first + s * a.width, mul_<TYPE>(mul_<TYPE>(g, d[s]), az), me.mine, a.pairs);
-                k = fma_<TYPE>(minus(z), g, g);
+            for (int p = 0; p < P; ++p) {
+                const float2 d = sub2(start[p], pair_of<TYPE>(w, p));
+                start[p] = fma2(nz[s][p], d, start[p]);
+                az[s][p] = mul2(d, az[s][p]);
             }
+        }
+        fetch_start(t - TEAMS * round_steps);
+        if (me.in_time) bar_sync<kTeam * 32>(kJoined + team);
+        float2 k[P];
+        get_state<TYPE>(k, here);
+        if (valid > 0 && me.mine > 0) {
+            char *dx = dx_out, *dgate = dgate_out;
+            auto run = [&](auto whole) {
+#pragma unroll
+                for (int s = kSpan - 1; s >= 0; --s) {
+                    const uint2 w = dh_feed.words(from + 2 * kSpanBytes<UNIT>, s, a.dh);
+                    float2 v[P], u[P];
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const float2 g = add2(pair_of<TYPE>(w, p), k[p]), nzg = mul2(nz[s][p], g);
+                        v[p] = make_float2(-nzg.x, -nzg.y);
+                        u[p] = mul2(g, az[s][p]);
+                        k[p] = add2(g, nzg);
+                    }
+                    if (whole.value || s < valid) {
+                        store_lane<TYPE, whole.value>(dx, v, me.mine);
+                        store_lane<TYPE, whole.value>(dgate, u, me.mine);
+                    }
+                    dx -= row;
+                    dgate -= row;
+                }
+            };
+            if (valid >= kSpan && a.whole) run(std::true_type()); else run(std::false_type());
         }
         __syncwarp();                                               // all lanes have read the stage
-        issue(round + kStages);
+        x_feed.read(-TEAMS * round_steps * a.x.step);
+        gate_feed.read(-TEAMS * round_steps * a.gate.step);
+        dh_feed.read(-TEAMS * round_steps * a.dh.step);
+        fetch(stage);
+        stage = stage == my_ring ? my_ring + STAGE : my_ring;
+        dx_out -= TEAMS * round_steps * row;
+        dgate_out -= TEAMS * round_steps * row;
+        t -= TEAMS * round_steps;
     }
-    if (me.rank == 0 && me.in_time == 0 && me.mine > 0 && a.dstate) {
-        a.dstate[state_at] = carry.x;
-        if (me.mine > 1) a.dstate[state_at + 1] = carry.y;
+    if (me.part == 0 && me.in_time == 0 && a.dstate && team == (rounds ? (rounds - 1) % TEAMS : 0)) me.store_state(a.dstate, carry);
+}
+
+// What the segments but the last (backward: but the first) do to a state: a CTA takes a piece of a segment, each of its warps an eighth of that, joined at the end.
+constexpr int kPartWarps = 8;
+template <int TYPE, int UNIT, bool BACK>
+__global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
+{
+    extern __shared__ float4 room[];
+    using Way = std::conditional_t<BACK, Backward, Forward>;
+    constexpr int P = kPairs<TYPE>, STAGE = kStageBytes<UNIT, 2>, STAGES = 3;
+    allow_next_kernel();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = blockIdx.y + BACK * a.pieces;
+    char* ring = reinterpret_cast<char*>(room);
+    float4* here = reinterpret_cast<float4*>(ring + kPartWarps * STAGES * STAGE) + lane;
+    const Place<TYPE> me(a, 0);
+    const uint32_t my_ring = shared_address(ring) + warp * STAGES * STAGE;
+    const int steps = a.part_steps / a.pieces, share = steps / kPartWarps, begin = piece * steps + warp * share, spans = share / kSpan;      // whole spans
+    int fetched = begin + (BACK ? share - kSpan : 0);
+    const Rows &one = BACK ? a.dh : a.x;
+    Feed<TYPE, UNIT> feed(one, me.sequence, me.column, fetched, lane), gate_feed(a.gate, me.sequence, me.column, fetched, lane);
+    int left = spans;
+    auto fetch = [&](uint32_t to) {
+        const int valid = left > 0 ? a.steps - fetched : 0;
+        feed.fetch(to, one, (BACK ? -kSpan : kSpan) * one.step, valid, me.channels, lane);
+        gate_feed.fetch(to + kSpanBytes<UNIT>, a.gate, (BACK ? -kSpan : kSpan) * a.gate.step, valid, me.channels, lane);
+        fetched += BACK ? -kSpan : kSpan;
+        --left;
+        copies_issued();
+    };
+    int t = fetched;
+#pragma unroll
+    for (int r = 0; r < STAGES; ++r) fetch(my_ring + r * STAGE);
+    uint32_t stage = my_ring;
+    Span all[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) all[p] = {both(0.0f), both(BACK ? 1.0f : 0.0f)};
+    for (int i = 0; i < spans; ++i) {
+        const int valid = a.steps - t;
+        const uint32_t from = stage + lane * 8;
+        copies_done<STAGES - 1>();
+        __syncwarp();
+        Span mine[P];
+        if constexpr (BACK) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f)};
+#pragma unroll
+            for (int s = kSpan - 1; s >= 0; --s) {
+                const uint2 w = feed.words(from, s, one), g = gate_feed.words(from + kSpanBytes<UNIT>, s, a.gate);
+                if (s >= valid) continue;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const float2 z = taken<TYPE>(pair_of<TYPE>(g, p)), nz = make_float2(-z.x, -z.y), sum = add2(pair_of<TYPE>(w, p), mine[p].b);
+                    mine[p].b = fma2(nz, sum, sum);
+                    mine[p].c = fma2(nz, mine[p].c, mine[p].c);
+                }
+            }
+        } else {
+            float2 keep[kSpan][P], zx[kSpan][P];
+            if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, keep, zx, feed, gate_feed, a, from, valid);
+            else form_span<TYPE, UNIT, false>(mine, keep, zx, feed, gate_feed, a, from, valid);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) all[p] = Way::join(all[p], mine[p]);
+        __syncwarp();                                               // all lanes have read the stage
+        feed.read((BACK ? -kSpan : kSpan) * one.step);
+        gate_feed.read((BACK ? -kSpan : kSpan) * a.gate.step);
+        fetch(stage);
+        stage = stage == my_ring + (STAGES - 1) * STAGE ? my_ring : stage + STAGE;
+        t += BACK ? -kSpan : kSpan;
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) here[(warp * P + p) * 32] = make_float4(all[p].b.x, all[p].b.y, all[p].c.x, all[p].c.y);
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            Span s = span_of(here[((BACK ? kPartWarps - 1 : 0) * P + p) * 32]);
+#pragma unroll
+            for (int w = 1; w < kPartWarps; ++w) s = Way::join(s, span_of(here[((BACK ? kPartWarps - 1 - w : w) * P + p) * 32]));
+            __stcg(me.piece(a, piece) + p * 32, make_float4(s.b.x, s.b.y, s.c.x, s.c.y));
+        }
     }
 }
 
@@ -418,7 +656,7 @@ __global__ void __launch_bounds__(128) k_scan_step(StepArgs a)
     values8<TYPE>(g, gr);
     values8<APMS_GRAD_F32>(h, hr);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = fmaf(taken<TYPE>(g[j]), x[j] - h[j], h[j]);
+    for (int j = 0; j < 8; ++j) h[j] = fmaf(taken<TYPE>(make_float2(g[j], 0.0f)).x, x[j] - h[j], h[j]);
     store8<APMS_GRAD_F32>(a.next, u * 8, h);
     store8<TYPE>(a.h, u * 8, h);
 }
@@ -429,67 +667,83 @@ __global__ void __launch_bounds__(128) k_scan_step_any(StepArgs a)
     const int64_t i = (int64_t)blockIdx.x * 128 + threadIdx.x;
     if (i >= a.batch * a.width) return;
     const int64_t row = i / a.width, col = i - row * a.width;
-    const float before = a.state[i], h = fmaf(taken<TYPE>(load1<TYPE>(a.gate, row * a.gate_stride + col)), load1<TYPE>(a.x, row * a.x_stride + col) - before, before);
+    const float before = a.state[i];
+    const float h = fmaf(taken<TYPE>(make_float2(load1<TYPE>(a.gate, row * a.gate_stride + col), 0.0f)).x, load1<TYPE>(a.x, row * a.x_stride + col) - before, before);
     a.next[i] = h;
     store1<TYPE>(a.h, i, h);
 }
 
 // ------------------------------------------------------------------------------------------ host
 
-// Warps in time: as many as the sequence has spans, up to 8.  CTAs in time: while there are fewer than two for each of about 148 SMs, and a round has
-// something for each.  Both by the sizes alone, so that results are the same on every GPU.
-int plan_scan(ScanArgs& a, int type, int most)
+// Warps in time: as many as the sequence has spans, up to a team.  Teams: two a CTA where the GPU's 148 SMs get no more than a slab each.  Segments: where they get fewer, as many as
+// fill the SMs, of 512 steps at least (below that the second kernel's launch costs more than it saves).  By the sizes alone, so that results are the same on every GPU.
+constexpr int kSms = 148, kLeastPart = 512;
+int plan_scan(ScanArgs& a, int64_t batch, int64_t steps, int64_t width, int type)
 {
-    const int64_t wide = type == APMS_GRAD_F32 ? 32 : 64;
-    a.slabs = (a.width + wide - 1) / wide;
+    const int64_t wide = type == APMS_GRAD_F32 ? 64 : 128;
+    a.batch = batch; a.steps = (int)steps; a.width = width;
+    a.slabs = (width + wide - 1) / wide;
     a.spans = (a.steps + kSpan - 1) / kSpan;
-    a.starts_width = (a.width + kStartsPad - 1) / kStartsPad * kStartsPad;
+    a.starts_width = (width + kStartsPad - 1) / kStartsPad * kStartsPad;
     a.warps = 1;
-    while (a.warps < kWarps && a.warps < a.spans) a.warps *= 2;
-    int ctas = 1;
-    while (ctas < most && a.batch * a.slabs * ctas * 2 <= 296 && (int64_t)ctas * 2 * kWarps <= a.spans) ctas *= 2;
-    a.rounds = (int)((a.spans + (int64_t)a.warps * ctas - 1) / ((int64_t)a.warps * ctas));
-    return ctas;
+    while (a.warps < kTeam && a.warps < a.spans) a.warps *= 2;
+    const int64_t sequences = std::max<int64_t>(1, batch * a.slabs), parts = std::max<int64_t>(1, std::min<int64_t>(kSms / sequences, steps / kLeastPart));
+    a.parts = a.pieces = 1;
+    a.part_steps = a.steps;
+    if (parts > 1) {                                                // pieces: two CTAs an SM, or nearly so
+        a.pieces = (int)std::min<int64_t>(4, 2 * kSms / (sequences * (parts - 1)));
+        const int64_t unit = a.pieces == 3 ? 384 : a.pieces == 4 ? 256 : 128;                              // rounds of two teams, and spans for a piece's warps
+        a.part_steps = (int)((steps + parts * unit - 1) / (parts * unit) * unit);
+        a.parts = (int)((steps + a.part_steps - 1) / a.part_steps);
+    }
+    return sequences <= kSms && a.spans > kTeam ? 2 : 1;
 }
+size_t segment_bytes(const ScanArgs& a, int type) { return a.parts > 1 ? (size_t)(a.batch * a.slabs * a.parts * a.pieces) * (type == APMS_GRAD_F32 ? 1 : 2) * 32 * sizeof(float4) : 0; }
 
-bool rows_on(const void* p, int64_t batch, int64_t batch_stride, int64_t steps, int64_t step_stride, int64_t es, int64_t unit)
+bool rows_on(const Rows& r, int64_t batch, int64_t steps, int64_t unit)
 {
-    return (uintptr_t)p % unit == 0 && (batch <= 1 || batch_stride * es % unit == 0) && (steps <= 1 || step_stride * es % unit == 0);
+    return (uintptr_t)r.p % unit == 0 && (batch <= 1 || r.batch % unit == 0) && (steps <= 1 || r.step % unit == 0);
 }
 
 template <int TYPE, int UNIT, bool BACK>
-cudaError_t launch_scan_unit(const ScanArgs& a, int ctas, cudaStream_t stream)
+cudaError_t launch_scan_unit(const ScanArgs& a, int teams, cudaStream_t stream)
 {
-    auto kernel = BACK ? k_scan_back<TYPE, UNIT> : k_scan<TYPE, UNIT>;
-    static Raised raised[kMostDevices];
-    cudaError_t e = raise_limits(raised, reinterpret_cast<const void*>(kernel), scan_shared<BACK>(BACK ? kMostClusterBack : kMostCluster), true);
+    auto one = BACK ? k_scan_back<TYPE, UNIT, 1> : k_scan<TYPE, UNIT, 1>, two = BACK ? k_scan_back<TYPE, UNIT, 2> : k_scan<TYPE, UNIT, 2>;
+    auto parts = k_scan_parts<TYPE, UNIT, BACK>;
+    constexpr int TENSORS = BACK ? 3 : 2, P = kPairs<TYPE>;
+    constexpr size_t part_shared = (size_t)kPartWarps * (3 * kStageBytes<UNIT, 2> + P * 32 * sizeof(float4));
+    static Raised raised[3][kMostDevices];
+    cudaError_t e = raise_limits(raised[0], reinterpret_cast<const void*>(one), scan_shared<UNIT, TENSORS>(1, P), false);
+    if (e == cudaSuccess) e = raise_limits(raised[1], reinterpret_cast<const void*>(two), scan_shared<UNIT, TENSORS>(2, P), false);
+    if (e == cudaSuccess) e = raise_limits(raised[2], reinterpret_cast<const void*>(parts), part_shared, false);
     if (e != cudaSuccess) return e;
-    const int64_t per_cta = kWarps / a.warps, clusters = (a.batch * a.slabs + per_cta - 1) / per_cta;
-    if (clusters * ctas > 0x7fffffff) return cudaErrorInvalidValue;
-    const dim3 grid((unsigned)(clusters * ctas));
-    if (ctas == 1) return launch(kernel, grid, kScanThreads, scan_shared<BACK>(1), stream, false, a, ctas);
-    return launch_clusters(kernel, ctas, grid, kScanThreads, scan_shared<BACK>(ctas), stream, a, ctas);
+    if (a.parts > 1) {
+        e = launch(parts, dim3((unsigned)(a.batch * a.slabs), (unsigned)((a.parts - 1) * a.pieces)), kPartWarps * 32, part_shared, stream, false, a);
+        if (e != cudaSuccess) return e;
+    }
+    const int64_t per_cta = kTeam / a.warps;
+    const dim3 grid((unsigned)((a.batch * a.slabs + per_cta - 1) / per_cta), (unsigned)a.parts);
+    return launch(teams == 2 ? two : one, grid, teams * kTeam * 32, scan_shared<UNIT, TENSORS>(teams, P), stream, a.parts > 1, a);
 }
 
 template <int TYPE, bool BACK>
-cudaError_t launch_scan(const ScanArgs& a, int ctas, cudaStream_t stream)
+cudaError_t launch_scan(const ScanArgs& a, int teams, cudaStream_t stream)
 {
     constexpr int64_t ES = kBytes<TYPE>;
     auto on = [&](int64_t unit) {
-        return a.width * ES % unit == 0 && rows_on(a.x, a.batch, a.x_batch, a.steps, a.x_step, ES, unit) && rows_on(a.gate, a.batch, a.gate_batch, a.steps, a.gate_step, ES, unit) &&
-               (!BACK || rows_on(a.dh, a.batch, a.dh_batch, a.steps, a.dh_step, ES, unit));
+        return a.width * ES % unit == 0 && rows_on(a.x, a.batch, a.steps, unit) && rows_on(a.gate, a.batch, a.steps, unit) && (!BACK || rows_on(a.dh, a.batch, a.steps, unit));
     };
-    if (on(16)) return launch_scan_unit<TYPE, 16, BACK>(a, ctas, stream);
-    if (ES == 4 || on(4)) return launch_scan_unit<TYPE, 4, BACK>(a, ctas, stream);
-    if constexpr (ES == 2) return launch_scan_unit<TYPE, 2, BACK>(a, ctas, stream);
+    if (on(16)) return launch_scan_unit<TYPE, 16, BACK>(a, teams, stream);
+    if (ES == 4 || on(4)) return launch_scan_unit<TYPE, 4, BACK>(a, teams, stream);
+    if constexpr (ES == 2) return launch_scan_unit<TYPE, 2, BACK>(a, teams, stream);
     return cudaErrorInvalidValue;
 }
 
 template <bool BACK>
-cudaError_t launch_scan_types(const ScanArgs& a, int type, int ctas, cudaStream_t stream)
+cudaError_t launch_scan_types(const ScanArgs& a, int type, int teams, cudaStream_t stream)
 {
-    return type == APMS_GRAD_F32 ? launch_scan<APMS_GRAD_F32, BACK>(a, ctas, stream)
-         : type == APMS_GRAD_BF16 ? launch_scan<APMS_GRAD_BF16, BACK>(a, ctas, stream) : launch_scan<APMS_GRAD_F16, BACK>(a, ctas, stream);
+    return type == APMS_GRAD_F32 ? launch_scan<APMS_GRAD_F32, BACK>(a, teams, stream)
+         : type == APMS_GRAD_BF16 ? launch_scan<APMS_GRAD_BF16, BACK>(a, teams, stream) : launch_scan<APMS_GRAD_F16, BACK>(a, teams, stream);
 }
 
 template <int TYPE>
@@ -499,17 +753,17 @@ cudaError_t launch_step(const StepArgs& a, bool vector, cudaStream_t stream)
     return launch(vector ? k_scan_step<TYPE> : k_scan_step_any<TYPE>, dim3((unsigned)((n + 127) / 128)), 128, 0, stream, false, a);
 }
 
-constexpr int64_t kMostScan = (int64_t)1 << 31, kMostScanElements = (int64_t)1 << 40;
+constexpr int64_t kMostScan = (int64_t)1 << 31, kMostSteps = (int64_t)1 << 30, kMostScanElements = (int64_t)1 << 40;
 
 bool scan_sizes(int64_t batch, int64_t steps, int64_t width)
 {
-    return batch >= 0 && steps >= 0 && width >= 1 && batch < kMostScan && steps < kMostScan && width < kMostScan && batch * width <= kMostScan && batch * width * steps <= kMostScanElements;
+    return batch >= 0 && steps >= 0 && width >= 1 && batch < kMostScan && steps <= kMostSteps && width < kMostScan && batch * width <= kMostScan && batch * width * steps <= kMostScanElements;
 }
 
 apms_status scan_check(const char* who, int64_t batch, int64_t steps, int64_t width, apms_grad_type type)
 {
     if (!scan_sizes(batch, steps, width))
-        return operator_fail(APMS_ERR_INVALID_ARG, "%s: %lld sequences of %lld steps of %lld channels: needs none below 0, width >= 1, batch * width <= 2^31 and at most 2^40 elements", who,
+        return operator_fail(APMS_ERR_INVALID_ARG, "%s: %lld sequences of %lld steps of %lld channels: needs none below 0, width >= 1, steps <= 2^30, batch * width <= 2^31 and at most 2^40 elements", who,
                              (long long)batch, (long long)steps, (long long)width);
     if (!known_type(type)) return operator_fail(APMS_ERR_INVALID_ARG, "%s: unknown element type", who);
     return APMS_OK;
@@ -518,6 +772,14 @@ apms_status scan_check(const char* who, int64_t batch, int64_t steps, int64_t wi
 }  // namespace
 
 extern "C" {
+
+size_t apms_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t width, apms_grad_type type)
+{
+    if (!scan_sizes(batch, steps, width) || !known_type(type)) return 0;
+    ScanArgs a = {};
+    plan_scan(a, batch, steps, width, type);
+    return segment_bytes(a, type);
+}
 
 size_t apms_gated_scan_starts_bytes(int64_t batch, int64_t steps, int64_t width)
 {
@@ -535,16 +797,20 @@ apms_status apms_gated_scan(const apms_gated_scan_args* args, void* cuda_stream)
     if (g.batch == 0) return APMS_OK;
     if (!g.last || (g.steps && (!g.x || !g.gate || !g.h))) return operator_fail(APMS_ERR_INVALID_ARG, "%s: x, gate, h or last is NULL", who);
     if (g.x_batch_stride < 0 || g.x_step_stride < 0 || g.gate_batch_stride < 0 || g.gate_step_stride < 0) return operator_fail(APMS_ERR_INVALID_ARG, "%s: a stride is below 0", who);
-    if (!on_element(g.x, g.type) || !on_element(g.gate, g.type) || !on_element(g.h, g.type) || !on_element(g.state, APMS_GRAD_F32) || !on_element(g.last, APMS_GRAD_F32) || !on_element(g.starts, APMS_GRAD_F32))
+    if (!on_element(g.x, g.type) || !on_element(g.gate, g.type) || !on_element(g.h, g.type) || !on_element(g.state, APMS_GRAD_F32) || !on_element(g.last, APMS_GRAD_F32) || !on_16(g.starts))
         return operator_fail(APMS_ERR_INVALID_ARG, "%s: an address is not aligned to its element size", who);
     ScanArgs a = {};
-    a.batch = g.batch; a.steps = g.steps; a.width = g.width;
-    a.x = g.x; a.x_batch = g.x_batch_stride; a.x_step = g.x_step_stride;
-    a.gate = g.gate; a.gate_batch = g.gate_batch_stride; a.gate_step = g.gate_step_stride;
+    const int64_t es = (int64_t)element_size(g.type);
+    const int teams = plan_scan(a, g.batch, g.steps, g.width, g.type);
+    if (a.parts > 1 && (!g.workspace_dev || !on_16(g.workspace_dev) || g.workspace_bytes < segment_bytes(a, g.type)))
+        return operator_fail(APMS_ERR_OOM, "%s: needs apms_gated_scan_workspace_bytes() of 16-byte aligned workspace", who);
+    a.segments = static_cast<float4*>(g.workspace_dev);
+    a.x = {g.x, g.x_batch_stride * es, g.x_step_stride * es};
+    a.gate = {g.gate, g.gate_batch_stride * es, g.gate_step_stride * es};
     a.state = g.state; a.h = g.h; a.last = g.last; a.starts = g.starts;
-    const int ctas = plan_scan(a, g.type, kMostCluster);
-    a.pairs = a.width % 2 == 0 && (uintptr_t)a.h % 4 == 0;
-    OPERATOR_CUDA("apms_gated_scan", launch_scan_types<false>(a, g.type, ctas, (cudaStream_t)cuda_stream));
+    a.whole = a.width * es % 8 == 0 && (uintptr_t)a.h % 8 == 0;
+    const cudaError_t e = launch_scan_types<false>(a, g.type, teams, (cudaStream_t)cuda_stream);
+    OPERATOR_CUDA("apms_gated_scan", e);
     return APMS_OK;
 }
 
@@ -560,17 +826,21 @@ apms_status apms_gated_scan_backward(const apms_gated_scan_backward_args* args, 
     if (g.x_batch_stride < 0 || g.x_step_stride < 0 || g.gate_batch_stride < 0 || g.gate_step_stride < 0 || g.dh_batch_stride < 0 || g.dh_step_stride < 0)
         return operator_fail(APMS_ERR_INVALID_ARG, "%s: a stride is below 0", who);
     if (!on_element(g.x, g.type) || !on_element(g.gate, g.type) || !on_element(g.dh, g.type) || !on_element(g.dx, g.type) || !on_element(g.dgate, g.type) ||
-        !on_element(g.starts, APMS_GRAD_F32) || !on_element(g.dlast, APMS_GRAD_F32) || !on_element(g.dstate, APMS_GRAD_F32))
+        !on_16(g.starts) || !on_element(g.dlast, APMS_GRAD_F32) || !on_element(g.dstate, APMS_GRAD_F32))
         return operator_fail(APMS_ERR_INVALID_ARG, "%s: an address is not aligned to its element size", who);
     ScanArgs a = {};
-    a.batch = g.batch; a.steps = g.steps; a.width = g.width;
-    a.x = g.x; a.x_batch = g.x_batch_stride; a.x_step = g.x_step_stride;
-    a.gate = g.gate; a.gate_batch = g.gate_batch_stride; a.gate_step = g.gate_step_stride;
-    a.dh = g.dh; a.dh_batch = g.dh_batch_stride; a.dh_step = g.dh_step_stride;
+    const int64_t es = (int64_t)element_size(g.type);
+    const int teams = plan_scan(a, g.batch, g.steps, g.width, g.type);
+    if (a.parts > 1 && (!g.workspace_dev || !on_16(g.workspace_dev) || g.workspace_bytes < segment_bytes(a, g.type)))
+        return operator_fail(APMS_ERR_OOM, "%s: needs apms_gated_scan_workspace_bytes() of 16-byte aligned workspace", who);
+    a.segments = static_cast<float4*>(g.workspace_dev);
+    a.x = {g.x, g.x_batch_stride * es, g.x_step_stride * es};
+    a.gate = {g.gate, g.gate_batch_stride * es, g.gate_step_stride * es};
+    a.dh = {g.dh, g.dh_batch_stride * es, g.dh_step_stride * es};
     a.starts = const_cast<float*>(g.starts); a.dlast = g.dlast; a.dx = g.dx; a.dgate = g.dgate; a.dstate = g.dstate;
-    const int ctas = plan_scan(a, g.type, kMostClusterBack);
-    a.pairs = a.width % 2 == 0 && (uintptr_t)a.dx % 4 == 0 && (uintptr_t)a.dgate % 4 == 0;
-    OPERATOR_CUDA("apms_gated_scan_backward", launch_scan_types<true>(a, g.type, ctas, (cudaStream_t)cuda_stream));
+    a.whole = a.width * es % 8 == 0 && (uintptr_t)a.dx % 8 == 0 && (uintptr_t)a.dgate % 8 == 0;
+    const cudaError_t e = launch_scan_types<true>(a, g.type, teams, (cudaStream_t)cuda_stream);
+    OPERATOR_CUDA("apms_gated_scan_backward", e);
     return APMS_OK;
 }
 

@@ -39,6 +39,7 @@ decltype(&apms_embedding) c_embedding;
 decltype(&apms_embedding_backward_workspace_bytes) c_embedding_bytes;
 decltype(&apms_embedding_backward) c_embedding_backward;
 decltype(&apms_dropout) c_dropout;
+decltype(&apms_gated_scan_workspace_bytes) c_scan_bytes;
 decltype(&apms_gated_scan_starts_bytes) c_starts_bytes;
 decltype(&apms_gated_scan) c_gated_scan;
 decltype(&apms_gated_scan_backward) c_gated_scan_backward;
@@ -422,6 +423,17 @@ std::vector<int64_t> starts_shape(const at::Tensor& x)
     return {x.size(0), row ? bytes / (int64_t)sizeof(float) / row : 0, row};
 }
 
+// The call's workspace, where it needs one.
+template <class Args>
+at::Tensor workspace_of(Args& a, const at::Device& device)
+{
+    a.workspace_bytes = c_scan_bytes(a.batch, a.steps, a.width, a.type);
+    if (!a.workspace_bytes) return at::Tensor();
+    at::Tensor w = empty({(int64_t)a.workspace_bytes}, at::kByte, device);
+    a.workspace_dev = w.data_ptr();
+    return w;
+}
+
 // gated_scan(x, gate, state or None, keep): (h, last, starts or None)
 PyObject* gated_scan(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -449,6 +461,7 @@ PyObject* gated_scan(PyObject*, PyObject* const* args, Py_ssize_t n)
             a.starts = static_cast<float*>(starts.data_ptr());
         }
         a.h = h.data_ptr(); a.last = static_cast<float*>(last.data_ptr());
+        const at::Tensor workspace = workspace_of(a, x.device());
         check(c_gated_scan(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
         if (!keep) { Py_INCREF(Py_None); return tuple_of({wrap(std::move(h)), wrap(std::move(last)), Py_None}); }
         return tuple_of({wrap(std::move(h)), wrap(std::move(last)), wrap(std::move(starts))});
@@ -481,6 +494,7 @@ PyObject* gated_scan_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
         }
         at::Tensor dx = empty(x.sizes(), x.scalar_type(), x.device()), dgate = empty(x.sizes(), x.scalar_type(), x.device()), dstate = empty({a.batch, a.width}, at::kFloat, x.device());
         a.dx = dx.data_ptr(); a.dgate = dgate.data_ptr(); a.dstate = static_cast<float*>(dstate.data_ptr());
+        const at::Tensor workspace = workspace_of(a, x.device());
         check(c_gated_scan_backward(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
         return tuple_of({wrap(std::move(dx)), wrap(std::move(dgate)), wrap(std::move(dstate))});
     });
@@ -752,6 +766,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
         c_embedding_bytes = (decltype(c_embedding_bytes))address("apms_embedding_backward_workspace_bytes");
         c_embedding_backward = (decltype(c_embedding_backward))address("apms_embedding_backward");
         c_dropout = (decltype(c_dropout))address("apms_dropout");
+        c_scan_bytes = (decltype(c_scan_bytes))address("apms_gated_scan_workspace_bytes");
         c_starts_bytes = (decltype(c_starts_bytes))address("apms_gated_scan_starts_bytes");
         c_gated_scan = (decltype(c_gated_scan))address("apms_gated_scan");
         c_gated_scan_backward = (decltype(c_gated_scan_backward))address("apms_gated_scan_backward");

@@ -248,10 +248,12 @@ def test_gates_without_bound_keep_and_replace():
     state = normal((2, 70), seed=54)
     check_scan(x, gate, state, dh, normal((2, 70), seed=55))
     h, last, _ = O.gated_scan_forward(x, gate, state)
-    # Kept to the last bit within spans of 16 steps and over spans that do nothing.  What step 111 leaves reaches step 112 as h + (B - C h) over the span before it,
-    # not step by step: both are the state within its error.
-    assert torch.equal(h[:, 99:100].expand(2, 13, 70), h[:, 99:112]) and torch.equal(h[:, 112:113].expand(2, 28, 70), h[:, 112:140])
-    assert ((h[:, 111] - h[:, 112]).abs() <= 2 * oracle.scan(x, gate, state)[1][:, 111] + h[:, 111].abs() * 2 * oracle.U32).all()
+    # Step by step nothing changes; where a group of steps that are formed together ends, the state behind it is h + (B - C h), not what the last of its steps left: both are
+    # the state within its error.  Where nothing but +infinity stands, B = C = 0, and the state stays to the last bit.
+    assert ((h[:, 99:100] - h[:, 100:140]).abs() <= 2 * oracle.scan(x, gate, state)[1][:, 99:100] + h[:, 99:100].abs() * 2 * oracle.U32).all()
+    for steps in (3, 200, 5000):
+        held, last, _ = O.gated_scan_forward(normal((2, steps, 70), seed=56), torch.full((2, steps, 70), float("inf"), device="cuda"), state)
+        assert torch.equal(last, state) and torch.equal(held, state[:, None].expand(2, steps, 70))
     flat = torch.full((1, 3000, 8), 40.0, device="cuda")
     held, _, _ = O.gated_scan_forward(normal((1, 3000, 8), seed=56), flat, state[:1, :8])
     assert (held - state[:1, None, :8]).abs().max() < 1e-12                         # z = 4e-18

@@ -91,7 +91,7 @@ SIZES = [({"batch": -1}, "below 0"), ({"steps": -1}, "below 0"), ({"width": 0}, 
          ({"type": 5}, "type"), ({"x": None}, "NULL"), ({"gate": None}, "NULL"), ({"x_step_stride": -1}, "stride"), ({"gate_batch_stride": -1}, "stride"), ({"x": 257}, "aligned")]
 
 
-@pytest.mark.parametrize("changes,words", SIZES + [({"h": None}, "NULL"), ({"last": None}, "NULL"), ({"state": 130}, "aligned"), ({"last": 2050}, "aligned"), ({"starts": 2}, "aligned"), ({"h": 1025}, "aligned")])
+@pytest.mark.parametrize("changes,words", SIZES + [({"h": None}, "NULL"), ({"last": None}, "NULL"), ({"state": 130}, "aligned"), ({"last": 2050}, "aligned"), ({"starts": 8}, "aligned"), ({"h": 1025}, "aligned")])
 def test_the_scan_refuses(changes, words):
     refused(lambda: B.apms_gated_scan(scan(**changes), None), words)
 
@@ -107,6 +107,15 @@ def test_the_scan_backward_refuses(changes, words):
 def test_the_step_refuses(changes, words):
     a = B.GatedScanStepArgs(batch=2, width=8, x=256, x_stride=8, gate=512, gate_stride=8, type=B.GRAD_BF16, state=1024, next=1024, h=2048)
     refused(lambda: B.apms_gated_scan_step(changed(a, changes), None), words)
+
+
+def test_long_sequences_of_few_channels_need_a_workspace():
+    need = B.apms_gated_scan_workspace_bytes(1, 5000, 64, B.GRAD_BF16)
+    assert need > 0 == B.apms_gated_scan_workspace_bytes(1, 5000, 64, 7) == B.apms_gated_scan_workspace_bytes(1, 100, 64, B.GRAD_BF16) == B.apms_gated_scan_workspace_bytes(-1, 5000, 64, 0)
+    long = dict(batch=1, steps=5000, width=64, x_step_stride=64, gate_step_stride=64)
+    for bad in ({}, {"workspace_dev": 4096 + 8, "workspace_bytes": need}, {"workspace_dev": 4096, "workspace_bytes": need - 1}):
+        refused(lambda: B.apms_gated_scan(scan(**long, **bad), None), "workspace", B.ERR_OOM)
+        refused(lambda: B.apms_gated_scan_backward(scan_back(**long, dh_step_stride=64, **bad), None), "workspace", B.ERR_OOM)
 
 
 def test_without_arguments_or_work():
