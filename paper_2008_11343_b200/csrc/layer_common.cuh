@@ -15,27 +15,25 @@ __device__ __forceinline__ float load1(const void* p, int64_t i) { return (float
 template <int TYPE>
 __device__ __forceinline__ void store1(void* p, int64_t i, float v) { store_element(p, i, TYPE, v); }
 
-// Elements i to i + 7 as they lie in memory: one 16-byte access for 16-bit types, two for binary32; p + i is 16-byte aligned.
-template <int TYPE> struct Eight { uint4 w[kBytes<TYPE> / 2]; };
+// Elements i to i + 7 as they lie in memory, in one access: of 16 bytes for 16-bit types, of 32 for binary32 (two of 16 would write half sectors); p + i lies on such a boundary.
+template <int TYPE> struct Eight { uint32_t w[2 * kBytes<TYPE>]; };
 template <int TYPE>
 __device__ __forceinline__ Eight<TYPE> load8(const void* p, int64_t i)
 {
-    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * kBytes<TYPE>);
+    const char* q = static_cast<const char*>(p) + i * kBytes<TYPE>;
     Eight<TYPE> e;
-#pragma unroll
-    for (int k = 0; k < kBytes<TYPE> / 2; ++k) e.w[k] = q[k];
+    if constexpr (TYPE == APMS_GRAD_F32) load32(e.w, q); else load16(e.w, q);
     return e;
 }
 template <int TYPE>
 __device__ __forceinline__ void values8(float* v, const Eight<TYPE>& e)
 {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(e.w);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         if constexpr (TYPE == APMS_GRAD_F32) {
-            v[2 * k] = __uint_as_float(w[2 * k]); v[2 * k + 1] = __uint_as_float(w[2 * k + 1]);
+            v[2 * k] = __uint_as_float(e.w[2 * k]); v[2 * k + 1] = __uint_as_float(e.w[2 * k + 1]);
         } else {
-            const float2 a = unpack16<TYPE>(w[k]);
+            const float2 a = unpack16<TYPE>(e.w[k]);
             v[2 * k] = a.x; v[2 * k + 1] = a.y;
         }
     }
@@ -43,12 +41,14 @@ __device__ __forceinline__ void values8(float* v, const Eight<TYPE>& e)
 template <int TYPE>
 __device__ __forceinline__ void store8(void* p, int64_t i, const float* v)
 {
-    uint4* q = reinterpret_cast<uint4*>(static_cast<char*>(p) + i * kBytes<TYPE>);
+    char* q = static_cast<char*>(p) + i * kBytes<TYPE>;
     if constexpr (TYPE == APMS_GRAD_F32) {
-        q[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        q[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[k]);
+        store32(q, w);
     } else {
-        q[0] = make_uint4(pack16<TYPE>(v[0], v[1]), pack16<TYPE>(v[2], v[3]), pack16<TYPE>(v[4], v[5]), pack16<TYPE>(v[6], v[7]));
+        *reinterpret_cast<uint4*>(q) = make_uint4(pack16<TYPE>(v[0], v[1]), pack16<TYPE>(v[2], v[3]), pack16<TYPE>(v[4], v[5]), pack16<TYPE>(v[6], v[7]));
     }
 }
 
@@ -57,6 +57,9 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Its two halves, the first without a release (which waits for the thread's stores to global memory, about a microsecond): for threads whose data no other CTA reads.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 // The address in CTA `rank` of what this CTA has at shared-memory address `a`.
 __device__ __forceinline__ uint32_t cluster_address(uint32_t a, uint32_t rank)
@@ -102,10 +105,11 @@ cudaError_t raise_limits(Raised* known, const void* kernel, size_t shared, bool 
 
 inline bool on_element(const void* p, int type) { return (uintptr_t)p % element_size(type) == 0; }
 inline bool on_16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-// Rows `stride` elements apart that begin on 16-byte boundaries and hold whole groups of eight elements.
+// What load8 and store8 need of an address, and of rows `stride` elements apart.
+inline bool on_eight(const void* p, int type) { return (uintptr_t)p % (8 * element_size(type)) == 0; }
 inline bool rows_of_eight(const void* p, int64_t rows, int64_t stride, int64_t width, int type)
 {
-    return !p || (on_16(p) && width % 8 == 0 && (rows <= 1 || stride * (int64_t)element_size(type) % 16 == 0));
+    return !p || (on_eight(p, type) && width % 8 == 0 && (rows <= 1 || stride % 8 == 0));
 }
 
 }  // namespace

@@ -169,7 +169,7 @@ extern "C" apms_status apms_dropout(const apms_dropout_args* args, void* cuda_st
     a.border = (uint32_t)floor(g.p * 65536.0 + 0.5);
     a.scale = a.border < 65536u ? (float)(65536.0 / (65536.0 - a.border)) : 0.0f;
     if (a.rows > 1 && a.x_stride == a.width && (!a.r || a.r_stride == a.width)) { a.width = a.numel; a.rows = 1; }
-    const bool vector = on_16(a.h) && (a.rows == 1 ? on_16(a.x) && on_16(a.r) : rows_of_eight(a.x, a.rows, a.x_stride, a.width, g.x_type) && rows_of_eight(a.r, a.rows, a.r_stride, a.width, g.h_type));
+    const bool vector = on_eight(a.h, g.h_type) && (a.rows == 1 ? on_eight(a.x, g.x_type) && on_eight(a.r, g.h_type) : rows_of_eight(a.x, a.rows, a.x_stride, a.width, g.x_type) && rows_of_eight(a.r, a.rows, a.r_stride, a.width, g.h_type));
     const cudaError_t e = g.x_type == APMS_GRAD_F32 ? launch_dropout_types<APMS_GRAD_F32>(a, g.h_type, vector, stream)
                         : g.x_type == APMS_GRAD_BF16 ? launch_dropout_types<APMS_GRAD_BF16>(a, g.h_type, vector, stream) : launch_dropout_types<APMS_GRAD_F16>(a, g.h_type, vector, stream);
     OPERATOR_CUDA("apms_dropout", e);

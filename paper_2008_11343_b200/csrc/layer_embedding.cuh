@@ -84,16 +84,16 @@ __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 // ------------------------------------------------------------------------------------------ gradient
 //
 // dw[v] = round(scale * sum of dout[i] over the i with tokens[i] = v), rows without a token 0.  Three kernels:
-//   k_embed_sort   the first cluster of CTAs sorts (token, position) by token, positions in order; the other clusters meanwhile write the zeros, so that
-//                  the sort costs no time of its own where the table is large
-//   k_embed_sums   `length` sorted entries a group of threads, eight rows of dout in flight: runs of one token that lie within are written,
-//                  what belongs to a run that goes on to the left or the right is left as a partial sum
-//   k_embed_joins  adds up the partial sums of the runs over several groups
+//   k_embed_sort   one cluster of CTAs sorts (token, position) by token, positions in order
+//   k_embed_zeros  meanwhile zeros into all of dw, which costs HBM nothing else in that time (only the rows that no token has: their bits have to be found first, by clusters
+//                  that the hardware puts on half of the SMs: 28 us for 512 tokens and 94 MB)
+//   k_embed_sums   `length` sorted entries a group of threads, eight rows of dout in flight: runs of one token within are written, as are those that end in the next group;
+//                  what belongs to a longer run is left as a partial sum
+//   k_embed_joins  adds up the partial sums of the longer runs, which k_embed_sums has listed
+// Up to 512 tokens need no sort: k_embed_few, a CTA a token, finds its equals itself (and leaves the work to the first of them).
 // The sums are binary32, in an order that the sizes fix.  Bound by HBM: dout read once, dw written once.
 
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBits = 8, kSortBins = 1 << kSortBits;
-constexpr int kMostClearing = 16;                                   // clusters that write zeros
-constexpr int kClearRows = 1 << 16;                                 // rows whose bits a CTA of them holds at once
+constexpr int kSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBits = 9, kSortBins = 1 << kSortBits;
 
 struct EmbedBackArgs {
     Tokens tokens;
@@ -102,46 +102,69 @@ struct EmbedBackArgs {
     void* dw;
     uint2 *sorted, *other;                                          // (token, position): the result, and the other buffer of the sort
     float *head, *tail;                                             // partial sums of each group: of the run that came from the left, of the one that goes on
+    uint32_t *listed, *list;                                        // how many groups have a longer run's beginning, and which (in any order)
     int64_t padded;                                                 // floats a partial sum's row takes
     int length, passes, digit;                                      // entries a group; of the sort, bits a pass
     int64_t groups;
     float scale;
 };
 
-// Which of the warp's lanes hold the same digit.
-__device__ __forceinline__ uint32_t same_digit(uint32_t d) { return __match_any_sync(0xffffffffu, d); }
+// Which of the warp's lanes hold the same digit of `bits` bits (and are `here`).
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool here)
+{
+    uint32_t same = __ballot_sync(0xffffffffu, here);
+    for (int b = 0; b < bits; ++b) {
+        const uint32_t ones = __ballot_sync(0xffffffffu, d >> b & 1);
+        same &= d >> b & 1 ? ones : ~ones;
+    }
+    return same;
+}
 
 // Stable radix sort, least significant digit first, by one cluster: each warp owns a run of consecutive entries and counts its digits, the CTAs read
-// one another's counts through shared memory, and each warp's entries move to their places in order.  Entries live in global memory (L2).
-__device__ void embed_sort(const EmbedBackArgs& a, uint32_t (*counts)[kSortBins], uint32_t* total, uint32_t* base, uint32_t* warp_sums)
+// one another's counts through shared memory, and each warp's entries move to their places in order.  Entries live in global memory (L2) and come eight a lane at a time,
+// so that a pass over them waits for memory a few times only (one at a time: 36 us for 65,536 tokens, where this takes 13).
+constexpr int kAhead = 8;
+struct SortShared { uint32_t counts[kSortWarps][kSortBins], total[kSortBins], base[kSortBins], warp_sums[kSortWarps]; };
+__device__ void embed_sort(const EmbedBackArgs& a, SortShared& s)
 {
+    auto& counts = s.counts;
+    uint32_t *total = s.total, *base = s.base, *warp_sums = s.warp_sums;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), bins = 1u << a.digit, mask = bins - 1;
     const int64_t share = ((a.count + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) / 32 * 32;
     const int64_t begin = min(a.count, ((int64_t)rank * kSortWarps + warp) * share), end = min(a.count, begin + share);
     for (int pass = 0; pass < a.passes; ++pass) {
         const int shift = pass * a.digit;
-        const uint2* from = pass & 1 ? ((a.passes & 1) ? a.sorted : a.other) : ((a.passes & 1) ? a.other : a.sorted);
-        uint2* to = pass & 1 ? ((a.passes & 1) ? a.other : a.sorted) : ((a.passes & 1) ? a.sorted : a.other);
-        auto entry = [&](int64_t i) { return pass == 0 ? make_uint2(a.tokens.row(i), (uint32_t)i) : __ldcg(from + i); };
+        const bool last_first = (a.passes & 1) != (pass & 1);       // into `sorted` in the last pass, and every second one before it
+        const uint2* from = last_first ? a.other : a.sorted;
+        uint2* to = last_first ? a.sorted : a.other;
+        uint2 e[kAhead] = {};
+        auto load = [&](int64_t i0) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t i = i0 + k * 32 + lane;
+                if (i < end) e[k] = pass == 0 ? make_uint2(a.tokens.row(i), (uint32_t)i) : __ldcg(from + i);
+            }
+        };
         for (uint32_t d = lane; d < bins; d += 32) counts[warp][d] = 0;
         __syncwarp();
-        for (int64_t i0 = begin; i0 < end; i0 += 32) {
-            const bool here = i0 + lane < end;
-            const uint32_t d = here ? (entry(i0 + lane).x >> shift) & mask : bins;
-            const uint32_t same = same_digit(d);
-            if (here && lane == __ffs(same) - 1) counts[warp][d] += __popc(same);
-            __syncwarp();
+        for (int64_t i0 = begin; i0 < end; i0 += kAhead * 32) {
+            load(i0);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (i0 + k * 32 + lane < end) atomicAdd(&counts[warp][(e[k].x >> shift) & mask], 1u);
         }
         __syncthreads();
         if (threadIdx.x < bins) {                                   // each warp's entries of a digit come after those of the warps before it
             uint32_t sum = 0;
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = counts[w][threadIdx.x]; counts[w][threadIdx.x] = sum; sum += c; }
             total[threadIdx.x] = sum;
         }
         cluster_barrier();
         uint32_t before = 0, all = 0;
         if (threadIdx.x < bins) {
+#pragma unroll
             for (uint32_t r = 0; r < kSortCtas; ++r) {
                 uint32_t c;
                 asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(cluster_address(shared_address(total + threadIdx.x), r)));
@@ -149,7 +172,9 @@ __device__ void embed_sort(const EmbedBackArgs& a, uint32_t (*counts)[kSortBins]
                 all += c;
             }
         }
-        uint32_t upto = all;                                        // digits in order: an inclusive scan over the CTA's first 256 threads
+        const bool last = pass == a.passes - 1;
+        if (last) cluster_arrive_relaxed();                         // no CTA ends before all have read its counts
+        uint32_t upto = all;                                        // digits in order: an inclusive scan over the CTA's first threads
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
         if (lane == 31) warp_sums[warp] = upto;
@@ -159,80 +184,55 @@ __device__ void embed_sort(const EmbedBackArgs& a, uint32_t (*counts)[kSortBins]
             base[threadIdx.x] = before + upto - all;
         }
         __syncthreads();
-        for (int64_t i0 = begin; i0 < end; i0 += 32) {
-            const bool here = i0 + lane < end;
-            const uint2 e = here ? entry(i0 + lane) : make_uint2(0, 0);
-            const uint32_t d = here ? (e.x >> shift) & mask : bins;
-            const uint32_t same = same_digit(d);
-            if (here) {
-                const uint32_t at = base[d] + counts[warp][d] + __popc(same & ((1u << lane) - 1));
-                __stcg(to + at, e);
+        for (uint32_t d = lane; d < bins; d += 32) counts[warp][d] += base[d];
+        __syncwarp();
+        for (int64_t i0 = begin; i0 < end; i0 += kAhead * 32) {
+            if (end - begin > kAhead * 32) load(i0);                // else they are still there
+            uint32_t same[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (i0 + k * 32 >= end) break;
+                same[k] = same_digit(e[k].x >> shift & mask, a.digit, i0 + k * 32 + lane < end);
             }
-            __syncwarp();
-            if (here && lane == __ffs(same) - 1) counts[warp][d] += __popc(same);
-            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (i0 + k * 32 >= end) break;
+                const bool here = i0 + k * 32 + lane < end;
+                uint32_t* count = &counts[warp][(e[k].x >> shift) & mask];
+                const uint32_t rank_in = __popc(same[k] & ((1u << lane) - 1)), at = here ? *count + rank_in : 0u;
+                if (here) __stcg(to + at, e[k]);
+                __syncwarp();
+                if (here && rank_in == 0) *count = at + __popc(same[k]);
+                __syncwarp();
+            }
         }
-        cluster_barrier();                                          // the entries are in place, and no CTA's counts are read any more
+        if (last) cluster_wait();
+        else cluster_barrier();                                     // the entries are in place, and no CTA's counts are read any more
     }
 }
 
-// Zeros into the rows of [begin, end) that no token has.  Each CTA of a cluster looks at a share of the tokens; the rows' bits are joined through shared memory.
-template <int OT>
-__device__ void embed_clear(const EmbedBackArgs& a, int64_t begin, int64_t end, uint32_t* bits, uint32_t* own, bool vector)
+__global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedBackArgs a)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
-    for (int64_t at = begin; at < end; at += kClearRows) {
-        const int64_t rows = min((int64_t)kClearRows, end - at);
-        const int words = (int)((rows + 31) / 32);
-        for (int w = threadIdx.x; w < words; w += kSortThreads) bits[w] = 0;
-        __syncthreads();
-        for (int64_t i = (int64_t)rank * kSortThreads + threadIdx.x; i < a.count; i += kSortCtas * kSortThreads) {
-            const int64_t r = (int64_t)a.tokens.row(i) - at;
-            if (r >= 0 && r < rows) atomicOr(bits + (r >> 5), 1u << (r & 31));
-        }
-        cluster_barrier();
-        const int mine = (words - (int)rank + kSortCtas - 1) / kSortCtas;                             // every eighth word's rows
-        for (int k = threadIdx.x; k < mine; k += kSortThreads) {
-            uint32_t taken = 0;
-            for (uint32_t r = 0; r < kSortCtas; ++r) {
-                uint32_t v;
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_address(shared_address(bits + rank + k * kSortCtas), r)));
-                taken |= v;
-            }
-            own[k] = taken;
-        }
-        __syncthreads();
-        const int64_t row_bytes = a.width * kBytes<OT>;
-        for (int i = warp; i < mine * 32; i += kSortWarps) {
-            const int64_t r = ((int64_t)rank + (i >> 5) * kSortCtas) * 32 + (i & 31);
-            if (r >= rows || (own[i >> 5] >> (i & 31) & 1)) continue;
-            char* row = static_cast<char*>(a.dw) + (at + r) * row_bytes;
-            if (vector) {
-                for (int64_t c = lane * 16; c < row_bytes; c += 512) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
-            } else {
-                for (int64_t c = lane; c < a.width; c += 32) store1<OT>(row, c, 0.0f);
-            }
-        }
-        cluster_barrier();
-    }
-}
-
-template <int OT>
-__global__ void __launch_bounds__(kSortThreads) k_embed_sort(EmbedBackArgs a, int clearing, int vector)
-{
-    __shared__ union {
-        struct { uint32_t counts[kSortWarps][kSortBins], total[kSortBins], base[kSortBins], warp_sums[kSortWarps]; } sort;
-        struct { uint32_t bits[kClearRows / 32], own[kClearRows / 32 / kSortCtas]; } clear;
-    } s;
+    extern __shared__ float4 room[];
     allow_next_kernel();
-    const int cluster = blockIdx.x / kSortCtas;
-    if (cluster == 0) {
-        embed_sort(a, s.sort.counts, s.sort.total, s.sort.base, s.sort.warp_sums);
-    } else {
-        const int64_t share = ((a.tokens.vocab + clearing - 1) / clearing + 31) / 32 * 32, begin = min(a.tokens.vocab, (cluster - 1) * share);
-        embed_clear<OT>(a, begin, min(a.tokens.vocab, begin + share), s.clear.bits, s.clear.own, vector);
-    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.listed = 0;
+    embed_sort(a, *reinterpret_cast<SortShared*>(room));
+}
+
+// Ends after the sort (the kernel launched before it), so that what waits for this kernel has waited for both.
+template <int OT>
+__global__ void __launch_bounds__(512) k_embed_zeros(EmbedBackArgs a)
+{
+    allow_next_kernel();
+    const int64_t bytes = a.tokens.vocab * a.width * kBytes<OT>, threads = (int64_t)gridDim.x * 512, first = (int64_t)blockIdx.x * 512 + threadIdx.x;
+    char* p = static_cast<char*>(a.dw);
+    const int64_t head = min(bytes, (int64_t)(-(uintptr_t)p & 15)), whole = (bytes - head) / 16, tail = bytes - head - whole * 16;       // whole elements: p lies on one
+    if (first < head / kBytes<OT>) store1<OT>(p, first, 0.0f);
+    if (first < tail / kBytes<OT>) store1<OT>(p + head + whole * 16, first, 0.0f);
+    uint4* q = reinterpret_cast<uint4*>(p + head);
+#pragma unroll 4
+    for (int64_t i = first; i < whole; i += threads) q[i] = make_uint4(0, 0, 0, 0);
+    wait_for_last_kernel();
 }
 
 // Columns of the groups of eight that a thread holds: consecutive where rows lie on 16-byte boundaries, else `lanes` apart.
@@ -245,7 +245,7 @@ struct Columns {
 
 // A group: `lanes` threads (a power of two up to 128) hold 8 columns each of a slice of 8 * lanes; blockIdx.y is the slice.
 template <int DT, int OT, bool VECTOR>
-__global__ void __launch_bounds__(128) k_embed_sums(EmbedBackArgs a, int lanes)
+__global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lanes)
 {
     constexpr int FLIGHT = 8;
     const int lane = threadIdx.x & (lanes - 1), per_cta = 128 / lanes;
@@ -256,13 +256,20 @@ __global__ void __launch_bounds__(128) k_embed_sums(EmbedBackArgs a, int lanes)
     if (group >= a.groups || columns.first >= a.width) return;
     const int64_t begin = group * a.length, end = min(a.count, begin + a.length);
     const uint32_t vocab = (uint32_t)a.tokens.vocab;
-    const uint32_t left = begin ? a.sorted[begin - 1].x : vocab, right = end < a.count ? a.sorted[end].x : vocab;
+    auto token = [&](int64_t i) { return i >= 0 && i < a.count ? a.sorted[i].x : vocab; };
+    // The run over the border to the left, and the one over that to the right, where they are short: each begins in the group before the border and ends in the one behind it,
+    // and is that one's whole work.  Longer runs leave partial sums.
+    const uint32_t last = token(end - 1), right = token(end), left = token(begin - 1);
+    const bool takes_right = right == last && last != vocab && left != last && token(end + a.length) != last;
+    const bool skips_left = left != vocab && left == token(begin) && token(begin - a.length - 1) != left && right != left;
+    const int64_t limit = takes_right ? min(a.count, end + a.length) : end;
     float sum[8];
     uint32_t run = vocab;                                           // the running token; `vocab`: none yet
     bool from_left = false;
 
     auto write = [&](bool goes_on) {
         if (run == vocab) return;
+        if (goes_on && !from_left && lane == 0 && blockIdx.y == 0) a.list[atomicAdd(a.listed, 1u)] = (uint32_t)group;
         float* partial = from_left ? a.head + group * a.padded : goes_on ? a.tail + group * a.padded : nullptr;
         if (VECTOR) {
             if (partial) { store8<APMS_GRAD_F32>(partial, columns.first, sum); return; }
@@ -280,10 +287,20 @@ __global__ void __launch_bounds__(128) k_embed_sums(EmbedBackArgs a, int lanes)
         }
     };
 
-    for (int64_t i0 = begin; i0 < end; i0 += FLIGHT) {
+    uint2 next[FLIGHT];                                             // one batch ahead of the rows
+    auto entries = [&](int64_t i0) {
+#pragma unroll
+        for (int k = 0; k < FLIGHT; ++k) next[k] = i0 + k < limit ? a.sorted[i0 + k] : make_uint2(vocab, 0);
+    };
+    entries(begin);
+    for (int64_t i0 = begin; i0 < limit; i0 += FLIGHT) {
         uint2 e[FLIGHT];
 #pragma unroll
-        for (int k = 0; k < FLIGHT; ++k) e[k] = i0 + k < end ? a.sorted[i0 + k] : make_uint2(vocab, 0);
+        for (int k = 0; k < FLIGHT; ++k) {
+            e[k] = next[k];
+            if ((skips_left && e[k].x == left) || (i0 + k >= end && e[k].x != last)) e[k].x = vocab;
+        }
+        if (i0 >= end && e[0].x == vocab) break;                    // behind the run that goes on
         float v[VECTOR ? 1 : FLIGHT][8];
         Eight<DT> raw[VECTOR ? FLIGHT : 1];
 #pragma unroll
@@ -296,6 +313,7 @@ __global__ void __launch_bounds__(128) k_embed_sums(EmbedBackArgs a, int lanes)
                 for (int j = 0; j < 8; ++j) v[k][j] = columns.at(j) < a.width ? load1<DT>(a.d, e[k].y * a.d_stride + columns.at(j)) : 0.0f;
             }
         }
+        entries(i0 + FLIGHT);
 #pragma unroll
         for (int k = 0; k < FLIGHT; ++k) {
             if (e[k].x == vocab) continue;                          // behind the group's entries, or no row (sorted last)
@@ -313,51 +331,125 @@ __global__ void __launch_bounds__(128) k_embed_sums(EmbedBackArgs a, int lanes)
             }
         }
     }
-    write(run == right);
+    write(run == right && !takes_right);
 }
 
-// The runs over several groups: 256 columns a CTA, four a thread, its four strips of threads taking every fourth partial sum.
+// The longer runs, one a time and 256 columns of it: four columns a thread, eight strips of threads each with an eighth of the partial sums.
+constexpr int kStrips = 8, kJoinCtas = 296;
 template <int OT>
-__global__ void __launch_bounds__(256) k_embed_joins(EmbedBackArgs a)
+__global__ void __launch_bounds__(kStrips * 64, 2) k_embed_joins(EmbedBackArgs a)
 {
-    __shared__ float4 sums[3][64];
-    const int64_t group = blockIdx.x, end = (group + 1) * a.length;
+    __shared__ float4 sums[kStrips - 1][64];
     const int lane = threadIdx.x & 63, strip = threadIdx.x >> 6;
     wait_for_last_kernel();
-    const uint32_t run = a.sorted[end - 1].x, before = group ? a.sorted[end - a.length - 1].x : (uint32_t)a.tokens.vocab;
-    // launched for all groups but the last, so end < count
-    if (a.sorted[end].x != run || before == run || run == (uint32_t)a.tokens.vocab) return;               // none goes on, or it began further left
-    int64_t low = group + 1, high = a.groups;                       // the last group that begins with the run: in [low, high)
-    while (high - low > 1) {
-        const int64_t middle = (low + high) / 2;
-        if (a.sorted[middle * a.length].x == run) low = middle; else high = middle;
-    }
-    for (int64_t c0 = (int64_t)blockIdx.y * 256; c0 < a.width; c0 += (int64_t)gridDim.y * 256) {
-        const int64_t c = c0 + lane * 4;                            // padded rows: whole groups of four
+    const int64_t slices = (a.width + 255) / 256, items = (int64_t)*a.listed * slices;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t group = a.list[item / slices], c = (item % slices) * 256 + lane * 4;       // padded rows: whole groups of four
+        const uint32_t run = a.sorted[(group + 1) * a.length].x;
+        int64_t low = group + 1, step = 1;                          // the last group that begins with the run: 32 probes at a time, first of the next groups
+        for (;;) {
+            const int64_t probe = low + ((threadIdx.x & 31) + 1) * step;
+            const uint32_t still = __ballot_sync(0xffffffffu, probe < a.groups && a.sorted[probe * a.length].x == run);
+            low += (still == 0xffffffffu ? 32 : __ffs(~still) - 1) * step;
+            if (still == 0xffffffffu) step *= 32;
+            else if (step == 1) break;
+            else step /= 32;
+        }
+        const int64_t partials = low - group, share = (partials + kStrips - 1) / kStrips, first = group + 1 + strip * share, end = min(low + 1, first + share);
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         auto add = [&](const float4& v) { sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; };
         if (c < a.width) {
             if (strip == 0) sum = *reinterpret_cast<const float4*>(a.tail + group * a.padded + c);
-            int64_t g = group + 1 + strip;
-            for (; g + 28 <= low; g += 32) {
+            for (int64_t g = first; g < end; g += 8) {
                 float4 v[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float4*>(a.head + (g + 4 * k) * a.padded + c);
+                for (int i = 0; i < 8; ++i)
+                    if (g + i < end) v[i] = *reinterpret_cast<const float4*>(a.head + (g + i) * a.padded + c);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) add(v[k]);
+                for (int i = 0; i < 8; ++i)
+                    if (g + i < end) add(v[i]);
             }
-            for (; g <= low; g += 4) add(*reinterpret_cast<const float4*>(a.head + g * a.padded + c));
         }
         __syncthreads();
         if (strip) sums[strip - 1][lane] = sum;
         __syncthreads();
         if (strip == 0 && c < a.width) {
-            for (int s = 0; s < 3; ++s) add(sums[s][lane]);
+            for (int s = 0; s < kStrips - 1; ++s) add(sums[s][lane]);
             const float v[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (c + j < a.width) store1<OT>(a.dw, run * a.width + c + j, v[j] * a.scale);
         }
+    }
+}
+
+// Up to kFew tokens: a CTA a token and slice of columns, its `512 / lanes` strips of threads each a share of the rows of its equals, in order.
+constexpr int kFew = 512;
+template <int DT, int OT, bool VECTOR>
+__global__ void __launch_bounds__(kFew, 2) k_embed_few(EmbedBackArgs a, int lanes)
+{
+    __shared__ uint32_t rows[kFew];
+    __shared__ int upto[kFew / 32];
+    __shared__ float sums[kFew * 8];
+    const int thread = threadIdx.x, lane = thread & (lanes - 1), strip = thread / lanes, strips = kFew / lanes, me = blockIdx.x;
+    const uint32_t vocab = (uint32_t)a.tokens.vocab;
+    const uint32_t mine = a.tokens.row(me), other = thread < a.count ? a.tokens.row(thread) : vocab;
+    const bool equal = other == mine;
+    const uint32_t equals = __ballot_sync(0xffffffffu, equal);
+    if ((thread & 31) == 0) upto[thread >> 5] = __popc(equals);
+    if (__syncthreads_or(mine == vocab || (equal && thread < me))) return;       // no row, or an earlier token's work
+    int before = 0, count = 0;
+    for (int w = 0; w < kFew / 32; ++w) {
+        if (w < thread >> 5) before += upto[w];
+        count += upto[w];
+    }
+    if (equal) rows[before + __popc(equals & ((1u << (thread & 31)) - 1))] = (uint32_t)thread;
+    __syncthreads();
+    const Columns<DT, VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
+    const int share = (count + strips - 1) / strips, begin = min(count, strip * share), end = min(count, begin + share);
+    float sum[8] = {};
+    if (columns.first < a.width) {
+        for (int i0 = begin; i0 < end; i0 += 4) {
+            float v[4][8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (i0 + k >= end) break;
+                const int64_t row = rows[i0 + k] * a.d_stride;
+                if constexpr (VECTOR) {
+                    const Eight<DT> raw = load8<DT>(a.d, row + columns.first);
+                    values8<DT>(v[k], raw);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[k][j] = columns.at(j) < a.width ? load1<DT>(a.d, row + columns.at(j)) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (i0 + k >= end) break;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += v[k][j];
+            }
+        }
+    }
+    if (share < count) {                                            // more strips than one had rows
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[j * kFew + thread] = sum[j];
+        __syncthreads();
+        if (strip == 0)
+            for (int s = 1; s * share < count; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += sums[j * kFew + s * lanes + lane];
+    }
+    wait_for_last_kernel();                                         // the zeros
+    if (strip || columns.first >= a.width) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+    if (VECTOR) {
+        store8<OT>(a.dw, mine * a.width + columns.first, sum);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (columns.at(j) < a.width) store1<OT>(a.dw, mine * a.width + columns.at(j), sum[j]);
     }
 }
 
@@ -381,16 +473,16 @@ cudaError_t launch_embed_to(const EmbedArgs& a, int out_type, bool vector, cudaS
 }
 
 // How the work is cut: by the sizes alone, so that the order of the sums is the same on every GPU.
-struct EmbedPlan { int lanes, length, passes, digit; int64_t slices, groups, padded; size_t entries, bytes; };
+struct EmbedPlan { int lanes, length, passes, digit; int64_t slices, groups, padded; size_t entries, listed, bytes; };
 EmbedPlan embed_plan(int64_t count, int64_t vocab, int64_t width)
 {
     EmbedPlan p = {};
     p.lanes = 1;
     while (p.lanes < 128 && p.lanes * 8 < width) p.lanes *= 2;
     p.slices = (width + 8 * p.lanes - 1) / (8 * p.lanes);
-    // about 1024 CTAs of 128 threads, of 8 to 128 entries: fewer partial sums with long groups, more in flight with many
+    // about 1024 CTAs of 128 threads, of 8 to 256 entries: several waves, since a group can take on as many entries again; the fewer, the more partial sums
     const int64_t per_cta = 128 / p.lanes;
-    p.length = (int)std::min<int64_t>(128, std::max<int64_t>(8, (count * p.slices + 1024 * per_cta - 1) / (1024 * per_cta)));
+    p.length = (int)std::min<int64_t>(256, std::max<int64_t>(8, (count * p.slices + 1024 * per_cta * 8 - 1) / (1024 * per_cta * 8) * 8));
     p.groups = (count + p.length - 1) / p.length;
     int bits = 1;                                                   // of the numbers 0 to vocab
     while ((vocab >> bits) > 0) ++bits;
@@ -398,23 +490,28 @@ EmbedPlan embed_plan(int64_t count, int64_t vocab, int64_t width)
     p.digit = (bits + p.passes - 1) / p.passes;
     p.padded = (width + 7) / 8 * 8;
     p.entries = ((size_t)count * sizeof(uint2) + 255) / 256 * 256;
-    p.bytes = 2 * p.entries + 2 * (size_t)p.groups * (size_t)p.padded * sizeof(float);
+    p.listed = 2 * p.entries + 2 * (size_t)p.groups * (size_t)p.padded * sizeof(float);
+    p.bytes = count <= kFew ? 0 : p.listed + (1 + (size_t)p.groups) * sizeof(uint32_t);
     return p;
 }
 
 template <int DT, int OT>
 cudaError_t launch_embed_back(const EmbedBackArgs& a, const EmbedPlan& p, bool vector, cudaStream_t stream)
 {
-    const int64_t bytes = a.tokens.vocab * a.width * kBytes<OT>;
-    const int clearing = (int)std::min<int64_t>(kMostClearing, std::max<int64_t>(1, bytes >> 19));       // half a megabyte a cluster at least
-    const bool clear16 = on_16(a.dw) && a.width * kBytes<OT> % 16 == 0;
-    cudaError_t e = launch_clusters(k_embed_sort<OT>, kSortCtas, dim3(kSortCtas * (1 + clearing)), kSortThreads, 0, stream, a, clearing, (int)clear16);
-    if (e != cudaSuccess) return e;
-    const int64_t per_cta = 128 / p.lanes;
-    const dim3 grid((unsigned)((p.groups + per_cta - 1) / per_cta), (unsigned)p.slices);
-    e = vector ? launch(k_embed_sums<DT, OT, true>, grid, 128, 0, stream, true, a, p.lanes) : launch(k_embed_sums<DT, OT, false>, grid, 128, 0, stream, true, a, p.lanes);
-    if (e != cudaSuccess || p.groups < 2) return e;
-    return launch(k_embed_joins<OT>, dim3((unsigned)(p.groups - 1), (unsigned)std::min<int64_t>(4, (a.width + 255) / 256)), 256, 0, stream, true, a);
+    const int64_t bytes = a.tokens.vocab * a.width * kBytes<OT>, per_cta = 128 / p.lanes;
+    const dim3 zeros((unsigned)std::min<int64_t>(1024, bytes / 32768 + 1)), grid((unsigned)((p.groups + per_cta - 1) / per_cta), (unsigned)p.slices), few((unsigned)a.count, (unsigned)p.slices);
+    if (a.count <= kFew) {
+        const cudaError_t e = launch(k_embed_zeros<OT>, zeros, 512, 0, stream, false, a);
+        if (e != cudaSuccess) return e;
+        return vector ? launch(k_embed_few<DT, OT, true>, few, kFew, 0, stream, true, a, p.lanes) : launch(k_embed_few<DT, OT, false>, few, kFew, 0, stream, true, a, p.lanes);
+    }
+    static Raised raised[kMostDevices];
+    cudaError_t e = raise_limits(raised, reinterpret_cast<const void*>(k_embed_sort), sizeof(SortShared), true);
+    if (e == cudaSuccess) e = launch_clusters(k_embed_sort, kSortCtas, dim3(kSortCtas), kSortThreads, sizeof(SortShared), stream, a);
+    if (e == cudaSuccess) e = launch(k_embed_zeros<OT>, zeros, 512, 0, stream, true, a);
+    if (e == cudaSuccess) e = vector ? launch(k_embed_sums<DT, OT, true>, grid, 128, 0, stream, true, a, p.lanes) : launch(k_embed_sums<DT, OT, false>, grid, 128, 0, stream, true, a, p.lanes);
+    if (e == cudaSuccess) e = launch(k_embed_joins<OT>, dim3(kJoinCtas), kStrips * 64, 0, stream, true, a);
+    return e;
 }
 
 template <int DT>
@@ -453,7 +550,7 @@ apms_status apms_embedding(const apms_embedding_args* args, void* cuda_stream)
     EmbedArgs a = {};
     a.tokens = {g.tokens, g.token_bytes == 8, g.vocab};
     a.count = g.count; a.width = g.width; a.w_stride = g.weight_stride; a.w = g.weight; a.out = g.out; a.scale = g.scale;
-    const bool vector = rows_of_eight(a.w, g.vocab, a.w_stride, a.width, g.weight_type) && on_16(a.out);
+    const bool vector = rows_of_eight(a.w, g.vocab, a.w_stride, a.width, g.weight_type) && on_eight(a.out, g.out_type);
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     OPERATOR_CUDA("apms_embedding", g.weight_type == APMS_GRAD_F32 ? launch_embed_to<APMS_GRAD_F32>(a, g.out_type, vector, stream)
                                   : g.weight_type == APMS_GRAD_BF16 ? launch_embed_to<APMS_GRAD_BF16>(a, g.out_type, vector, stream)
@@ -486,7 +583,7 @@ apms_status apms_embedding_backward(const apms_embedding_backward_args* args, vo
         return APMS_OK;
     }
     const EmbedPlan p = embed_plan(g.count, g.vocab, g.width);
-    if (!g.workspace_dev || ((uintptr_t)g.workspace_dev & 255u) || g.workspace_bytes < p.bytes)
+    if (p.bytes && (!g.workspace_dev || ((uintptr_t)g.workspace_dev & 255u) || g.workspace_bytes < p.bytes))
         return operator_fail(APMS_ERR_OOM, "%s: needs apms_embedding_backward_workspace_bytes() of 256-byte aligned workspace", who);
     EmbedBackArgs a = {};
     a.tokens = {g.tokens, g.token_bytes == 8, g.vocab};
@@ -495,7 +592,8 @@ apms_status apms_embedding_backward(const apms_embedding_backward_args* args, vo
     char* w = static_cast<char*>(g.workspace_dev);
     a.sorted = reinterpret_cast<uint2*>(w); a.other = reinterpret_cast<uint2*>(w + p.entries);
     a.head = reinterpret_cast<float*>(w + 2 * p.entries); a.tail = a.head + p.groups * p.padded;
-    const bool vector = rows_of_eight(a.d, a.count, a.d_stride, a.width, g.dout_type) && on_16(a.dw);
+    a.listed = reinterpret_cast<uint32_t*>(w + p.listed); a.list = a.listed + 1;
+    const bool vector = rows_of_eight(a.d, a.count, a.d_stride, a.width, g.dout_type) && on_eight(a.dw, g.dweight_type);
     OPERATOR_CUDA("apms_embedding_backward", g.dout_type == APMS_GRAD_F32 ? launch_embed_back_to<APMS_GRAD_F32>(a, p, g.dweight_type, vector, stream)
                                            : g.dout_type == APMS_GRAD_BF16 ? launch_embed_back_to<APMS_GRAD_BF16>(a, p, g.dweight_type, vector, stream)
                                                                            : launch_embed_back_to<APMS_GRAD_F16>(a, p, g.dweight_type, vector, stream));

@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(128) k_scan_step_any(StepArgs a)
 
 // Warps in time: as many as the sequence has spans, up to a team.  Teams: two a CTA where the GPU's 148 SMs get no more than a slab each.  Segments: where they get fewer, as many as
 // fill the SMs, of 512 steps at least (below that the second kernel's launch costs more than it saves).  By the sizes alone, so that results are the same on every GPU.
-constexpr int kSms = 148, kLeastPart = 512;
+constexpr int kSms = 148, kLeastPart = 128;
 int plan_scan(ScanArgs& a, int64_t batch, int64_t steps, int64_t width, int type)
 {
     const int64_t wide = type == APMS_GRAD_F32 ? 64 : 128;
@@ -857,7 +857,7 @@ apms_status apms_gated_scan_step(const apms_gated_scan_step_args* args, void* cu
     if (!on_element(g.x, g.type) || !on_element(g.gate, g.type) || !on_element(g.h, g.type) || !on_element(g.state, APMS_GRAD_F32) || !on_element(g.next, APMS_GRAD_F32))
         return operator_fail(APMS_ERR_INVALID_ARG, "%s: an address is not aligned to its element size", who);
     const StepArgs a = {g.batch, g.width, g.x_stride, g.gate_stride, g.x, g.gate, g.state, g.h, g.next};
-    const bool vector = rows_of_eight(a.x, a.batch, a.x_stride, a.width, g.type) && rows_of_eight(a.gate, a.batch, a.gate_stride, a.width, g.type) && on_16(a.h) && on_16(a.state) && on_16(a.next);
+    const bool vector = rows_of_eight(a.x, a.batch, a.x_stride, a.width, g.type) && rows_of_eight(a.gate, a.batch, a.gate_stride, a.width, g.type) && on_eight(a.h, g.type) && on_eight(a.state, APMS_GRAD_F32) && on_eight(a.next, APMS_GRAD_F32);
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     OPERATOR_CUDA("apms_gated_scan_step", g.type == APMS_GRAD_F32 ? launch_step<APMS_GRAD_F32>(a, vector, stream)
                                         : g.type == APMS_GRAD_BF16 ? launch_step<APMS_GRAD_BF16>(a, vector, stream) : launch_step<APMS_GRAD_F16>(a, vector, stream));
