@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 //   k_embed_sort   one cluster of CTAs sorts (token, position) by token, positions in order
 //   k_embed_zeros  meanwhile zeros into all of dw, which costs HBM nothing else in that time (only the rows that no token has: their bits have to be found first, by clusters
 //                  that the hardware puts on half of the SMs: 28 us for 512 tokens and 94 MB)
-//   k_embed_sums   `length` sorted entries a group of threads, eight rows of dout in flight: runs of one token within are written, as are those that end in the next group;
+//   k_embed_sums   `length` sorted entries a group of threads, up to eight rows of dout in flight: runs of one token within are written, as are those that end in the next group;
 //                  what belongs to a longer run is left as a partial sum
 //   k_embed_joins  adds up the partial sums of the longer runs, which k_embed_sums has listed
 // Up to 512 tokens need no sort: k_embed_few, a CTA a token, finds its equals itself (and leaves the work to the first of them).
@@ -247,7 +247,7 @@ struct Columns {
 template <int DT, int OT, bool VECTOR>
 __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lanes)
 {
-    constexpr int FLIGHT = 8;
+    constexpr int FLIGHT = VECTOR && DT != APMS_GRAD_F32 ? 8 : 4;
     const int lane = threadIdx.x & (lanes - 1), per_cta = 128 / lanes;
     const int64_t group = (int64_t)blockIdx.x * per_cta + threadIdx.x / lanes;
     const Columns<DT, VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
@@ -287,48 +287,57 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
         }
     };
 
-    uint2 next[FLIGHT];                                             // one batch ahead of the rows
-    auto entries = [&](int64_t i0) {
-#pragma unroll
-        for (int k = 0; k < FLIGHT; ++k) next[k] = i0 + k < limit ? a.sorted[i0 + k] : make_uint2(vocab, 0);
+    // Rolling: as a row is added its place is loaded with the row FLIGHT entries on, whose entry came FLIGHT entries before that, so that FLIGHT rows are always in flight.
+    uint32_t key[FLIGHT];                                           // of the rows in flight; `vocab`: none
+    uint2 next[FLIGHT];
+    float v[VECTOR ? 1 : FLIGHT][8];
+    Eight<DT> raw[VECTOR ? FLIGHT : 1];
+    auto entry = [&](int64_t i) {
+        uint2 e = i < limit ? a.sorted[i] : make_uint2(vocab, 0);
+        if ((skips_left && e.x == left) || (i >= end && e.x != last)) e.x = vocab;
+        return e;
     };
-    entries(begin);
+    auto load = [&](int k, const uint2& e) {
+        key[k] = e.x;
+        if (e.x == vocab) return;
+        if constexpr (VECTOR) {
+            raw[k] = load8<DT>(a.d, e.y * a.d_stride + columns.first);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = columns.at(j) < a.width ? load1<DT>(a.d, e.y * a.d_stride + columns.at(j)) : 0.0f;
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) next[k] = entry(begin + k);
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k) {
+        load(k, next[k]);
+        next[k] = entry(begin + FLIGHT + k);
+    }
     for (int64_t i0 = begin; i0 < limit; i0 += FLIGHT) {
-        uint2 e[FLIGHT];
+        if (i0 >= end && key[0] == vocab) break;                    // behind the run that goes on
 #pragma unroll
         for (int k = 0; k < FLIGHT; ++k) {
-            e[k] = next[k];
-            if ((skips_left && e[k].x == left) || (i0 + k >= end && e[k].x != last)) e[k].x = vocab;
-        }
-        if (i0 >= end && e[0].x == vocab) break;                    // behind the run that goes on
-        float v[VECTOR ? 1 : FLIGHT][8];
-        Eight<DT> raw[VECTOR ? FLIGHT : 1];
+            if (key[k] != vocab) {                                  // else behind the group's entries, or no row (sorted last)
+                float one[8];
+                if constexpr (VECTOR) values8<DT>(one, raw[k]);
+                else {
 #pragma unroll
-        for (int k = 0; k < FLIGHT; ++k) {
-            if (e[k].x == vocab) continue;
-            if constexpr (VECTOR) {
-                raw[k] = load8<DT>(a.d, e[k].y * a.d_stride + columns.first);
-            } else {
+                    for (int j = 0; j < 8; ++j) one[j] = v[k][j];
+                }
+                if (key[k] != run) {
+                    write(false);
+                    from_left = run == vocab && key[k] == left;
+                    run = key[k];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[k][j] = columns.at(j) < a.width ? load1<DT>(a.d, e[k].y * a.d_stride + columns.at(j)) : 0.0f;
+                    for (int j = 0; j < 8; ++j) sum[j] = one[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += one[j];
+                }
             }
-        }
-        entries(i0 + FLIGHT);
-#pragma unroll
-        for (int k = 0; k < FLIGHT; ++k) {
-            if (e[k].x == vocab) continue;                          // behind the group's entries, or no row (sorted last)
-            float one[8];
-            if constexpr (VECTOR) values8<DT>(one, raw[k]);
-            if (e[k].x != run) {
-                write(false);
-                from_left = run == vocab && e[k].x == left;
-                run = e[k].x;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] = VECTOR ? one[j] : v[VECTOR ? 0 : k][j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += VECTOR ? one[j] : v[VECTOR ? 0 : k][j];
-            }
+            load(k, next[k]);
+            next[k] = entry(i0 + 2 * FLIGHT + k);
         }
     }
     write(run == right && !takes_right);
