@@ -673,7 +673,8 @@ apms_status apms_embedding_backward(const apms_embedding_backward_args* args, vo
  * runs, so that a captured call follows them; used_dev (NULL or two such) receives what was read.
  * The gradient of x is the same call with dh in the place of x, no residual and the same numbers.
  * x: rows x_stride apart; residual (NULL or of h_type): rows residual_stride apart; h: contiguous rows.  With a residual h_type is
- * x_type or binary32; without one x_type, or any type if x is binary32.  rows * width <= APMS_DROPOUT_MAX. */
+ * x_type or binary32; without one x_type, or any type if x is binary32.  rows * width <= APMS_DROPOUT_MAX, and
+ * where there are several rows width <= 2^31 - 256. */
 #define APMS_DROPOUT_MAX ((int64_t)1 << 34)
 typedef struct {
     int64_t rows, width;

@@ -89,33 +89,74 @@ __global__ void __launch_bounds__(256) k_dropout(DropArgs a)
     }
 }
 
-// Any width and alignment: a warp takes 256 consecutive elements, whose 32 blocks its lanes form and share, and goes over them 32 at a time.
-template <int XT, int RT, bool RESIDUAL, int HT>
-__global__ void __launch_bounds__(256) k_dropout_any(DropArgs a)
+// Any width and alignment: a warp takes kSpans times 256 consecutive elements, whose 32 blocks its lanes form and share, and goes over them 64 at a time, two a lane.  FLAT: one row.
+// Bound by the instructions beside HBM: places are stepped on from one pair to the next.
+constexpr int kSpans = 2;
+template <int XT, int RT, bool RESIDUAL, int HT, bool FLAT>
+__global__ void __launch_bounds__(256) k_dropout_any(DropArgs a, int pairs)
 {
     __shared__ uint4 words[8][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t first = ((int64_t)blockIdx.x * 8 + warp) * 256;
-    if (first >= a.numel) return;
+    int64_t span = ((int64_t)blockIdx.x * 8 + warp) * (256 * kSpans), first = span + lane * 2;
+    if (span >= a.numel) return;
+    const int width = FLAT ? 0 : (int)a.width;
+    const int64_t row = FLAT ? 0 : a.numel <= 0xffffffffll ? (uint32_t)first / (uint32_t)width : first / width;
+    int col = FLAT ? 0 : (int)(first - row * width);
+    const auto* px = static_cast<const typename Element<XT>::T*>(a.x) + (FLAT ? first : row * a.x_stride + col);
+    const auto* pr = static_cast<const typename Element<RT>::T*>(a.r) + (FLAT ? first : row * a.r_stride + col);
+    const int64_t x_next = FLAT ? 0 : a.x_stride - width, r_next = FLAT ? 0 : a.r_stride - width;        // from a row's end to the next one's beginning
+    auto* h = static_cast<typename Element<HT>::T*>(a.h) + first;
+    const uint32_t* bits = reinterpret_cast<const uint32_t*>(words[warp]) + lane;
     const Source source(a);
-    words[warp][lane] = source.eight((uint32_t)(first / 8) + lane);
-    __syncwarp();
-    const uint16_t* bits = reinterpret_cast<const uint16_t*>(words[warp]);
-    int64_t i = first + lane, row = i / a.width, col = i - row * a.width;
-    float x[8], r[8];
+
+    auto pass = [&](auto whole, int64_t left) {                     // left: elements from this lane's first one on
+        float x[4][2], r[4][2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (i + k * 32 < a.numel) {
-            x[k] = load1<XT>(a.x, row * a.x_stride + col);
-            if (RESIDUAL) r[k] = load1<RT>(a.r, row * a.r_stride + col);
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                x[k][j] = r[k][j] = 0.0f;
+                const bool next = !FLAT && j && col + 1 == width;   // the second of a pair, in the next row
+                if (whole.value || k * 64 + j < left) {
+                    x[k][j] = (float)px[next ? x_next + 1 : j];
+                    if (RESIDUAL) r[k][j] = (float)pr[next ? r_next + 1 : j];
+                }
+            }
+            px += 64;
+            if (RESIDUAL) pr += 64;
+            if (!FLAT)
+                for (col += 64; col >= width; col -= width) {
+                    px += x_next;
+                    if (RESIDUAL) pr += r_next;
+                }
         }
-        for (col += 32; col >= a.width; col -= a.width) ++row;
-    }
+        words[warp][lane] = source.eight((uint32_t)(span / 8) + lane);          // behind the loads
+        __syncwarp();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (i + k * 32 >= a.numel) break;
-        const float v = dropped(x[k], bits[k * 32 + lane], a);
-        store1<HT>(a.h, i + k * 32, RESIDUAL ? v + r[k] : v);
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = bits[k * 32];
+            float v[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                v[j] = dropped(x[k][j], j ? w >> 16 : w & 0xffffu, a);
+                if (RESIDUAL) v[j] += r[k][j];
+            }
+            if (pairs && (whole.value || k * 64 + 1 < left)) {
+                if constexpr (HT == APMS_GRAD_F32) *reinterpret_cast<float2*>(h + k * 64) = make_float2(v[0], v[1]);
+                else *reinterpret_cast<uint32_t*>(h + k * 64) = pack16<HT>(v[0], v[1]);
+            } else {
+                if (whole.value || k * 64 < left) store1<HT>(h, k * 64, v[0]);
+                if (whole.value || k * 64 + 1 < left) store1<HT>(h, k * 64 + 1, v[1]);
+            }
+        }
+        __syncwarp();
+        h += 256;
+    };
+    for (int s = 0; s < kSpans && span < a.numel; ++s) {
+        const int64_t left = a.numel - first;
+        if (span + 256 <= a.numel) pass(std::true_type(), left); else pass(std::false_type(), left);
+        span += 256;
+        first += 256;
     }
 }
 
@@ -123,7 +164,11 @@ __global__ void __launch_bounds__(256) k_dropout_any(DropArgs a)
 template <int XT, int RT, bool RESIDUAL, int HT>
 cudaError_t launch_dropout(const DropArgs& a, bool vector, cudaStream_t stream)
 {
-    if (!vector) return launch(k_dropout_any<XT, RT, RESIDUAL, HT>, dim3((unsigned)((a.numel + 2047) / 2048)), 256, 0, stream, false, a);
+    if (!vector) {
+        const int pairs = (uintptr_t)a.h % (2 * kBytes<HT>) == 0;
+        auto kernel = a.rows == 1 ? k_dropout_any<XT, RT, RESIDUAL, HT, true> : k_dropout_any<XT, RT, RESIDUAL, HT, false>;
+        return launch(kernel, dim3((unsigned)((a.numel + 2048 * kSpans - 1) / (2048 * kSpans))), 256, 0, stream, false, a, pairs);
+    }
     constexpr int MANY = XT == APMS_GRAD_F32 || RT == APMS_GRAD_F32 ? 2 : 4;
     const int64_t units = a.numel / 8;
     if (units < (int64_t)1024 * 256 * MANY) return launch(k_dropout<XT, RT, RESIDUAL, HT, 1>, dim3((unsigned)(units / 256 + 1)), 256, 0, stream, false, a);
@@ -149,6 +194,7 @@ extern "C" apms_status apms_dropout(const apms_dropout_args* args, void* cuda_st
     const apms_dropout_args& g = *args;
     if (g.rows < 0 || g.width < 1 || g.width > APMS_DROPOUT_MAX || g.rows > APMS_DROPOUT_MAX / g.width)
         return operator_fail(APMS_ERR_INVALID_ARG, "%s: %lld rows of %lld: needs rows >= 0, width >= 1 and at most 2^34 elements", who, (long long)g.rows, (long long)g.width);
+    if (g.rows > 1 && g.width > 0x7fffff00) return operator_fail(APMS_ERR_INVALID_ARG, "%s: %lld rows of %lld: several rows have at most 2^31 - 256 elements each", who, (long long)g.rows, (long long)g.width);
     if (!known_type(g.x_type) || !known_type(g.h_type)) return operator_fail(APMS_ERR_INVALID_ARG, "%s: unknown element type", who);
     if (g.residual ? g.h_type != g.x_type && g.h_type != APMS_GRAD_F32 : g.h_type != g.x_type && g.x_type != APMS_GRAD_F32)
         return operator_fail(APMS_ERR_INVALID_ARG, "%s: h has x's type, or binary32 with a residual, or 16 bits of a binary32 x without one", who);

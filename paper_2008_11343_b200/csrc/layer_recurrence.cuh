@@ -40,34 +40,38 @@ template <int TYPE> constexpr int kLaneChannels = 2 * kPairs<TYPE>;
 __device__ __forceinline__ float exp2_fast(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 __device__ __forceinline__ float reciprocal_fast(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 __device__ __forceinline__ float lower(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-constexpr float kLog2E = 1.44269504f;
+__device__ __forceinline__ float higher(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+constexpr float kLog2E = 1.44269504f, kLog2ELow = 1.92596303e-8f, kLn2 = 0.693147181f;               // log2(e) as a sum of two
 
-// z and, for the backward pass, -z and a z of a gate.  16-bit types take the approximate exponential and reciprocal (about 2^-19 relative to z at
-// |gate| = 16, beside their 2^-9 and 2^-12; a z below 2^-126 counts as 0), binary32 the library's.  Neither loses digits where z or a is small.
+// exp(gate) for z = 1 / (1 + exp(gate)), from the approximate power of two (2^-22).  In 16 bits the rounding of its argument adds about 2^-19 at |gate| = 16, beside the types' own
+// 2^-9 and 2^-12; binary32 takes what was rounded off as a factor 1 + ln 2 * rest.  BOUND: finite for any gate.
+template <int TYPE, bool BOUND>
+__device__ __forceinline__ float2 exp_of(float2 gate)
+{
+    if constexpr (TYPE == APMS_GRAD_F32) {
+        gate = make_float2(higher(lower(gate.x, 88.0f), -120.0f), higher(lower(gate.y, 88.0f), -120.0f));
+        const float2 t = mul2(gate, both(kLog2E)), rest = fma2(gate, both(kLog2ELow), fma2(gate, both(kLog2E), make_float2(-t.x, -t.y)));
+        const float2 e = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+        return fma2(mul2(rest, both(kLn2)), e, e);
+    } else {
+        float2 t = mul2(gate, both(kLog2E));
+        if (BOUND) t = make_float2(lower(t.x, 127.0f), lower(t.y, 127.0f));
+        return make_float2(exp2_fast(t.x), exp2_fast(t.y));
+    }
+}
+// z and, for the backward pass, -z and a z.  Neither loses digits where z or a is small; a z below 2^-126 counts as 0.
 template <int TYPE>
 __device__ __forceinline__ float2 taken(float2 gate)
 {
-    if constexpr (TYPE == APMS_GRAD_F32) {
-        return make_float2(1.0f / (1.0f + expf(gate.x)), 1.0f / (1.0f + expf(gate.y)));
-    } else {
-        const float2 e = mul2(gate, both(kLog2E)), d = add2(make_float2(exp2_fast(e.x), exp2_fast(e.y)), both(1.0f));
-        return make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
-    }
+    const float2 d = add2(exp_of<TYPE, false>(gate), both(1.0f));
+    return make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
 }
 template <int TYPE>
 __device__ __forceinline__ void minus_taken_and_slope(float2 gate, float2& nz, float2& az)
 {
-    if constexpr (TYPE == APMS_GRAD_F32) {
-        const float2 z = taken<TYPE>(gate);
-        nz = make_float2(-z.x, -z.y);
-        az = mul2(taken<TYPE>(make_float2(-gate.x, -gate.y)), z);
-    } else {
-        float2 e = mul2(gate, both(kLog2E));
-        e = make_float2(exp2_fast(lower(e.x, 127.0f)), exp2_fast(lower(e.y, 127.0f)));           // finite, so that e z z is 0 where z is
-        const float2 d = fma2(e, both(-1.0f), both(-1.0f));
-        nz = make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
-        az = mul2(mul2(e, nz), nz);
-    }
+    const float2 e = exp_of<TYPE, true>(gate), d = fma2(e, both(-1.0f), both(-1.0f));              // e is finite: e z z is 0 where z is
+    nz = make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
+    az = mul2(mul2(e, nz), nz);
 }
 __device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, both(-1.0f), a); }  // exact product: rounded as a difference
 

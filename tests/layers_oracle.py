@@ -78,8 +78,9 @@ def dropout(x, p, seed, step, site, residual=None):
 # ------------------------------------------------------------------------------------------ gated linear recurrence
 
 def sigmoid_error(kind):
-    """Relative error of z = 1 / (1 + exp(gate)) in units of 2^-24.  binary32: exp 4, the sum 1, the quotient 1, and 2 to spare.  16 bits, |gate| <= 16: the exponential's
-    argument 1.5 |gate| = 24, its result and the reciprocal 4 each, the sum 1, and 1 to spare."""
+    """Relative error of z = 1 / (1 + exp(gate)) in units of 2^-24.  binary32: the power of two 4 (its documented 2^-22), the
+    factor for its argument's rest 1, the sum 1, the reciprocal 2 (one unit in the last place).  16 bits, |gate| <= 16: the argument 1.5 |gate| = 24, the power of two 4, the
+    sum 1, the reciprocal 2, and 3 to spare."""
     return 8.0 if kind == torch.float32 else 34.0
 
 
