@@ -651,7 +651,7 @@ apms_status apms_embedding(const apms_embedding_args* args, void* cuda_stream);
 /* dweight[v] = scale * (sum of dout[i] over the i with tokens[i] = v), 0 for a v that is no token: all vocab rows are written, contiguous.
  * Summed in binary32, in an order fixed by count, vocab, width and the tokens; rounded once to dweight_type.  Tokens outside
  * [0, vocab) contribute nothing.  dout: rows dout_stride >= 0 elements apart.  dweight must not overlap dout or tokens.
- * workspace_dev: apms_embedding_backward_workspace_bytes(count, vocab, width), 256-byte aligned (0 bytes for a count up to 512). */
+ * workspace_dev: apms_embedding_backward_workspace_bytes(count, vocab, width), 256-byte aligned (0 bytes for a count up to 1024). */
 typedef struct {
     int64_t count, vocab, width;
     const void* tokens;   int token_bytes;

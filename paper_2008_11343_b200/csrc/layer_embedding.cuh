@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 //   k_embed_sums   `length` sorted entries a group of threads, up to eight rows of dout in flight: runs of one token within are written, as are those that end in the next group;
 //                  what belongs to a longer run is left as a partial sum
 //   k_embed_joins  adds up the partial sums of the longer runs, which k_embed_sums has listed
-// Up to 512 tokens need no sort: k_embed_few, a CTA a token, finds its equals itself (and leaves the work to the first of them).
+// Up to 1024 tokens need no sort: k_embed_few, a CTA a token, finds its equals itself (and leaves the work to the first of them).
 // The sums are binary32, in an order that the sizes fix.  Bound by HBM: dout read once, dw written once.
 
 constexpr int kSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBits = 9, kSortBins = 1 << kSortBits;
@@ -392,27 +392,35 @@ __global__ void __launch_bounds__(kStrips * 64, 2) k_embed_joins(EmbedBackArgs a
     }
 }
 
-// Up to kFew tokens: a CTA a token and slice of columns, its `512 / lanes` strips of threads each a share of the rows of its equals, in order.
-constexpr int kFew = 512;
+// Up to kFew tokens: a CTA a token and slice of columns, its `kFewThreads / lanes` strips of threads each a share of the rows of its equals, in order.
+constexpr int kFew = 1024, kFewThreads = 512, kFewWarps = kFewThreads / 32;
 template <int DT, int OT, bool VECTOR>
-__global__ void __launch_bounds__(kFew, 2) k_embed_few(EmbedBackArgs a, int lanes)
+__global__ void __launch_bounds__(kFewThreads, 2) k_embed_few(EmbedBackArgs a, int lanes)
 {
     __shared__ uint32_t rows[kFew];
     __shared__ int upto[kFew / 32];
-    __shared__ float sums[kFew * 8];
-    const int thread = threadIdx.x, lane = thread & (lanes - 1), strip = thread / lanes, strips = kFew / lanes, me = blockIdx.x;
-    const uint32_t vocab = (uint32_t)a.tokens.vocab;
-    const uint32_t mine = a.tokens.row(me), other = thread < a.count ? a.tokens.row(thread) : vocab;
-    const bool equal = other == mine;
-    const uint32_t equals = __ballot_sync(0xffffffffu, equal);
-    if ((thread & 31) == 0) upto[thread >> 5] = __popc(equals);
-    if (__syncthreads_or(mine == vocab || (equal && thread < me))) return;       // no row, or an earlier token's work
-    int before = 0, count = 0;
+    __shared__ float sums[kFewThreads * 8];
+    const int thread = threadIdx.x, lane = thread & (lanes - 1), strip = thread / lanes, strips = kFewThreads / lanes, me = blockIdx.x;
+    const uint32_t vocab = (uint32_t)a.tokens.vocab, mine = a.tokens.row(me);
+    uint32_t equals[kFew / kFewThreads];                            // of the warp's 32 tokens, 512 apart
+    bool earlier = false;
+#pragma unroll
+    for (int q = 0; q < kFew / kFewThreads; ++q) {
+        const int i = q * kFewThreads + thread;
+        const bool equal = i < a.count && a.tokens.row(i) == mine;
+        earlier |= equal && i < me;
+        equals[q] = __ballot_sync(0xffffffffu, equal);
+        if ((thread & 31) == 0) upto[q * kFewWarps + (thread >> 5)] = __popc(equals[q]);
+    }
+    if (__syncthreads_or(mine == vocab || earlier)) return;         // no row, or an earlier token's work
+    int count = 0;
+#pragma unroll
     for (int w = 0; w < kFew / 32; ++w) {
-        if (w < thread >> 5) before += upto[w];
+        if (w / kFewWarps * kFewThreads >= a.count) break;
+        const uint32_t own = equals[w / kFewWarps];
+        if (w % kFewWarps == thread >> 5 && (own >> (thread & 31) & 1)) rows[count + __popc(own & ((1u << (thread & 31)) - 1))] = (uint32_t)(w / kFewWarps * kFewThreads + thread);
         count += upto[w];
     }
-    if (equal) rows[before + __popc(equals & ((1u << (thread & 31)) - 1))] = (uint32_t)thread;
     __syncthreads();
     const Columns<DT, VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
     const int share = (count + strips - 1) / strips, begin = min(count, strip * share), end = min(count, begin + share);
@@ -442,12 +450,12 @@ __global__ void __launch_bounds__(kFew, 2) k_embed_few(EmbedBackArgs a, int lane
     }
     if (share < count) {                                            // more strips than one had rows
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[j * kFew + thread] = sum[j];
+        for (int j = 0; j < 8; ++j) sums[j * kFewThreads + thread] = sum[j];
         __syncthreads();
         if (strip == 0)
             for (int s = 1; s * share < count; ++s)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += sums[j * kFew + s * lanes + lane];
+                for (int j = 0; j < 8; ++j) sum[j] += sums[j * kFewThreads + s * lanes + lane];
     }
     wait_for_last_kernel();                                         // the zeros
     if (strip || columns.first >= a.width) return;
@@ -512,7 +520,7 @@ cudaError_t launch_embed_back(const EmbedBackArgs& a, const EmbedPlan& p, bool v
     if (a.count <= kFew) {
         const cudaError_t e = launch(k_embed_zeros<OT>, zeros, 512, 0, stream, false, a);
         if (e != cudaSuccess) return e;
-        return vector ? launch(k_embed_few<DT, OT, true>, few, kFew, 0, stream, true, a, p.lanes) : launch(k_embed_few<DT, OT, false>, few, kFew, 0, stream, true, a, p.lanes);
+        return vector ? launch(k_embed_few<DT, OT, true>, few, kFewThreads, 0, stream, true, a, p.lanes) : launch(k_embed_few<DT, OT, false>, few, kFewThreads, 0, stream, true, a, p.lanes);
     }
     static Raised raised[kMostDevices];
     cudaError_t e = raise_limits(raised, reinterpret_cast<const void*>(k_embed_sort), sizeof(SortShared), true);

@@ -142,7 +142,33 @@ def _operator_cases():
         rstd = torch.rand(rows, device="cuda")
         return lambda: O.rms_norm_backward(dy, h, w, rstd, dh), rows * width * (2 * dtype.itemsize + (3 if both else 2) * stream.itemsize)
 
+    def lookup(tokens, width, back=False, vocabulary=30_522):
+        t = torch.randint(0, vocabulary, (tokens,), device="cuda")
+        if back:
+            dout, out = tensor(tokens, width), torch.empty(vocabulary, width, device="cuda")
+            return lambda: O.embedding_backward(dout, t, vocabulary, out=out), 8 * tokens + 2 * tokens * width + 4 * vocabulary * width
+        table = tensor(vocabulary, width)
+        return lambda: O.embedding_forward(t, table, 2.0), 8 * tokens + 2 * width * (len(t.unique()) + tokens)
+
+    def drop(rows, width, junction=True):
+        x, rng = tensor(rows, width), torch.tensor([1, 2], device="cuda")
+        r = tensor(rows, width) if junction else None
+        return lambda: O.dropout_forward(x, 0.1, rng, 0, r), rows * width * (6 if junction else 4)
+
+    def scan(batch, steps, width, back=False, dtype=torch.bfloat16):
+        x, gate, dh = (torch.empty(batch, steps, width, device="cuda", dtype=dtype).normal_() for _ in range(3))
+        n = batch * steps * width * dtype.itemsize
+        if not back:
+            return lambda: O.gated_scan_forward(x, gate), 3 * n
+        starts = O.gated_scan_forward(x, gate, keep=True)[2]
+        return lambda: O.gated_scan_backward(dh, x, gate, starts), 5 * n
+
     return {
+        "k_embed": lambda: lookup(65_536, 1024), "k_embed_few": lambda: lookup(512, 1024, back=True), "k_embed_sort": lambda: lookup(65_536, 1024, back=True),
+        "k_embed_zeros": lambda: lookup(65_536, 1024, back=True), "k_embed_sums": lambda: lookup(65_536, 1024, back=True), "k_embed_joins": lambda: lookup(65_536, 1024, back=True),
+        "k_dropout": lambda: drop(8192, 4096, junction=False), "k_dropout_junction": lambda: drop(8192, 4096), "k_dropout_any": lambda: drop(8191, 4095),
+        "k_scan": lambda: scan(16, 2048, 2048), "k_scan_f32": lambda: scan(8, 2048, 2048, dtype=torch.float32), "k_scan_odd": lambda: scan(16, 2048, 2047), "k_scan_parts": lambda: scan(1, 32_768, 1024),
+        "k_scan_back": lambda: scan(16, 2048, 2048, back=True), "k_scan_back_f32": lambda: scan(8, 2048, 2048, back=True, dtype=torch.float32),
         "k_tile_squares": lambda: gradients(False), "k_list_norm": lambda: gradients(False), "k_one_norm": lambda: gradients(False, 4), "k_scale_tiles": lambda: gradients(True),
         "k_scale_tiles_in_place": lambda: gradients(True, in_place=True),
         "k_rms_staged": lambda: forward(8192, 4096), "k_rms_staged_row_scale": lambda: forward(8192, 4096, group=0),

@@ -57,7 +57,7 @@ def test_the_gradient_refuses(changes, words):
 
 def test_the_gradient_needs_its_workspace():
     need = B.apms_embedding_backward_workspace_bytes(3000, 5, 8)
-    assert need >= 2 * 3000 * 8 and 0 == B.apms_embedding_backward_workspace_bytes(-1, 5, 8) == B.apms_embedding_backward_workspace_bytes(3000, 0, 8) == B.apms_embedding_backward_workspace_bytes(512, 5, 8)
+    assert need >= 2 * 3000 * 8 and 0 == B.apms_embedding_backward_workspace_bytes(-1, 5, 8) == B.apms_embedding_backward_workspace_bytes(3000, 0, 8) == B.apms_embedding_backward_workspace_bytes(1024, 5, 8)
     for bad in ({"workspace_dev": None}, {"workspace_dev": 4096 + 128}, {"workspace_bytes": need - 1}):
         refused(lambda: B.apms_embedding_backward(gradient(count=3000, **bad), None), "workspace", B.ERR_OOM)
 
