@@ -672,7 +672,7 @@ apms_status apms_embedding_backward(const apms_embedding_backward_args* args, vo
  * s = 65536 / (65536 - T).  What is dropped counts as 0 whatever it is.  rng_dev: two 64-bit integers {seed, step} in device memory, read when the kernel
  * runs, so that a captured call follows them; used_dev (NULL or two such) receives what was read.
  * The gradient of x is the same call with dh in the place of x, no residual and the same numbers.
- * x: rows x_stride apart; residual (NULL or of h_type): rows residual_stride apart; h: contiguous rows.  With a residual h_type is
+ * x: rows x_stride apart; residual (NULL or of h_type): rows residual_stride apart; h: contiguous rows, overlapping neither.  With a residual h_type is
  * x_type or binary32; without one x_type, or any type if x is binary32.  rows * width <= APMS_DROPOUT_MAX, and
  * where there are several rows width <= 2^31 - 256. */
 #define APMS_DROPOUT_MAX ((int64_t)1 << 34)
@@ -692,8 +692,8 @@ apms_status apms_dropout(const apms_dropout_args* args, void* cuda_stream);
  *
  * Per sequence and channel, with z_t = 1 / (1 + exp(gate_t)):   h_t = h_(t-1) + z_t (x_t - h_(t-1)),   h_(-1) = state (0 where it is NULL).
  * States are held in binary32 from step to step; h (batch x steps x width, contiguous, of `type`) is rounded once.  gate = +infinity keeps a state,
- * -infinity replaces it.  x and gate: elements of a step consecutive, steps and sequences *_step_stride and *_batch_stride >= 0 elements apart.
- * steps <= 2^30, batch * width <= 2^31.  state, last: batch x width floats; last receives the states behind the last step (with steps = 0: the first ones).
+ * -infinity replaces it, where all are finite (0 times an infinity or NaN is NaN).  x and gate: elements of a step consecutive, steps and sequences *_step_stride and *_batch_stride >= 0 elements apart.
+ * steps <= 2^30, batch * width <= 2^31.  h, last and starts overlap no input.  state, last: batch x width floats; last receives the states behind the last step (with steps = 0: the first ones).
  * starts (NULL, or apms_gated_scan_starts_bytes, 16-byte aligned): what the backward pass needs of the forward pass.
  * workspace_dev: apms_gated_scan_workspace_bytes, 16-byte aligned (0 bytes where sequences are not cut into segments), for both passes. */
 typedef struct {
@@ -713,7 +713,7 @@ apms_status apms_gated_scan(const apms_gated_scan_args* args, void* cuda_stream)
 
 /* Gradients: with G_t = dh_t + a_(t+1) G_(t+1), a = 1 - z, and dlast (NULL: 0) in the place of a G behind the last step,
  *   dx_t = z_t G_t,   dgate_t = G_t (h_(t-1) - x_t) a_t z_t,   dstate = a_0 G_0 (NULL: not written; dlast where steps = 0),
- * the states being formed again from x, gate and starts.  dx, dgate: contiguous, of `type`. */
+ * the states being formed again from x, gate and starts.  dx, dgate: contiguous, of `type`, overlapping no input. */
 typedef struct {
     int64_t batch, steps, width;
     const void* dh;       int64_t dh_batch_stride, dh_step_stride;
@@ -730,7 +730,7 @@ typedef struct {
 apms_status apms_gated_scan_backward(const apms_gated_scan_backward_args* args, void* cuda_stream);
 
 /* One step of `batch` sequences: x and gate are batch rows, *_stride elements apart, of `type`; state and next batch x width floats (next may be
- * state); h: batch x width, contiguous, of `type`. */
+ * state, and overlaps nothing else); h: batch x width, contiguous, of `type`. */
 typedef struct {
     int64_t batch, width;
     const void* x;        int64_t x_stride;

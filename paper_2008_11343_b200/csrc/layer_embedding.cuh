@@ -62,23 +62,26 @@ __global__ void __launch_bounds__(256) k_embed(EmbedArgs a)
     }
 }
 
-// Any width and alignment, element by element, eight a thread.
+// Any width and alignment: a warp a row and 256 columns of it at a time, eight elements a lane.
 template <int WT, int OT>
 __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 {
-    const int64_t numel = a.count * a.width, first = (int64_t)blockIdx.x * 2048 + threadIdx.x;
-    float v[8] = {};
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int64_t i = first + k * 256;
-        if (i >= numel) break;
-        const int64_t row = numel <= 0xffffffffll ? (uint32_t)i / (uint32_t)a.width : i / a.width;
+    const int lane = threadIdx.x & 31;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < a.count; row += (int64_t)gridDim.x * 8) {
         const uint32_t from = a.tokens.row(row);
-        if (from < a.tokens.vocab) v[k] = load1<WT>(a.w, from * a.w_stride + (i - row * a.width)) * a.scale;
-    }
+        const auto* w = static_cast<const typename Element<WT>::T*>(a.w) + from * a.w_stride;
+        for (int64_t c0 = lane; c0 < a.width; c0 += 256) {
+            float v[8] = {};
+            if (from < a.tokens.vocab) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (first + k * 256 < numel) store1<OT>(a.out, first + k * 256, v[k]);
+                for (int k = 0; k < 8; ++k)
+                    if (c0 + k * 32 < a.width) v[k] = (float)w[c0 + k * 32] * a.scale;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c0 + k * 32 < a.width) store1<OT>(a.out, row * a.width + c0 + k * 32, v[k]);
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------ gradient
@@ -412,7 +415,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_embed_few(EmbedBackArgs a, i
         equals[q] = __ballot_sync(0xffffffffu, equal);
         if ((thread & 31) == 0) upto[q * kFewWarps + (thread >> 5)] = __popc(equals[q]);
     }
-    if (__syncthreads_or(mine == vocab || earlier)) return;         // no row, or an earlier token's work
+    if (__syncthreads_or(mine == vocab || earlier)) {               // no row, or an earlier token's work
+        wait_for_last_kernel();                                     // even if all CTAs end here, the grid must not end before the zeros are written
+        return;
+    }
     int count = 0;
 #pragma unroll
     for (int w = 0; w < kFew / 32; ++w) {
@@ -476,7 +482,7 @@ template <int WT, int OT>
 cudaError_t launch_embed(const EmbedArgs& a, bool vector, cudaStream_t stream)
 {
     const int64_t numel = a.count * a.width, units = numel / 8;
-    if (!vector) return launch(k_embed_any<WT, OT>, dim3((unsigned)((numel + 2047) / 2048)), 256, 0, stream, false, a);
+    if (!vector) return launch(k_embed_any<WT, OT>, dim3((unsigned)std::min<int64_t>(1 << 20, (a.count + 7) / 8)), 256, 0, stream, false, a);
     constexpr int MANY = WT == APMS_GRAD_F32 ? 2 : 4;
     if (units < (int64_t)1024 * 256 * MANY) return launch(k_embed<WT, OT, 1>, dim3((unsigned)((units + 255) / 256)), 256, 0, stream, false, a);
     return launch(k_embed<WT, OT, MANY>, dim3((unsigned)((units + 256 * MANY - 1) / (256 * MANY))), 256, 0, stream, false, a);

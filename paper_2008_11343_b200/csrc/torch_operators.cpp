@@ -525,6 +525,11 @@ PyObject* gated_scan_step(PyObject*, PyObject* const* args, Py_ssize_t n)
         a.state = static_cast<const float*>(state.const_data_ptr());
         a.next = static_cast<float*>(next.data_ptr());
         if (a.state != a.next && a.state < a.next + next.numel() && a.next < a.state + state.numel()) refuse("out shares part of state's memory");
+        auto meets = [&](const Rows& r) {
+            const char *p0 = static_cast<const char*>(r.p), *n0 = reinterpret_cast<const char*>(a.next);
+            return a.batch && p0 < n0 + next.nbytes() && n0 < p0 + ((a.batch - 1) * r.stride + a.width) * (int64_t)x.element_size();
+        };
+        if (meets(xr) || meets(gr)) refuse("the new states share memory with x or gate");
         a.h = h.data_ptr();
         check(c_gated_scan_step(&a, c10::cuda::getCurrentCUDAStream(x.get_device()).stream()));
         note_write(next.unsafeGetTensorImpl());

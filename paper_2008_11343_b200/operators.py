@@ -215,7 +215,7 @@ def gated_scan_forward(x, gate, state=None, keep: bool = False):
     """(h, last, starts): over the steps of x and gate, (batch, steps, width) of one type, h_t = h_(t-1) + sigmoid(-gate_t) (x_t - h_(t-1)) for every
     channel, from `state` ((batch, width) float32; zeros without one).  States are binary32 from step to step; h has x's type, last is the state
     behind the last step (float32).  starts: with keep what gated_scan_backward needs, else None.  A gate of +infinity keeps the state, one of -infinity
-    replaces it by x (where a packed sequence begins, say)."""
+    replaces it by x (where a packed sequence begins, say) - as long as x and the state are finite: 0 times infinity is NaN."""
     return _load().gated_scan(x, gate, state, keep)
 
 

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import layers_oracle as oracle
+from paper_2008_11343_b200 import binding as B
 from paper_2008_11343_b200 import operators as O
 
 pytestmark = pytest.mark.gpu
@@ -360,9 +361,11 @@ def all_of_them(rng, tokens, weight, gate, state):
     return (d, last, *torch.autograd.grad(d.float().sum() + last.sum(), (weight, gate, state)))
 
 
-def test_a_run_of_them_captured_and_replayed_follows_its_inputs():
-    tokens = tokens_for(4 * 60, 100, 80).view(4, 60)
-    weight, gate, state = normal((100, 64), BF16, seed=81).requires_grad_(), gates((4, 60, 64), BF16, 82).requires_grad_(), normal((4, 64), seed=83).requires_grad_()
+@pytest.mark.parametrize("steps", [60, 700])                                       # without and with a sort, a sequence whole and in segments
+def test_a_run_of_them_captured_and_replayed_follows_its_inputs(steps):
+    shape = (4, steps)
+    tokens = tokens_for(4 * steps, 100, 80).view(shape)
+    weight, gate, state = normal((100, 64), BF16, seed=81).requires_grad_(), gates((*shape, 64), BF16, 82).requires_grad_(), normal((4, 64), seed=83).requires_grad_()
     rng = rng_of(3, 0)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -376,10 +379,50 @@ def test_a_run_of_them_captured_and_replayed_follows_its_inputs():
     for step in range(3):
         with torch.no_grad():
             weight.normal_(generator=gen(84 + step))
-            tokens.copy_(tokens_for(4 * 60, 100, 90 + step).view(4, 60))
+            tokens.copy_(tokens_for(4 * steps, 100, 90 + step).view(shape))
         want = all_of_them(rng_of(3, step), tokens, weight, gate, state)
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(outputs, want)) and rng.tolist() == [3, step + 1]
+
+
+@pytest.mark.parametrize("count", [500, 3000])
+def test_a_captured_gradient_without_any_row_is_whole_before_what_follows(count):
+    """No CTA of the summing kernels has work: what comes next in the graph still finds all zeros written."""
+    tokens, dout = torch.full((count,), -100, device="cuda"), normal((count, 512), F32, seed=95)
+    out = torch.empty(60_000, 512, device="cuda")
+    O.embedding_backward(dout, tokens, 60_000, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        O.embedding_backward(dout, tokens, 60_000, out=out)
+        seen = out.clone()
+    for _ in range(5):
+        out.fill_(1.0)
+        graph.replay()
+        assert not seen.any()
+
+
+@pytest.mark.parametrize("where", ["cpu", "type", "shape", "overlap"])
+def test_refusals(where):
+    x, state = normal((3, 8)), normal((3, 8))
+    tokens, weight, rng = torch.zeros(3, dtype=torch.int64, device="cuda"), normal((5, 8)), rng_of(1, 2)
+    scan = normal((2, 5, 8))
+    calls = {
+        "cpu": [lambda: O.embedding(tokens.cpu(), weight), lambda: O.embedding_backward(x, tokens.cpu(), 5), lambda: O.dropout(x, 0.1, rng.cpu()), lambda: O.gated_scan(scan, scan.cpu()),
+                lambda: O.gated_scan(scan, scan, normal((2, 8)).cpu()), lambda: O.gated_scan_step(x, x, state.cpu())],
+        "type": [lambda: O.embedding(tokens.float(), weight), lambda: O.embedding(tokens, weight.double()), lambda: O.embedding(tokens, weight, dtype=torch.int32), lambda: O.dropout(x, 0.1, rng.int()),
+                 lambda: O.dropout(x, 0.1, rng, residual=x.half()), lambda: O.gated_scan(scan, scan.half()), lambda: O.gated_scan(scan, scan, normal((2, 8), F16)),
+                 lambda: O.gated_scan_step(x, x.half(), state), lambda: O.embedding_backward(x, tokens, 5, out=torch.empty(5, 8, dtype=torch.int32, device="cuda"))],
+        "shape": [lambda: O.embedding(tokens, weight[0]), lambda: O.embedding_backward(x, tokens[:2], 5), lambda: O.embedding_backward(x, tokens, 0), lambda: O.embedding_backward(x, tokens, 5, out=weight[:4]),
+                  lambda: O.dropout(x, 0.1, rng, residual=x[:2]), lambda: O.dropout(x, 0.1, rng[:1]), lambda: O.gated_scan(scan, scan[:, :4]), lambda: O.gated_scan(x, x), lambda: O.gated_scan(scan, scan, state),
+                  lambda: O.gated_scan_backward(scan, scan, scan, state), lambda: O.gated_scan_step(scan, scan, state), lambda: O.gated_scan_step(x, x, state.t())],
+        "overlap": [lambda: O.embedding_backward(x, tokens[:3], 3, out=x), lambda: O.gated_scan_step(x, x, state, out=x), lambda: O.gated_scan_step(x, x.clone(), state.view(-1)[:24].view(3, 8), out=state.new_empty(0).view(0, 8))],
+    }
+    for call in calls[where]:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: O.dropout(x, 1.5, rng), lambda: O.dropout(x, float("nan"), rng), lambda: O.dropout(x, 0.1, rng, -1), lambda: O.dropout_backward(x.half(), 0.1, rng, dtype=F32)):
+        with pytest.raises(B.ApmsError):
+            call()
 
 
 def test_calls_on_two_streams_do_not_meet():
