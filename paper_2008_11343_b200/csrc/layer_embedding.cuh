@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 //
 // dw[v] = round(scale * sum of dout[i] over the i with tokens[i] = v), rows without a token 0.  Three kernels:
 //   k_embed_sort   one cluster of CTAs sorts (token, position) by token, positions in order
-//   k_embed_zeros  meanwhile zeros into all of dw, which costs HBM nothing else in that time (only the rows that no token has: their bits have to be found first, by clusters
-//                  that the hardware puts on half of the SMs: 28 us for 512 tokens and 94 MB)
+//   k_embed_zeros  meanwhile zeros into all of dw (into the rows that no token has alone: they have to be found first, which every CTA for its own rows takes 41 us for 65,536
+//                  tokens where the zeros take 31, clusters that share the looking, and that the hardware puts on half of the SMs, 28 us for 512 tokens where this takes 15)
 //   k_embed_sums   `length` sorted entries a group of threads, up to eight rows of dout in flight: runs of one token within are written, as are those that end in the next group;
 //                  what belongs to a longer run is left as a partial sum
 //   k_embed_joins  adds up the partial sums of the longer runs, which k_embed_sums has listed
@@ -125,7 +125,7 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool here)
 
 // Stable radix sort, least significant digit first, by one cluster: each warp owns a run of consecutive entries and counts its digits, the CTAs read
 // one another's counts through shared memory, and each warp's entries move to their places in order.  Entries live in global memory (L2) and come eight a lane at a time,
-// so that a pass over them waits for memory a few times only (one at a time: 36 us for 65,536 tokens, where this takes 13).
+// so that a pass over them waits for memory a few times only.  21 us for 65,536 tokens of a vocabulary of 30,522, hidden behind the zeros where the table is large.
 constexpr int kAhead = 8;
 struct SortShared { uint32_t counts[kSortWarps][kSortBins], total[kSortBins], base[kSortBins], warp_sums[kSortWarps]; };
 __device__ void embed_sort(const EmbedBackArgs& a, SortShared& s)
@@ -295,14 +295,10 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
     uint2 next[FLIGHT];
     float v[VECTOR ? 1 : FLIGHT][8];
     Eight<DT> raw[VECTOR ? FLIGHT : 1];
-    auto entry = [&](int64_t i) {
-        uint2 e = i < limit ? a.sorted[i] : make_uint2(vocab, 0);
-        if ((skips_left && e.x == left) || (i >= end && e.x != last)) e.x = vocab;
-        return e;
-    };
-    auto load = [&](int k, const uint2& e) {
-        key[k] = e.x;
-        if (e.x == vocab) return;
+    auto entry = [&](int64_t i) { return i < limit ? a.sorted[i] : make_uint2(vocab, 0); };
+    auto load = [&](int k, const uint2& e, int64_t i) {             // i: the entry's place (looked at here, so that nothing waits for an entry when it is asked for)
+        key[k] = (skips_left && e.x == left) || (i >= end && e.x != last) ? vocab : e.x;
+        if (key[k] == vocab) return;
         if constexpr (VECTOR) {
             raw[k] = load8<DT>(a.d, e.y * a.d_stride + columns.first);
         } else {
@@ -314,7 +310,7 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
     for (int k = 0; k < FLIGHT; ++k) next[k] = entry(begin + k);
 #pragma unroll
     for (int k = 0; k < FLIGHT; ++k) {
-        load(k, next[k]);
+        load(k, next[k], begin + k);
         next[k] = entry(begin + FLIGHT + k);
     }
     for (int64_t i0 = begin; i0 < limit; i0 += FLIGHT) {
@@ -339,7 +335,7 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
                     for (int j = 0; j < 8; ++j) sum[j] += one[j];
                 }
             }
-            load(k, next[k]);
+            load(k, next[k], i0 + FLIGHT + k);
             next[k] = entry(i0 + 2 * FLIGHT + k);
         }
     }
@@ -358,14 +354,10 @@ __global__ void __launch_bounds__(kStrips * 64, 2) k_embed_joins(EmbedBackArgs a
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t group = a.list[item / slices], c = (item % slices) * 256 + lane * 4;       // padded rows: whole groups of four
         const uint32_t run = a.sorted[(group + 1) * a.length].x;
-        int64_t low = group + 1, step = 1;                          // the last group that begins with the run: 32 probes at a time, first of the next groups
-        for (;;) {
-            const int64_t probe = low + ((threadIdx.x & 31) + 1) * step;
-            const uint32_t still = __ballot_sync(0xffffffffu, probe < a.groups && a.sorted[probe * a.length].x == run);
-            low += (still == 0xffffffffu ? 32 : __ffs(~still) - 1) * step;
-            if (still == 0xffffffffu) step *= 32;
-            else if (step == 1) break;
-            else step /= 32;
+        int64_t low = group + 1;                                    // the last group that begins with the run: as many probes as threads at a time
+        for (int more = kStrips * 64; more == kStrips * 64; low += more) {
+            const int64_t probe = low + 1 + threadIdx.x;
+            more = __syncthreads_count(probe < a.groups && a.sorted[probe * a.length].x == run);
         }
         const int64_t partials = low - group, share = (partials + kStrips - 1) / kStrips, first = group + 1 + strip * share, end = min(low + 1, first + share);
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);

@@ -36,7 +36,7 @@ def tokens_for(count, vocabulary, seed, kind=torch.int64, hot=0.3):
     return t.to(kind)
 
 
-EMBEDDINGS = [(1, 1, 1), (1, 30522, 64), (3, 7, 8), (31, 2, 65), (257, 300, 1000), (1000, 33, 1001), (4097, 70001, 24), (513, 255, 1032), (2048, 256, 136), (700, 65536, 4), (130, 40, 3333), (1024, 30, 72), (1025, 30, 72), (1100, 2000, 2600)]
+EMBEDDINGS = [(1, 1, 1), (1, 30522, 64), (3, 7, 8), (31, 2, 65), (257, 300, 1000), (1000, 33, 1001), (4097, 70001, 24), (513, 255, 1032), (2048, 256, 136), (700, 65536, 4), (130, 40, 3333), (1024, 30, 72), (1025, 30, 72), (1100, 2000, 2600), (3000, 5000, 200), (2000, 9000, 1001), (1500, 200000, 8)]
 
 
 @pytest.mark.parametrize("count,vocabulary,width", EMBEDDINGS)
