@@ -52,14 +52,11 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float* v)
     }
 }
 
-// All threads of the cluster's CTAs: what each wrote before (to global memory or to the others' shared memory) the others may read after.
-__device__ __forceinline__ void cluster_barrier()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Its two halves, the first without a release (which waits for the thread's stores to global memory, about a microsecond): for threads whose data no other CTA reads.
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+// The barrier of all threads of a cluster's CTAs, in two halves and whole: what each wrote before (to global memory or to the others' shared memory) the others may read after,
+// and what each read before has been read.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wait(); }
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 // The address in CTA `rank` of what this CTA has at shared-memory address `a`.
 __device__ __forceinline__ uint32_t cluster_address(uint32_t a, uint32_t rank)

@@ -46,7 +46,7 @@ struct Source {
 
 __device__ __forceinline__ float dropped(float x, uint32_t bits, const DropArgs& a) { return bits >= a.border ? x * a.scale : 0.0f; }
 
-// Rows of whole groups of eight on 16-byte boundaries (contiguous tensors: one row of any length): UNITS groups a thread, all loaded first.
+// Rows of whole groups of eight that load8 can read (contiguous tensors: one row of any length): UNITS groups a thread, all loaded first.
 // Bound by HBM: 16384 x 4096 bfloat16 with a residual moves at the rate of a copy, without one the 7 rounds cost about 3 %.
 template <int XT, int RT, bool RESIDUAL, int HT, int UNITS>
 __global__ void __launch_bounds__(256) k_dropout(DropArgs a)

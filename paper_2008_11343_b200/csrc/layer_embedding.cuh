@@ -26,7 +26,7 @@ struct EmbedArgs {
 
 // ------------------------------------------------------------------------------------------ lookup
 
-// out = round(scale * w[token]), by groups of eight elements (rows on 16-byte boundaries), UNITS groups a thread so that as many chains of
+// out = round(scale * w[token]), by groups of eight elements (rows that load8 can read), UNITS groups a thread so that as many chains of
 // token -> row are in flight.  Bound by HBM: the distinct rows once (repeats come from L2), the output once.
 template <int WT, int OT, int UNITS>
 __global__ void __launch_bounds__(256) k_embed(EmbedArgs a)
@@ -176,7 +176,7 @@ __device__ void embed_sort(const EmbedBackArgs& a, SortShared& s)
             }
         }
         const bool last = pass == a.passes - 1;
-        if (last) cluster_arrive_relaxed();                         // no CTA ends before all have read its counts
+        if (last) cluster_arrive();                                 // no CTA ends before all have read its counts
         uint32_t upto = all;                                        // digits in order: an inclusive scan over the CTA's first threads
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(512) k_embed_zeros(EmbedBackArgs a)
     wait_for_last_kernel();
 }
 
-// Columns of the groups of eight that a thread holds: consecutive where rows lie on 16-byte boundaries, else `lanes` apart.
+// Columns of the groups of eight that a thread holds: consecutive where load8 can read the rows, else `lanes` apart.
 template <int DT, bool VECTOR>
 struct Columns {
     int64_t first;
