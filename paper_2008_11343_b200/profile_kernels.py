@@ -150,8 +150,8 @@ def _operator_cases():
         table = tensor(vocabulary, width)
         return lambda: O.embedding_forward(t, table, 2.0), 8 * tokens + 2 * width * (len(t.unique()) + tokens)
 
-    def drop(rows, width, junction=True):
-        x, rng = tensor(rows, width), torch.tensor([1, 2], device="cuda")
+    def drop(rows, width, junction=True, pad=0):
+        x, rng = tensor(rows, width + pad)[:, :width], torch.tensor([1, 2], device="cuda")
         r = tensor(rows, width) if junction else None
         return lambda: O.dropout_forward(x, 0.1, rng, 0, r), rows * width * (6 if junction else 4)
 
@@ -166,7 +166,7 @@ def _operator_cases():
     return {
         "k_embed": lambda: lookup(65_536, 1024), "k_embed_few": lambda: lookup(512, 1024, back=True), "k_embed_sort": lambda: lookup(65_536, 1024, back=True),
         "k_embed_zeros": lambda: lookup(65_536, 1024, back=True), "k_embed_sums": lambda: lookup(65_536, 1024, back=True), "k_embed_joins": lambda: lookup(65_536, 1024, back=True),
-        "k_dropout": lambda: drop(8192, 4096, junction=False), "k_dropout_junction": lambda: drop(8192, 4096), "k_dropout_any": lambda: drop(8191, 4095),
+        "k_dropout": lambda: drop(8192, 4096, junction=False), "k_dropout_junction": lambda: drop(8192, 4096), "k_dropout_any": lambda: drop(8191, 4095, pad=1),
         "k_scan": lambda: scan(16, 2048, 2048), "k_scan_f32": lambda: scan(8, 2048, 2048, dtype=torch.float32), "k_scan_odd": lambda: scan(16, 2048, 2047), "k_scan_parts": lambda: scan(1, 32_768, 1024),
         "k_scan_back": lambda: scan(16, 2048, 2048, back=True), "k_scan_back_f32": lambda: scan(8, 2048, 2048, back=True, dtype=torch.float32),
         "k_tile_squares": lambda: gradients(False), "k_list_norm": lambda: gradients(False), "k_one_norm": lambda: gradients(False, 4), "k_scale_tiles": lambda: gradients(True),
