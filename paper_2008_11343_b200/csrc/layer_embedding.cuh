@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 
 // ------------------------------------------------------------------------------------------ gradient
 //
-// dw[v] = round(scale * sum of dout[i] over the i with tokens[i] = v), rows without a token 0.  Three kernels:
+// dw[v] = round(scale * sum of dout[i] over the i with tokens[i] = v), rows without a token 0.  Four kernels:
 //   k_embed_sort   one cluster of CTAs sorts (token, position) by token, positions in order
 //   k_embed_zeros  meanwhile zeros into all of dw (into the rows that no token has alone: they have to be found first, which every CTA for its own rows takes 41 us for 65,536
 //                  tokens where the zeros take 31, clusters that share the looking, and that the hardware puts on half of the SMs, 28 us for 512 tokens where this takes 15)
