@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
     // Rolling: as a row is added its place is loaded with the row FLIGHT entries on, whose entry came FLIGHT entries before that, so that FLIGHT rows are always in flight.
     uint32_t key[FLIGHT];                                           // of the rows in flight; `vocab`: none
     uint2 next[FLIGHT];
-    float v[VECTOR ? 1 : FLIGHT][8];
+    typename Element<DT>::T v[VECTOR ? 1 : FLIGHT][8];              // as loaded: a conversion would wait for its load
     Eight<DT> raw[VECTOR ? FLIGHT : 1];
     auto entry = [&](int64_t i) { return i < limit ? a.sorted[i] : make_uint2(vocab, 0); };
     auto load = [&](int k, const uint2& e, int64_t i) {             // i: the entry's place (looked at here, so that nothing waits for an entry when it is asked for)
@@ -304,7 +304,8 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
             raw[k] = load8<DT>(a.d, e.y * a.d_stride + columns.first);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = columns.at(j) < a.width ? load1<DT>(a.d, e.y * a.d_stride + columns.at(j)) : 0.0f;
+            for (int j = 0; j < 8; ++j)
+                if (columns.at(j) < a.width) v[k][j] = static_cast<const typename Element<DT>::T*>(a.d)[e.y * a.d_stride + columns.at(j)];
         }
     };
 #pragma unroll
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
                 if constexpr (VECTOR) values8<DT>(one, raw[k]);
                 else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) one[j] = v[k][j];
+                    for (int j = 0; j < 8; ++j) one[j] = columns.at(j) < a.width ? (float)v[k][j] : 0.0f;
                 }
                 if (key[k] != run) {
                     write(false);
