@@ -62,24 +62,42 @@ __global__ void __launch_bounds__(256) k_embed(EmbedArgs a)
     }
 }
 
-// Any width and alignment: a warp a row and 256 columns of it at a time, eight elements a lane.
-template <int WT, int OT>
+// Any width and alignment: a warp a row and 256 columns of it at a time, eight elements a lane; PAIRS: two at a time, where width and addresses are even.
+template <int WT, int OT, bool PAIRS>
 __global__ void __launch_bounds__(256) k_embed_any(EmbedArgs a)
 {
+    constexpr int EACH = PAIRS ? 2 : 1, N = 8 / EACH;
     const int lane = threadIdx.x & 31;
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < a.count; row += (int64_t)gridDim.x * 8) {
         const uint32_t from = a.tokens.row(row);
         const auto* w = static_cast<const typename Element<WT>::T*>(a.w) + from * a.w_stride;
-        for (int64_t c0 = lane; c0 < a.width; c0 += 256) {
-            float v[8] = {};
+        auto* out = static_cast<typename Element<OT>::T*>(a.out) + row * a.width;
+        for (int64_t c0 = lane * EACH; c0 < a.width; c0 += 256) {
+            float2 v[N];
             if (from < a.tokens.vocab) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (c0 + k * 32 < a.width) v[k] = (float)w[c0 + k * 32] * a.scale;
+                for (int k = 0; k < N; ++k) {
+                    const int64_t c = c0 + k * 32 * EACH;
+                    v[k] = make_float2(0.0f, 0.0f);
+                    if (c >= a.width) continue;
+                    if constexpr (!PAIRS) v[k].x = (float)w[c];
+                    else if constexpr (WT == APMS_GRAD_F32) v[k] = *reinterpret_cast<const float2*>(w + c);
+                    else v[k] = unpack16<WT>(*reinterpret_cast<const uint32_t*>(w + c));
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] = make_float2(0.0f, 0.0f);
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c0 + k * 32 < a.width) store1<OT>(a.out, row * a.width + c0 + k * 32, v[k]);
+            for (int k = 0; k < N; ++k) {
+                const int64_t c = c0 + k * 32 * EACH;
+                if (c >= a.width) break;
+                const float2 s = make_float2(v[k].x * a.scale, v[k].y * a.scale);
+                if constexpr (!PAIRS) store1<OT>(out, c, from < a.tokens.vocab ? s.x : 0.0f);
+                else if (from >= a.tokens.vocab) *reinterpret_cast<std::conditional_t<OT == APMS_GRAD_F32, uint2, uint32_t>*>(out + c) = {};
+                else if constexpr (OT == APMS_GRAD_F32) *reinterpret_cast<float2*>(out + c) = s;
+                else *reinterpret_cast<uint32_t*>(out + c) = pack16<OT>(s);
+            }
         }
     }
 }
@@ -476,7 +494,10 @@ template <int WT, int OT>
 cudaError_t launch_embed(const EmbedArgs& a, bool vector, cudaStream_t stream)
 {
     const int64_t numel = a.count * a.width, units = numel / 8;
-    if (!vector) return launch(k_embed_any<WT, OT>, dim3((unsigned)std::min<int64_t>(1 << 20, (a.count + 7) / 8)), 256, 0, stream, false, a);
+    if (!vector) {
+        const bool pairs = a.width % 2 == 0 && a.w_stride % 2 == 0 && (uintptr_t)a.w % (2 * kBytes<WT>) == 0 && (uintptr_t)a.out % (2 * kBytes<OT>) == 0;
+        return launch(pairs ? k_embed_any<WT, OT, true> : k_embed_any<WT, OT, false>, dim3((unsigned)std::min<int64_t>(1 << 20, (a.count + 7) / 8)), 256, 0, stream, false, a);
+    }
     constexpr int MANY = WT == APMS_GRAD_F32 ? 2 : 4;
     if (units < (int64_t)1024 * 256 * MANY) return launch(k_embed<WT, OT, 1>, dim3((unsigned)((units + 255) / 256)), 256, 0, stream, false, a);
     return launch(k_embed<WT, OT, MANY>, dim3((unsigned)((units + 256 * MANY - 1) / (256 * MANY))), 256, 0, stream, false, a);

@@ -89,7 +89,7 @@ def test_values_that_are_not_finite_stay_in_their_rows():
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("width,pad,offset", [(64, 8, 0), (64, 3, 0), (64, 0, 1), (50, 6, 2), (33, 7, 8)])
+@pytest.mark.parametrize("width,pad,offset", [(64, 8, 0), (64, 3, 0), (64, 0, 1), (50, 6, 2), (33, 7, 8), (50, 0, 1), (550, 2, 0), (2, 0, 0)])
 def test_rows_anywhere(kind, width, pad, offset):
     tokens = tokens_for(500, 90, 8).view(20, 25)
     weight = normal((90, width), kind, seed=9, pad=pad, offset=offset)
