@@ -5,16 +5,17 @@
 namespace {
 
 // Per channel, with z = sigmoid(-gate) and a = 1 - z = sigmoid(gate):  h_t = a_t h_(t-1) + z_t x_t, so within a span of 8 steps: one dependent operation a step (h + z (x - h) has
-// two).  From span to span a state goes to h + (B + D h): B what the span makes of h = 0, -D = 1 - the product of its a, formed as a C + z.  What the rounding of a, 2^-25, forgets of a
-// state every step so adds up over a span at most, and a state that has reached its input stays there however long it is held.
+// two).  From span to span, with B what the span makes of h = 0, A the product of its a and C = 1 - A, formed as a C + z, a state goes to h + (B - C h) where the span keeps half of it or
+// more: what the rounding of a, 2^-25, forgets of a state every step so adds up over a span at most, and a state that has reached its input stays there however long it is held.  Where
+// the span forgets more than half, h + (B - C h) would leave the rounding of a state that is gone (2^-24 of it) in the one that is there; the state goes to B + A h.
 // Backward, with G_t the gradient of h_t and k what arrives from later steps:  G = dh + k,  dx = z G,  dgate = G (h_(t-1) - x) a z,  k = G - z G;  a span takes k to
 // B + A k.  The states come from `starts`, those that the forward pass had before every 8 steps, and x and gate again.
 //
 // A lane holds 8 bytes of channels (two pairs of 16-bit ones, one pair of binary32), a warp a slab of 256 bytes, over a span of 8 steps, whose operands fit into registers.
-// Eight warps lie one behind the other in time (in a short sequence fewer, and several slabs together): a round of the loop.  Per round each warp forms its span's (B, D),
+// Eight warps lie one behind the other in time (in a short sequence fewer, and several slabs together): a round of the loop.  Per round each warp forms its span's (B, A or C),
 // the first one takes the state through them, and each runs its steps from its own first state.  An SM holds two such teams: two CTAs, or, where there are too few slabs
 // for that, the two halves of one CTA that take turns at a slab's rounds; one team forms its spans (bound by the exponentials and reciprocals) while the other one finishes.
-// Where there are fewer slabs than SMs, a sequence is cut into segments, whose (B, D) a kernel of its own forms first; each segment then begins with the state behind those
+// Where there are fewer slabs than SMs, a sequence is cut into segments, whose (B, A or C) a kernel of its own forms first; each segment then begins with the state behind those
 // before it.  The operands come by asynchronous copies two rounds ahead, each warp its own.  Inputs are read once (before the last segment twice) and outputs written once.
 // 8 x 4096 x 2048 bfloat16: 70 to 74 us, 5.5 TB/s (in step, 16 warps: 86; clusters of two CTAs: 92; two channels a lane: 82); backward 119 to 125 us; 1 x 32,768 x 1024: 65 us (clusters of 16
 // CTAs that exchange every round: 135).  Bound by HBM where there are slabs for two teams an SM; else by the rounds, whose exponentials and reciprocals take a quarter to a half of the time.
@@ -30,9 +31,9 @@ struct ScanArgs {
     const float *state, *dlast;
     void *h, *dx, *dgate;
     float *last, *starts, *dstate;
-    float4* segments;                                               // (B, D) of the segments' pieces: [sequence and slab][segment][piece][pair][lane]
+    float4* segments;                                               // what the segments' pieces do to a state: [sequence and slab][segment][piece][pair][lane]
     int64_t slabs, starts_width;
-    int steps, spans, warps, parts, part_steps, pieces;             // warps in time of a team; segments, their steps, and what their (B, D) are formed in
+    int steps, spans, warps, parts, part_steps, pieces;             // warps in time of a team; segments, their steps, and the pieces that these are formed in
     int whole;                                                      // outputs can be written eight bytes at a time
 };
 
@@ -75,6 +76,7 @@ __device__ __forceinline__ void minus_taken_and_slope(float2 gate, float2& nz, f
     nz = make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
     az = mul2(mul2(e, nz), nz);
 }
+__device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
 __device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, both(-1.0f), a); }  // exact product: rounded as a difference
 
 __device__ __forceinline__ void copy_async16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory"); }
@@ -198,20 +200,39 @@ struct Place {
             if (2 * p + 1 < mine) to[state_at + 2 * p + 1] = v[p].y;
         }
     }
-    // Where the (B, D) of this slab's piece s lies.
+    // Where what this slab's piece s does to a state lies.
     __device__ __forceinline__ float4* piece(const ScanArgs& a, int s) const { return a.segments + ((slab * a.parts * a.pieces + s) * kPairs<TYPE>) * 32 + (threadIdx.x & 31); }
 };
 
-// One pair of channels over a span, and what it does to a state.
-struct Span { float2 b, c; };
-__device__ __forceinline__ Span span_of(const float4& v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
+// One pair of channels over a span, and what it does to a state.  Forward: to k h + (b + c h), with k = 1 and c = -C or k = 0 and c = A.  k is the sign of c (-0 where all is held).
+struct Span { float2 b, c, k; };
+__device__ __forceinline__ float kind(float c) { return __float_as_int(c) < 0 ? 1.0f : 0.0f; }
+__device__ __forceinline__ Span span_of(const float4& v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w), make_float2(kind(v.z), kind(v.w))}; }
 struct Forward {
-    static __device__ __forceinline__ float2 apply(const Span& s, float2 h) { return add2(h, fma2(s.c, h, s.b)); }
-    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {add2(e.b, fma2(l.c, e.b, l.b)), add2(fma2(l.c, e.c, e.c), l.c)}; }
+    static __device__ __forceinline__ float2 apply(const Span& s, float2 h) { return fma2(s.k, h, fma2(s.c, h, s.b)); }
+    // c and k of a span whose A and C are known.
+    static __device__ __forceinline__ void choose(Span& s, float2 product, float2 forgotten)
+    {
+        const bool x = forgotten.x > 0.5f, y = forgotten.y > 0.5f;
+        s.c = make_float2(x ? fabsf(product.x) : -forgotten.x, y ? fabsf(product.y) : -forgotten.y);
+        s.k = make_float2(x ? 0.0f : 1.0f, y ? 0.0f : 1.0f);
+    }
+    // c of two spans.
+    static __device__ __forceinline__ float both_of(float e, float l)
+    {
+        if (kind(e) == 0.0f || kind(l) == 0.0f) return (kind(e) + e) * (kind(l) + l);
+        const float c = fmaf(l, -e, -e) - l;
+        return c > 0.5f ? 1.0f - c : -c;                            // exact: 1 / 2 to 1 from 1
+    }
+    static __device__ __forceinline__ Span join(const Span& e, const Span& l)
+    {
+        const float2 c = make_float2(both_of(e.c.x, l.c.x), both_of(e.c.y, l.c.y));
+        return {apply(l, e.b), c, make_float2(kind(c.x), kind(c.y))};
+    }
 };
 struct Backward {
     static __device__ __forceinline__ float2 apply(const Span& s, float2 k) { return fma2(s.c, k, s.b); }
-    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {fma2(l.c, e.b, l.b), mul2(l.c, e.c)}; }
+    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {fma2(l.c, e.b, l.b), mul2(l.c, e.c), e.k}; }
 };
 
 // Barriers of a team's warps: the spans are there (all wait), the states are there (the warps that join them only arrive); and of two teams' first warps: the carried state is.
@@ -219,29 +240,37 @@ template <int THREADS> __device__ __forceinline__ void bar_arrive(int id) { asm 
 template <int THREADS> __device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(THREADS) : "memory"); }
 constexpr int kFormed = 1, kJoined = 3, kCarried = 5;               // + the team
 
-// Takes the state through a round's spans.  here: [pair][warp][lane], a span's (b, c), which becomes (the state that it begins with, .), from the group's first warp on.
+// A span's (b, c) as it lies in shared memory, [pair][warp][lane], and forward its k.
+template <class Way>
+__device__ __forceinline__ Span shared_span(const float4& v, const float2* kinds, int at)
+{
+    return {make_float2(v.x, v.y), make_float2(v.z, v.w), std::is_same<Way, Forward>::value ? kinds[at] : make_float2(0.0f, 0.0f)};
+}
+
+// Takes the state through a round's spans, which become (the state that they begin with, .), from the group's first warp on.
 template <int TYPE, class Way>
-__device__ __forceinline__ void join_spans(float2* carry, int warps, float4* here)
+__device__ __forceinline__ void join_spans(float2* carry, int warps, float4* here, const float2* kinds)
 {
     constexpr int P = kPairs<TYPE>;
     if (warps == kTeam) {
 #pragma unroll
         for (int w0 = 0; w0 < kTeam; w0 += 4) {                     // loads first: four spans at a time
-            float4 v[4][P];
+            Span v[4][P];
 #pragma unroll
-            for (int w = 0; w < 4 * P; ++w) v[w / P][w % P] = here[(w % P * kTeam + w0 + w / P) * 32];
+            for (int w = 0; w < 4 * P; ++w) { const int at = (w % P * kTeam + w0 + w / P) * 32; v[w / P][w % P] = shared_span<Way>(here[at], kinds, at); }
 #pragma unroll
             for (int w = 0; w < 4 * P; ++w) {
                 *reinterpret_cast<float2*>(here + (w % P * kTeam + w0 + w / P) * 32) = carry[w % P];
-                carry[w % P] = Way::apply(span_of(v[w / P][w % P]), carry[w % P]);
+                carry[w % P] = Way::apply(v[w / P][w % P], carry[w % P]);
             }
         }
     } else {
         for (int w = 0; w < warps; ++w)
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const Span s = span_of(here[(p * kTeam + w) * 32]);
-                *reinterpret_cast<float2*>(here + (p * kTeam + w) * 32) = carry[p];
+                const int at = (p * kTeam + w) * 32;
+                const Span s = shared_span<Way>(here[at], kinds, at);
+                *reinterpret_cast<float2*>(here + at) = carry[p];
                 carry[p] = Way::apply(s, carry[p]);
             }
     }
@@ -271,7 +300,7 @@ __device__ __forceinline__ void through_pieces(float2* carry, const float4* from
 
 // One round's join by the team's first warps in time: with two teams the carried state comes from and goes to the other one's.
 template <int TYPE, class Way, int TEAMS>
-__device__ __forceinline__ void join_round(float2* carry, int round, int rounds, int warps, float4* here, float2* carried)
+__device__ __forceinline__ void join_round(float2* carry, int round, int rounds, int warps, float4* here, const float2* kinds, float2* carried)
 {
     constexpr int P = kPairs<TYPE>;
     const int lane = threadIdx.x & 31;
@@ -280,7 +309,7 @@ __device__ __forceinline__ void join_round(float2* carry, int round, int rounds,
 #pragma unroll
         for (int p = 0; p < P; ++p) carry[p] = carried[p * 32 + lane];
     }
-    join_spans<TYPE, Way>(carry, warps, here);
+    join_spans<TYPE, Way>(carry, warps, here, kinds);
     if (TEAMS == 2 && round + 1 < rounds) {
 #pragma unroll
         for (int p = 0; p < P; ++p) carried[p * 32 + lane] = carry[p];
@@ -289,11 +318,14 @@ __device__ __forceinline__ void join_round(float2* carry, int round, int rounds,
 }
 
 // A warp's span in, the state that it begins with out.
-template <int TYPE>
-__device__ __forceinline__ void put_span(const Span* mine, float4* at)
+template <int TYPE, class Way>
+__device__ __forceinline__ void put_span(const Span* mine, float4* at, float2* kinds)
 {
 #pragma unroll
-    for (int p = 0; p < kPairs<TYPE>; ++p) at[p * kTeam * 32] = make_float4(mine[p].b.x, mine[p].b.y, mine[p].c.x, mine[p].c.y);
+    for (int p = 0; p < kPairs<TYPE>; ++p) {
+        at[p * kTeam * 32] = make_float4(mine[p].b.x, mine[p].b.y, mine[p].c.x, mine[p].c.y);
+        if (std::is_same<Way, Forward>::value) kinds[p * kTeam * 32] = mine[p].k;
+    }
 }
 template <int TYPE>
 __device__ __forceinline__ void get_state(float2* state, const float4* at)
@@ -302,19 +334,19 @@ __device__ __forceinline__ void get_state(float2* state, const float4* at)
     for (int p = 0; p < kPairs<TYPE>; ++p) state[p] = *reinterpret_cast<const float2*>(at + p * kTeam * 32);
 }
 
-// Shared memory: the rings, the teams' spans, the carried state.
+// Shared memory: the rings, the teams' spans, the carried state, forward the spans' kinds.
 template <int UNIT, int TENSORS> constexpr int kStageBytes = TENSORS * kSpanBytes<UNIT>;
 template <int UNIT, int TENSORS>
-constexpr size_t scan_shared(int teams, int pairs) { return (size_t)teams * kTeam * kStages * kStageBytes<UNIT, TENSORS> + (size_t)pairs * 32 * (teams * kTeam * sizeof(float4) + sizeof(float2)); }
+constexpr size_t scan_shared(int teams, int pairs) { return (size_t)teams * kTeam * kStages * kStageBytes<UNIT, TENSORS> + (size_t)pairs * 32 * (teams * kTeam * (sizeof(float4) + (TENSORS == 2 ? sizeof(float2) : 0)) + sizeof(float2)); }
 
-// The (B, D) of a span from its gates and x, and a and z x of each step; VALID of its steps exist.
+// What a span does to a state (also its A and C) from its gates and x, and a and z x of each step; VALID of its steps exist.
 template <int TYPE, int UNIT, bool WHOLE>
-__device__ __forceinline__ void form_span(Span* mine, float2 (*keep)[kPairs<TYPE>], float2 (*zx)[kPairs<TYPE>], const Feed<TYPE, UNIT>& x_feed, const Feed<TYPE, UNIT>& gate_feed, const ScanArgs& a,
-                                          uint32_t at, int valid)
+__device__ __forceinline__ void form_span(Span* mine, float2* product, float2* forgotten, float2 (*keep)[kPairs<TYPE>], float2 (*zx)[kPairs<TYPE>], const Feed<TYPE, UNIT>& x_feed,
+                                          const Feed<TYPE, UNIT>& gate_feed, const ScanArgs& a, uint32_t at, int valid)
 {
     constexpr int P = kPairs<TYPE>;
 #pragma unroll
-    for (int p = 0; p < P; ++p) mine[p].b = mine[p].c = both(0.0f);
+    for (int p = 0; p < P; ++p) mine[p].b = forgotten[p] = both(0.0f);
 #pragma unroll
     for (int s = 0; s < kSpan; ++s) {
         const uint2 g = gate_feed.words(at + kSpanBytes<UNIT>, s, a.gate), x = x_feed.words(at, s, a.x);
@@ -325,11 +357,12 @@ __device__ __forceinline__ void form_span(Span* mine, float2 (*keep)[kPairs<TYPE
             zx[s][p] = mul2(z, pair_of<TYPE>(x, p));
             if (!WHOLE && s >= valid) { keep[s][p] = both(1.0f); z = zx[s][p] = both(0.0f); }            // behind the sequence the state stays
             mine[p].b = fma2(keep[s][p], mine[p].b, zx[s][p]);
-            mine[p].c = fma2(keep[s][p], mine[p].c, z);
+            forgotten[p] = fma2(keep[s][p], forgotten[p], z);
+            product[p] = s ? mul2(product[p], keep[s][p]) : keep[s][p];
         }
     }
 #pragma unroll
-    for (int p = 0; p < P; ++p) mine[p].c = make_float2(-mine[p].c.x, -mine[p].c.y);
+    for (int p = 0; p < P; ++p) Forward::choose(mine[p], product[p], forgotten[p]);
 }
 
 template <int TYPE, int UNIT, int TEAMS>
@@ -341,6 +374,7 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan(ScanArgs
     char* ring = reinterpret_cast<char*>(room);
     float4* here = reinterpret_cast<float4*>(ring + TEAMS * kTeam * kStages * STAGE);
     float2* carried = reinterpret_cast<float2*>(here + TEAMS * P * kTeam * 32);
+    float2* kinds = carried + P * 32 + team * P * kTeam * 32 + warp * 32 + lane;
     here += team * P * kTeam * 32 + warp * 32 + lane;
     const Place<TYPE> me(a, warp);
     const uint32_t my_ring = shared_address(ring) + (threadIdx.x >> 5) * kStages * STAGE;
@@ -370,14 +404,14 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan(ScanArgs
         const uint32_t from = stage + lane * 8;
         copies_done<kStages - 1>();
         __syncwarp();
-        float2 keep[kSpan][P], zx[kSpan][P];
+        float2 keep[kSpan][P], zx[kSpan][P], product[P], forgotten[P];
         Span mine[P];
-        if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, keep, zx, x_feed, gate_feed, a, from, valid);
-        else form_span<TYPE, UNIT, false>(mine, keep, zx, x_feed, gate_feed, a, from, valid);
-        put_span<TYPE>(mine, here);
+        if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, product, forgotten, keep, zx, x_feed, gate_feed, a, from, valid);
+        else form_span<TYPE, UNIT, false>(mine, product, forgotten, keep, zx, x_feed, gate_feed, a, from, valid);
+        put_span<TYPE, Forward>(mine, here, kinds);
         bar_sync<kTeam * 32>(kFormed + team);
         if (me.in_time == 0) {
-            join_round<TYPE, Forward, TEAMS>(carry, round, rounds, a.warps, here, carried);
+            join_round<TYPE, Forward, TEAMS>(carry, round, rounds, a.warps, here, kinds, carried);
             bar_arrive<kTeam * 32>(kJoined + team);
         }
         x_feed.read(TEAMS * round_steps * a.x.step);
@@ -488,7 +522,7 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
         }
         Span mine[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f)};
+        for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f), both(0.0f)};
 #pragma unroll
         for (int s = kSpan - 1; s >= 0; --s) {
             const uint2 w = dh_feed.words(from + 2 * kSpanBytes<UNIT>, s, a.dh);
@@ -499,10 +533,10 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
                 mine[p].c = fma2(nz[s][p], mine[p].c, mine[p].c);
             }
         }
-        put_span<TYPE>(mine, here);
+        put_span<TYPE, Backward>(mine, here, nullptr);
         bar_sync<kTeam * 32>(kFormed + team);
         if (me.in_time == 0) {
-            join_round<TYPE, Backward, TEAMS>(carry, round, rounds, a.warps, here, carried);
+            join_round<TYPE, Backward, TEAMS>(carry, round, rounds, a.warps, here, nullptr, carried);
             bar_arrive<kTeam * 32>(kJoined + team);
         }
 #pragma unroll
@@ -588,8 +622,13 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
     for (int r = 0; r < STAGES; ++r) fetch(my_ring + r * STAGE);
     uint32_t stage = my_ring;
     Span all[P];
+    float2 all_product[P], all_forgotten[P];                        // forward
 #pragma unroll
-    for (int p = 0; p < P; ++p) all[p] = {both(0.0f), both(BACK ? 1.0f : 0.0f)};
+    for (int p = 0; p < P; ++p) {
+        all[p] = {both(0.0f), both(1.0f), both(0.0f)};
+        all_product[p] = both(1.0f);
+        all_forgotten[p] = both(0.0f);
+    }
     for (int i = 0; i < spans; ++i) {
         const int valid = a.steps - t;
         const uint32_t from = stage + lane * 8;
@@ -598,7 +637,7 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
         Span mine[P];
         if constexpr (BACK) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f)};
+            for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f), both(0.0f)};
 #pragma unroll
             for (int s = kSpan - 1; s >= 0; --s) {
                 const uint2 w = feed.words(from, s, one), g = gate_feed.words(from + kSpanBytes<UNIT>, s, a.gate);
@@ -610,13 +649,19 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
                     mine[p].c = fma2(nz, mine[p].c, mine[p].c);
                 }
             }
-        } else {
-            float2 keep[kSpan][P], zx[kSpan][P];
-            if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, keep, zx, feed, gate_feed, a, from, valid);
-            else form_span<TYPE, UNIT, false>(mine, keep, zx, feed, gate_feed, a, from, valid);
-        }
 #pragma unroll
-        for (int p = 0; p < P; ++p) all[p] = Way::join(all[p], mine[p]);
+            for (int p = 0; p < P; ++p) all[p] = Backward::join(all[p], mine[p]);
+        } else {
+            float2 keep[kSpan][P], zx[kSpan][P], product[P], forgotten[P];
+            if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, product, forgotten, keep, zx, feed, gate_feed, a, from, valid);
+            else form_span<TYPE, UNIT, false>(mine, product, forgotten, keep, zx, feed, gate_feed, a, from, valid);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                all[p].b = Forward::apply(mine[p], all[p].b);
+                all_product[p] = mul2(product[p], all_product[p]);
+                all_forgotten[p] = add2(forgotten[p], fma2(minus(forgotten[p]), all_forgotten[p], all_forgotten[p]));
+            }
+        }
         __syncwarp();                                               // all lanes have read the stage
         feed.read((BACK ? -kSpan : kSpan) * one.step);
         gate_feed.read((BACK ? -kSpan : kSpan) * a.gate.step);
@@ -624,6 +669,9 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
         stage = stage == my_ring + (STAGES - 1) * STAGE ? my_ring : stage + STAGE;
         t += BACK ? -kSpan : kSpan;
     }
+    if constexpr (!BACK)
+#pragma unroll
+        for (int p = 0; p < P; ++p) Forward::choose(all[p], all_product[p], all_forgotten[p]);
 #pragma unroll
     for (int p = 0; p < P; ++p) here[(warp * P + p) * 32] = make_float4(all[p].b.x, all[p].b.y, all[p].c.x, all[p].c.y);
     __syncthreads();
