@@ -164,6 +164,21 @@ __device__ __forceinline__ void store_lane(char* p, const float2* v, int mine)
     }
 }
 
+// A lane's channels with the other sign, rounded; WHOLE: all exist and can be written at once.
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ void store_minus(char* p, const float2* v, int mine)
+{
+    if constexpr (WHOLE) {
+        constexpr uint32_t SIGNS = TYPE == APMS_GRAD_F32 ? 0x80000000u : 0x80008000u;
+        const uint2 w = TYPE == APMS_GRAD_F32 ? make_uint2(__float_as_uint(v[0].x), __float_as_uint(v[0].y)) : make_uint2(pack16<TYPE>(v[0]), pack16<TYPE>(v[kPairs<TYPE> - 1]));
+        *reinterpret_cast<uint2*>(p) = make_uint2(w.x ^ SIGNS, w.y ^ SIGNS);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLaneChannels<TYPE>; ++i)
+            if (i < mine) store1<TYPE>(p, i, i & 1 ? -v[i / 2].y : -v[i / 2].x);
+    }
+}
+
 // Where a warp works: which sequence and slab, which segment.
 template <int TYPE>
 struct Place {
@@ -540,13 +555,15 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
             bar_arrive<kTeam * 32>(kJoined + team);
         }
 #pragma unroll
-        for (int s = 0; s < kSpan; ++s) {                           // az becomes (h_(t-1) - x_t) a z
+        for (int p = 0; p < P; ++p) start[p] = minus(start[p]);
+#pragma unroll
+        for (int s = 0; s < kSpan; ++s) {                           // az becomes (x_t - h_(t-1)) a z; the states, all with the other sign, as the forward pass formed them
             const uint2 w = x_feed.words(from, s, a.x);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const float2 d = sub2(start[p], pair_of<TYPE>(w, p));
-                start[p] = fma2(nz[s][p], d, start[p]);
-                az[s][p] = mul2(d, az[s][p]);
+                const float2 x = pair_of<TYPE>(w, p);
+                az[s][p] = mul2(add2(x, start[p]), az[s][p]);
+                start[p] = fma2(add2(nz[s][p], both(1.0f)), start[p], mul2(nz[s][p], x));
             }
         }
         fetch_start(t - TEAMS * round_steps);
@@ -563,13 +580,13 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
                         const float2 g = add2(pair_of<TYPE>(w, p), k[p]), nzg = mul2(nz[s][p], g);
-                        v[p] = make_float2(-nzg.x, -nzg.y);
+                        v[p] = nzg;
                         u[p] = mul2(g, az[s][p]);
                         k[p] = add2(g, nzg);
                     }
                     if (whole.value || s < valid) {
-                        store_lane<TYPE, whole.value>(dx, v, me.mine);
-                        store_lane<TYPE, whole.value>(dgate, u, me.mine);
+                        store_minus<TYPE, whole.value>(dx, v, me.mine);
+                        store_minus<TYPE, whole.value>(dgate, u, me.mine);
                     }
                     dx -= row;
                     dgate -= row;

@@ -107,3 +107,44 @@ def test_an_outlier_among_small_values(shape, kind):
     x[:, 5], x[:, t // 2] = 3e4, -3e4
     gate[:, 20:30] = float("inf")
     check(x, gate, states(b, d, kind, 1e6, 9))
+
+
+def gradient(dh, x, gate, state, dlast):
+    """((dx, error), (dgate, error), (dstate, error)).  G = dh + k rounds once; k = G - z G is off by z's error and two roundings of G, from span to span by 20 of itself; a z = e z z by
+    three errors of the exponential, two of z beside that and two roundings; h - x by the error of h and a rounding."""
+    z, a, units, exact = taken(gate)
+    _, _, _, _, before, before_error = scan(x, gate, state)
+    exponential = 6.0 if gate.dtype == F32 else 1.5 * gate.double().abs().clamp(max=1e4) + 4
+    x, dh = x.double(), dh.double()
+    az = a * z
+    k = dlast.double()
+    size, error = k.abs(), torch.zeros_like(k)
+    out = [[], [], [], []]
+    for t in reversed(range(x.shape[1])):
+        g, size = dh[:, t] + k, dh[:, t].abs() + size
+        error = error + U * size
+        zt, at, e = z[:, t], a[:, t], before[:, t] - x[:, t]
+        dgate = g * e * az[:, t]
+        relative = 3 * (exponential if gate.dtype == F32 else exponential[:, t]) + 8 + 3
+        for values, v in zip(out, (zt * g, 1.01 * zt * (error + size * (units[:, t] + 1) * U), dgate,
+                                   1.01 * (az[:, t] * (error * e.abs() + size * (before_error[:, t] + e.abs() * U)) + dgate.abs() * relative * U))):
+            values.append(v)
+        k, error, size = at * g, at * error + 1.01 * U * (~exact[:, t]).double() * size * (zt * units[:, t] + 2), at * size
+        if t % SPAN == 0:
+            error = error + 20 * U * size
+    dx, dx_error, dg, dg_error = (torch.stack(v[::-1], 1) for v in out)
+    return (dx, dx_error), (dg, dg_error), (k, error)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("low,high,at", [(-1.0, 6.0, 0), (-1.0, 6.0, 3), (-1.0, 6.0, 8), (-1.0, 6.0, -1), (-3.0, 0.0, None)])
+def test_gradients_behind_a_state_that_is_gone(shape, kind, low, high, at):
+    """The states that dgate takes are formed again, from the kept ones that may be as large as they like."""
+    b, t, d = shape
+    x, gate, state, dh, dlast = normal(shape, kind, seed=10), uniform(shape, low, high, kind, seed=11), states(b, d, kind, 1e8, 12), normal(shape, kind, 1e-2, seed=13), normal((b, d), F32, 1e-2, seed=14)
+    if at is not None:
+        gate[:, at] = gate[:, t // 2] = -float("inf")
+    starts = O.gated_scan_forward(x, gate, state, keep=True)[2]
+    for got, (want, error), name in zip(O.gated_scan_backward(dh, x, gate, starts, dlast), gradient(dh, x, gate, state, dlast), ("dx", "dgate", "dstate")):
+        oracle.within(got, want, error, name)
