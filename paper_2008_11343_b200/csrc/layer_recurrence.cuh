@@ -713,6 +713,10 @@ struct StepArgs {
     float* next;
 };
 
+// Where z is above 1/2 as a span's steps are formed: 1 - z is exact, and the rounding of x - h, 2^-24 of a state that is gone, stays out of the new one.  Below, h + z (x - h) forgets nothing
+// of a state to the rounding of 1 - z, however many tokens hold it.
+__device__ __forceinline__ float step_of(float z, float x, float h) { return z > 0.5f ? fmaf(1.0f - z, h, z * x) : fmaf(z, x - h, h); }
+
 // One token of each sequence against its state: eight channels a thread.  Latency: one launch.
 template <int TYPE>
 __global__ void __launch_bounds__(128) k_scan_step(StepArgs a)
@@ -727,7 +731,7 @@ __global__ void __launch_bounds__(128) k_scan_step(StepArgs a)
     values8<TYPE>(g, gr);
     values8<APMS_GRAD_F32>(h, hr);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = fmaf(taken<TYPE>(make_float2(g[j], 0.0f)).x, x[j] - h[j], h[j]);
+    for (int j = 0; j < 8; ++j) h[j] = step_of(taken<TYPE>(make_float2(g[j], 0.0f)).x, x[j], h[j]);
     store8<APMS_GRAD_F32>(a.next, u * 8, h);
     store8<TYPE>(a.h, u * 8, h);
 }
@@ -738,8 +742,7 @@ __global__ void __launch_bounds__(128) k_scan_step_any(StepArgs a)
     const int64_t i = (int64_t)blockIdx.x * 128 + threadIdx.x;
     if (i >= a.batch * a.width) return;
     const int64_t row = i / a.width, col = i - row * a.width;
-    const float before = a.state[i];
-    const float h = fmaf(taken<TYPE>(make_float2(load1<TYPE>(a.gate, row * a.gate_stride + col), 0.0f)).x, load1<TYPE>(a.x, row * a.x_stride + col) - before, before);
+    const float h = step_of(taken<TYPE>(make_float2(load1<TYPE>(a.gate, row * a.gate_stride + col), 0.0f)).x, load1<TYPE>(a.x, row * a.x_stride + col), a.state[i]);
     a.next[i] = h;
     store1<TYPE>(a.h, i, h);
 }

@@ -148,3 +148,19 @@ def test_gradients_behind_a_state_that_is_gone(shape, kind, low, high, at):
     starts = O.gated_scan_forward(x, gate, state, keep=True)[2]
     for got, (want, error), name in zip(O.gated_scan_backward(dh, x, gate, starts, dlast), gradient(dh, x, gate, state, dlast), ("dx", "dgate", "dstate")):
         oracle.within(got, want, error, name)
+
+
+@pytest.mark.parametrize("shape", [(3, 64), (5, 1001), (64, 1000)])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [1.0, 1e4, 1e8])
+def test_one_token_replaces_a_state_of_any_size(shape, kind, size):
+    """As a sequence of one step does; its sum h + z (x - h), where z is 1/2 or less, rounds x - h beside: z u |x - h|, within a u |h| + z u |x|."""
+    b, d = shape
+    x, gate, state = normal(shape, kind, 1e-2, seed=15), uniform(shape, -3.0, 6.0, kind, seed=16), states(b, d, kind, size, 17)
+    gate[:, ::3] = -float("inf")
+    want, error, _, _, _, _ = scan(x[:, None], gate[:, None], state)
+    out = torch.empty_like(state)
+    h = O.gated_scan_step(x, gate, state, out=out)
+    oracle.within(h, want[:, 0], error[:, 0])
+    oracle.within(out, want[:, 0], error[:, 0])
+    assert torch.equal(h[:, ::3], x[:, ::3]) and torch.equal(out[:, ::3], x[:, ::3].float())
