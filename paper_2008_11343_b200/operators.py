@@ -231,8 +231,8 @@ def gated_scan_step(x, gate, state, out=None):
 
 class _GatedScan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, gate, state):
-        keep = any(ctx.needs_input_grad)
+    def forward(ctx, x, gate, state, recorded):
+        keep = recorded and any(ctx.needs_input_grad)        # the latter are the inputs' own wishes, in every mode
         h, last, starts = gated_scan_forward(x, gate, state, keep)
         if keep:
             ctx.save_for_backward(x, gate, starts)
@@ -243,13 +243,13 @@ class _GatedScan(torch.autograd.Function):
     def backward(ctx, dh, dlast):
         x, gate, starts = ctx.saved_tensors
         if dh is None and dlast is None:
-            return None, None, None
+            return None, None, None, None
         if dh is None:
             dh = torch.zeros_like(x)
         dx, dgate, dstate = _derivative("gated_scan", gated_scan_backward, dh, x, gate, starts, dlast)
-        return dx, dgate, dstate if ctx.needs_input_grad[2] else None
+        return dx, dgate, dstate if ctx.needs_input_grad[2] else None, None
 
 
 def gated_scan(x, gate, state=None):
     """(h, last) of gated_scan_forward, differentiable in all three (once: a second derivative raises RuntimeError)."""
-    return _GatedScan.apply(x, gate, state)
+    return _GatedScan.apply(x, gate, state, torch.is_grad_enabled())
