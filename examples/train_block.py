@@ -9,7 +9,7 @@ residual junction (operators.rms_norm; with --eight-bit the matrix products read
 worker's gradients - bfloat16 matrices, binary32 norm weights - clipped by their global norm INTO that worker's flat binary32
 gradient (operators.TensorList.clip_grads), and one step of Algorithm 1 on the flat gradients (Context.step: Adam during
 warmup, the 1-bit compressed step after it).  The task is synthetic: the next token is a fixed affine map of the
-current one, with --sequence of the one before it.
+current one, with --sequence of the one before it (nothing is asked of a sequence's first one).
 """
 from __future__ import annotations
 
@@ -52,6 +52,13 @@ def shapes(vocab: int, width: int, layers: int, recurrent: bool = False):
     if recurrent:
         block = [(width,), (width, 2 * width), (width, width), *block]    # norm weight, values and gates, out
     return [(vocab, width), *(block * layers), (width,), (width, vocab)]
+
+
+def labels(tokens, vocab: int):
+    """What is to be predicted at each token; -100: nothing, which the loss leaves out."""
+    if tokens.dim() == 1:
+        return (tokens * 5 + 3) % vocab
+    return F.pad((tokens[:, :-1] * 5 + 3) % vocab, (1, 0), value=-100)
 
 
 def loss_of(leaves, tokens, targets, eight_bit: bool = False, dropout: float = 0.0, rng=None):
@@ -99,8 +106,7 @@ def train(steps: int = 60, workers: int = 4, vocab: int = 256, width: int = 192,
         step_losses, step_norms = [], []
         for i in range(workers):
             tokens = torch.randint(vocab, (batch // sequence, sequence) if sequence else (batch,), device="cuda", generator=gen)
-            known = tokens.roll(1, dims=-1) if sequence else tokens
-            loss = loss_of(leaves, tokens, (known * 5 + 3) % vocab, eight_bit, dropout, rngs[i])
+            loss = loss_of(leaves, tokens, labels(tokens, vocab), eight_bit, dropout, rngs[i])
             rngs[i][1] += 1
             grads = torch.autograd.grad(loss, leaves)
             if gradients is None:
