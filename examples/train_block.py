@@ -87,7 +87,9 @@ def loss_of(leaves, tokens, targets, eight_bit: bool = False, dropout: float = 0
 def train(steps: int = 60, workers: int = 4, vocab: int = 256, width: int = 192, layers: int = 3, batch: int = 512,
           warmup: int = 40, lr: float = 5e-3, max_norm: float = 1.0, eight_bit: bool = False, seed: int = 0, sequence: int = 0,
           dropout: float = 0.0):
-    """Mean loss over the workers and mean gradient norm before clipping, one of each per step."""
+    """Mean loss over the workers and mean gradient norm before clipping, one of each per step.  sequence: 0, or a divisor of batch above 1."""
+    if sequence and (sequence < 2 or batch % sequence):
+        raise ValueError(f"sequence must be 0 or a divisor of the batch of {batch} tokens above 1, not {sequence}")
     gen = torch.Generator(device="cuda").manual_seed(seed)
     sizes = shapes(vocab, width, layers, recurrent=sequence > 0)
     counts = [math.prod(s) for s in sizes]
@@ -127,7 +129,7 @@ def main():
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--workers", type=int, default=4)
     ap.add_argument("--eight-bit", action="store_true", help="the norms' 8-bit output feeds the matrix products")
-    ap.add_argument("--sequence", type=int, default=0, help="tokens come as sequences of this length (a divisor of 512), with a recurrence in front of each block")
+    ap.add_argument("--sequence", type=int, default=0, help="tokens come as sequences of this length (a divisor of 512 above 1), with a recurrence in front of each block")
     ap.add_argument("--dropout", type=float, default=0.0)
     args = ap.parse_args()
     losses, norms, phase, launches = train(steps=args.steps, workers=args.workers, eight_bit=args.eight_bit, sequence=args.sequence, dropout=args.dropout)
