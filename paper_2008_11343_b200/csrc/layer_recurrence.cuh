@@ -750,7 +750,9 @@ __global__ void __launch_bounds__(128) k_scan_step_any(StepArgs a)
 // ------------------------------------------------------------------------------------------ host
 
 // Warps in time: as many as the sequence has spans, up to a team.  Teams: two a CTA where the GPU's 148 SMs get no more than a slab each.  Segments: where they get fewer, as many as
-// fill the SMs, of 512 steps at least (below that the second kernel's launch costs more than it saves).  By the sizes alone, so that results are the same on every GPU.
+// fill the SMs, one for every 128 steps at most, so that a sequence of 257 is cut already: 8 slabs of 511 bfloat16 steps take 10.5 us (backward 12.5), whole 12.5 (18.6); of 1024
+// 10.6 (12.6), in segments of 512 at least 14.7 (20.4); of 257 9.0 (12.5) and 10.4 (12.9).  The one loss: the forward pass of 48 to 72 slabs of 257 to 384 steps, 12.5 us where a whole
+// sequence takes 10.4.  By the sizes alone, so that results are the same on every GPU.
 constexpr int kSms = 148, kLeastPart = 128;
 int plan_scan(ScanArgs& a, int64_t batch, int64_t steps, int64_t width, int type)
 {
