@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(512) k_embed_zeros(EmbedBackArgs a)
 }
 
 // Columns of the groups of eight that a thread holds: consecutive where load8 can read the rows, else `lanes` apart.
-template <int DT, bool VECTOR>
+template <bool VECTOR>
 struct Columns {
     int64_t first;
     int lanes;
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(128, 4) k_embed_sums(EmbedBackArgs a, int lane
     constexpr int FLIGHT = VECTOR && DT != APMS_GRAD_F32 ? 8 : 4;
     const int lane = threadIdx.x & (lanes - 1), per_cta = 128 / lanes;
     const int64_t group = (int64_t)blockIdx.x * per_cta + threadIdx.x / lanes;
-    const Columns<DT, VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
+    const Columns<VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
     wait_for_last_kernel();
     allow_next_kernel();
     if (group >= a.groups || columns.first >= a.width) return;
@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_embed_few(EmbedBackArgs a, i
         count += upto[w];
     }
     __syncthreads();
-    const Columns<DT, VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
+    const Columns<VECTOR> columns = {(int64_t)blockIdx.y * 8 * lanes + (VECTOR ? lane * 8 : lane), lanes};
     const int share = (count + strips - 1) / strips, begin = min(count, strip * share), end = min(count, begin + share);
     float sum[8] = {};
     if (columns.first < a.width) {
