@@ -219,35 +219,29 @@ struct Place {
     __device__ __forceinline__ float4* piece(const ScanArgs& a, int s) const { return a.segments + ((slab * a.parts * a.pieces + s) * kPairs<TYPE>) * 32 + (threadIdx.x & 31); }
 };
 
-// One pair of channels over a span, and what it does to a state.  Forward: to k h + (b + c h), with k = 1 and c = -C or k = 0 and c = A.  k is the sign of c (-0 where all is held).
-struct Span { float2 b, c, k; };
-__device__ __forceinline__ float kind(float c) { return __float_as_int(c) < 0 ? 1.0f : 0.0f; }
-__device__ __forceinline__ Span span_of(const float4& v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w), make_float2(kind(v.z), kind(v.w))}; }
+// One pair of channels over a span, and what it does to a state.  Forward: to h + (b + c h) with c = -C, or to b + c h with c = A: the sign of c says which (-0 where all is held).
+struct Span { float2 b, c; };
+__device__ __forceinline__ Span span_of(const float4& v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
 struct Forward {
-    static __device__ __forceinline__ float2 apply(const Span& s, float2 h) { return fma2(s.k, h, fma2(s.c, h, s.b)); }
-    // c and k of a span whose A and C are known.
-    static __device__ __forceinline__ void choose(Span& s, float2 product, float2 forgotten)
+    // What is added to b + c h: 1 or 0 times h.
+    static __device__ __forceinline__ float held(float c) { return __float_as_int(c) < 0 ? 1.0f : 0.0f; }
+    static __device__ __forceinline__ float2 apply(const Span& s, float2 h) { return fma2(make_float2(held(s.c.x), held(s.c.y)), h, fma2(s.c, h, s.b)); }
+    // c of a span whose A and C are known, and of two spans.
+    static __device__ __forceinline__ float2 choose(float2 product, float2 forgotten)
     {
-        const bool x = forgotten.x > 0.5f, y = forgotten.y > 0.5f;
-        s.c = make_float2(x ? fabsf(product.x) : -forgotten.x, y ? fabsf(product.y) : -forgotten.y);
-        s.k = make_float2(x ? 0.0f : 1.0f, y ? 0.0f : 1.0f);
+        return make_float2(forgotten.x > 0.5f ? fabsf(product.x) : -forgotten.x, forgotten.y > 0.5f ? fabsf(product.y) : -forgotten.y);
     }
-    // c of two spans.
     static __device__ __forceinline__ float both_of(float e, float l)
     {
-        if (kind(e) == 0.0f || kind(l) == 0.0f) return (kind(e) + e) * (kind(l) + l);
+        if (held(e) == 0.0f || held(l) == 0.0f) return (held(e) + e) * (held(l) + l);
         const float c = fmaf(l, -e, -e) - l;
         return c > 0.5f ? 1.0f - c : -c;                            // exact: 1 / 2 to 1 from 1
     }
-    static __device__ __forceinline__ Span join(const Span& e, const Span& l)
-    {
-        const float2 c = make_float2(both_of(e.c.x, l.c.x), both_of(e.c.y, l.c.y));
-        return {apply(l, e.b), c, make_float2(kind(c.x), kind(c.y))};
-    }
+    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {apply(l, e.b), make_float2(both_of(e.c.x, l.c.x), both_of(e.c.y, l.c.y))}; }
 };
 struct Backward {
     static __device__ __forceinline__ float2 apply(const Span& s, float2 k) { return fma2(s.c, k, s.b); }
-    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {fma2(l.c, e.b, l.b), mul2(l.c, e.c), e.k}; }
+    static __device__ __forceinline__ Span join(const Span& e, const Span& l) { return {fma2(l.c, e.b, l.b), mul2(l.c, e.c)}; }
 };
 
 // Barriers of a team's warps: the spans are there (all wait), the states are there (the warps that join them only arrive); and of two teams' first warps: the carried state is.
@@ -255,37 +249,29 @@ template <int THREADS> __device__ __forceinline__ void bar_arrive(int id) { asm 
 template <int THREADS> __device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(THREADS) : "memory"); }
 constexpr int kFormed = 1, kJoined = 3, kCarried = 5;               // + the team
 
-// A span's (b, c) as it lies in shared memory, [pair][warp][lane], and forward its k.
-template <class Way>
-__device__ __forceinline__ Span shared_span(const float4& v, const float2* kinds, int at)
-{
-    return {make_float2(v.x, v.y), make_float2(v.z, v.w), std::is_same<Way, Forward>::value ? kinds[at] : make_float2(0.0f, 0.0f)};
-}
-
-// Takes the state through a round's spans, which become (the state that they begin with, .), from the group's first warp on.
+// Takes the state through a round's spans.  here: [pair][warp][lane], a span's (b, c), which becomes (the state that it begins with, .), from the group's first warp on.
 template <int TYPE, class Way>
-__device__ __forceinline__ void join_spans(float2* carry, int warps, float4* here, const float2* kinds)
+__device__ __forceinline__ void join_spans(float2* carry, int warps, float4* here)
 {
     constexpr int P = kPairs<TYPE>;
     if (warps == kTeam) {
 #pragma unroll
         for (int w0 = 0; w0 < kTeam; w0 += 4) {                     // loads first: four spans at a time
-            Span v[4][P];
+            float4 v[4][P];
 #pragma unroll
-            for (int w = 0; w < 4 * P; ++w) { const int at = (w % P * kTeam + w0 + w / P) * 32; v[w / P][w % P] = shared_span<Way>(here[at], kinds, at); }
+            for (int w = 0; w < 4 * P; ++w) v[w / P][w % P] = here[(w % P * kTeam + w0 + w / P) * 32];
 #pragma unroll
             for (int w = 0; w < 4 * P; ++w) {
                 *reinterpret_cast<float2*>(here + (w % P * kTeam + w0 + w / P) * 32) = carry[w % P];
-                carry[w % P] = Way::apply(v[w / P][w % P], carry[w % P]);
+                carry[w % P] = Way::apply(span_of(v[w / P][w % P]), carry[w % P]);
             }
         }
     } else {
         for (int w = 0; w < warps; ++w)
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int at = (p * kTeam + w) * 32;
-                const Span s = shared_span<Way>(here[at], kinds, at);
-                *reinterpret_cast<float2*>(here + at) = carry[p];
+                const Span s = span_of(here[(p * kTeam + w) * 32]);
+                *reinterpret_cast<float2*>(here + (p * kTeam + w) * 32) = carry[p];
                 carry[p] = Way::apply(s, carry[p]);
             }
     }
@@ -315,7 +301,7 @@ __device__ __forceinline__ void through_pieces(float2* carry, const float4* from
 
 // One round's join by the team's first warps in time: with two teams the carried state comes from and goes to the other one's.
 template <int TYPE, class Way, int TEAMS>
-__device__ __forceinline__ void join_round(float2* carry, int round, int rounds, int warps, float4* here, const float2* kinds, float2* carried)
+__device__ __forceinline__ void join_round(float2* carry, int round, int rounds, int warps, float4* here, float2* carried)
 {
     constexpr int P = kPairs<TYPE>;
     const int lane = threadIdx.x & 31;
@@ -324,7 +310,7 @@ __device__ __forceinline__ void join_round(float2* carry, int round, int rounds,
 #pragma unroll
         for (int p = 0; p < P; ++p) carry[p] = carried[p * 32 + lane];
     }
-    join_spans<TYPE, Way>(carry, warps, here, kinds);
+    join_spans<TYPE, Way>(carry, warps, here);
     if (TEAMS == 2 && round + 1 < rounds) {
 #pragma unroll
         for (int p = 0; p < P; ++p) carried[p * 32 + lane] = carry[p];
@@ -333,14 +319,11 @@ __device__ __forceinline__ void join_round(float2* carry, int round, int rounds,
 }
 
 // A warp's span in, the state that it begins with out.
-template <int TYPE, class Way>
-__device__ __forceinline__ void put_span(const Span* mine, float4* at, float2* kinds)
+template <int TYPE>
+__device__ __forceinline__ void put_span(const Span* mine, float4* at)
 {
 #pragma unroll
-    for (int p = 0; p < kPairs<TYPE>; ++p) {
-        at[p * kTeam * 32] = make_float4(mine[p].b.x, mine[p].b.y, mine[p].c.x, mine[p].c.y);
-        if (std::is_same<Way, Forward>::value) kinds[p * kTeam * 32] = mine[p].k;
-    }
+    for (int p = 0; p < kPairs<TYPE>; ++p) at[p * kTeam * 32] = make_float4(mine[p].b.x, mine[p].b.y, mine[p].c.x, mine[p].c.y);
 }
 template <int TYPE>
 __device__ __forceinline__ void get_state(float2* state, const float4* at)
@@ -349,10 +332,10 @@ __device__ __forceinline__ void get_state(float2* state, const float4* at)
     for (int p = 0; p < kPairs<TYPE>; ++p) state[p] = *reinterpret_cast<const float2*>(at + p * kTeam * 32);
 }
 
-// Shared memory: the rings, the teams' spans, the carried state, forward the spans' kinds.
+// Shared memory: the rings, the teams' spans, the carried state.
 template <int UNIT, int TENSORS> constexpr int kStageBytes = TENSORS * kSpanBytes<UNIT>;
 template <int UNIT, int TENSORS>
-constexpr size_t scan_shared(int teams, int pairs) { return (size_t)teams * kTeam * kStages * kStageBytes<UNIT, TENSORS> + (size_t)pairs * 32 * (teams * kTeam * (sizeof(float4) + (TENSORS == 2 ? sizeof(float2) : 0)) + sizeof(float2)); }
+constexpr size_t scan_shared(int teams, int pairs) { return (size_t)teams * kTeam * kStages * kStageBytes<UNIT, TENSORS> + (size_t)pairs * 32 * (teams * kTeam * sizeof(float4) + sizeof(float2)); }
 
 // What a span does to a state (also its A and C) from its gates and x, and a and z x of each step; VALID of its steps exist.
 template <int TYPE, int UNIT, bool WHOLE>
@@ -377,7 +360,7 @@ __device__ __forceinline__ void form_span(Span* mine, float2* product, float2* f
         }
     }
 #pragma unroll
-    for (int p = 0; p < P; ++p) Forward::choose(mine[p], product[p], forgotten[p]);
+    for (int p = 0; p < P; ++p) mine[p].c = Forward::choose(product[p], forgotten[p]);
 }
 
 template <int TYPE, int UNIT, int TEAMS>
@@ -389,7 +372,6 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan(ScanArgs
     char* ring = reinterpret_cast<char*>(room);
     float4* here = reinterpret_cast<float4*>(ring + TEAMS * kTeam * kStages * STAGE);
     float2* carried = reinterpret_cast<float2*>(here + TEAMS * P * kTeam * 32);
-    float2* kinds = carried + P * 32 + team * P * kTeam * 32 + warp * 32 + lane;
     here += team * P * kTeam * 32 + warp * 32 + lane;
     const Place<TYPE> me(a, warp);
     const uint32_t my_ring = shared_address(ring) + (threadIdx.x >> 5) * kStages * STAGE;
@@ -423,10 +405,10 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan(ScanArgs
         Span mine[P];
         if (valid >= kSpan) form_span<TYPE, UNIT, true>(mine, product, forgotten, keep, zx, x_feed, gate_feed, a, from, valid);
         else form_span<TYPE, UNIT, false>(mine, product, forgotten, keep, zx, x_feed, gate_feed, a, from, valid);
-        put_span<TYPE, Forward>(mine, here, kinds);
+        put_span<TYPE>(mine, here);
         bar_sync<kTeam * 32>(kFormed + team);
         if (me.in_time == 0) {
-            join_round<TYPE, Forward, TEAMS>(carry, round, rounds, a.warps, here, kinds, carried);
+            join_round<TYPE, Forward, TEAMS>(carry, round, rounds, a.warps, here, carried);
             bar_arrive<kTeam * 32>(kJoined + team);
         }
         x_feed.read(TEAMS * round_steps * a.x.step);
@@ -537,7 +519,7 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
         }
         Span mine[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f), both(0.0f)};
+        for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f)};
 #pragma unroll
         for (int s = kSpan - 1; s >= 0; --s) {
             const uint2 w = dh_feed.words(from + 2 * kSpanBytes<UNIT>, s, a.dh);
@@ -548,10 +530,10 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
                 mine[p].c = fma2(nz[s][p], mine[p].c, mine[p].c);
             }
         }
-        put_span<TYPE, Backward>(mine, here, nullptr);
+        put_span<TYPE>(mine, here);
         bar_sync<kTeam * 32>(kFormed + team);
         if (me.in_time == 0) {
-            join_round<TYPE, Backward, TEAMS>(carry, round, rounds, a.warps, here, nullptr, carried);
+            join_round<TYPE, Backward, TEAMS>(carry, round, rounds, a.warps, here, carried);
             bar_arrive<kTeam * 32>(kJoined + team);
         }
 #pragma unroll
@@ -642,7 +624,7 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
     float2 all_product[P], all_forgotten[P];                        // forward
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        all[p] = {both(0.0f), both(1.0f), both(0.0f)};
+        all[p] = {both(0.0f), both(1.0f)};
         all_product[p] = both(1.0f);
         all_forgotten[p] = both(0.0f);
     }
@@ -654,7 +636,7 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
         Span mine[P];
         if constexpr (BACK) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f), both(0.0f)};
+            for (int p = 0; p < P; ++p) mine[p] = {both(0.0f), both(1.0f)};
 #pragma unroll
             for (int s = kSpan - 1; s >= 0; --s) {
                 const uint2 w = feed.words(from, s, one), g = gate_feed.words(from + kSpanBytes<UNIT>, s, a.gate);
@@ -688,7 +670,7 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
     }
     if constexpr (!BACK)
 #pragma unroll
-        for (int p = 0; p < P; ++p) Forward::choose(all[p], all_product[p], all_forgotten[p]);
+        for (int p = 0; p < P; ++p) all[p].c = Forward::choose(all_product[p], all_forgotten[p]);
 #pragma unroll
     for (int p = 0; p < P; ++p) here[(warp * P + p) * 32] = make_float4(all[p].b.x, all[p].b.y, all[p].c.x, all[p].c.y);
     __syncthreads();
