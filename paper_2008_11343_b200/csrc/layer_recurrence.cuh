@@ -164,21 +164,6 @@ __device__ __forceinline__ void store_lane(char* p, const float2* v, int mine)
     }
 }
 
-// A lane's channels with the other sign, rounded; WHOLE: all exist and can be written at once.
-template <int TYPE, bool WHOLE>
-__device__ __forceinline__ void store_minus(char* p, const float2* v, int mine)
-{
-    if constexpr (WHOLE) {
-        constexpr uint32_t SIGNS = TYPE == APMS_GRAD_F32 ? 0x80000000u : 0x80008000u;
-        const uint2 w = TYPE == APMS_GRAD_F32 ? make_uint2(__float_as_uint(v[0].x), __float_as_uint(v[0].y)) : make_uint2(pack16<TYPE>(v[0]), pack16<TYPE>(v[kPairs<TYPE> - 1]));
-        *reinterpret_cast<uint2*>(p) = make_uint2(w.x ^ SIGNS, w.y ^ SIGNS);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kLaneChannels<TYPE>; ++i)
-            if (i < mine) store1<TYPE>(p, i, i & 1 ? -v[i / 2].y : -v[i / 2].x);
-    }
-}
-
 // Where a warp works: which sequence and slab, which segment.
 template <int TYPE>
 struct Place {
@@ -486,6 +471,8 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
     uint32_t stage = my_ring;
     float2 carry[P];                                                // in the first warps in time
     me.load_state(carry, a.dlast);
+#pragma unroll
+    for (int p = 0; p < P; ++p) carry[p] = minus(carry[p]);         // with the other sign throughout: -G = -k - dh, dx = -z (-G), -k = -G + dx
     if (me.part < a.parts - 1 && me.in_time == 0 && team == 0) {
         wait_for_last_kernel();
         through_pieces<TYPE, Backward>(carry, me.piece(a, a.parts * a.pieces - 1), -P * 32, (a.parts - 1 - me.part) * a.pieces);
@@ -525,7 +512,7 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
             const uint2 w = dh_feed.words(from + 2 * kSpanBytes<UNIT>, s, a.dh);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const float2 g = add2(pair_of<TYPE>(w, p), mine[p].b);
+                const float2 g = sub2(mine[p].b, pair_of<TYPE>(w, p));
                 mine[p].b = fma2(nz[s][p], g, g);
                 mine[p].c = fma2(nz[s][p], mine[p].c, mine[p].c);
             }
@@ -539,13 +526,13 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
 #pragma unroll
         for (int p = 0; p < P; ++p) start[p] = minus(start[p]);
 #pragma unroll
-        for (int s = 0; s < kSpan; ++s) {                           // az becomes (x_t - h_(t-1)) a z; the states, all with the other sign, as the forward pass formed them
+        for (int s = 0; s < kSpan; ++s) {                           // az becomes (x_t - h_(t-1)) a z; -h goes to (-h - z (-h)) - z x: of an h that z = 1 replaces nothing is left
             const uint2 w = x_feed.words(from, s, a.x);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const float2 x = pair_of<TYPE>(w, p);
                 az[s][p] = mul2(add2(x, start[p]), az[s][p]);
-                start[p] = fma2(add2(nz[s][p], both(1.0f)), start[p], mul2(nz[s][p], x));
+                start[p] = fma2(nz[s][p], x, fma2(nz[s][p], start[p], start[p]));
             }
         }
         fetch_start(t - TEAMS * round_steps);
@@ -561,14 +548,14 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
                     float2 v[P], u[P];
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
-                        const float2 g = add2(pair_of<TYPE>(w, p), k[p]), nzg = mul2(nz[s][p], g);
-                        v[p] = nzg;
+                        const float2 g = sub2(k[p], pair_of<TYPE>(w, p));
+                        v[p] = mul2(nz[s][p], g);
                         u[p] = mul2(g, az[s][p]);
-                        k[p] = add2(g, nzg);
+                        k[p] = add2(g, v[p]);
                     }
                     if (whole.value || s < valid) {
-                        store_minus<TYPE, whole.value>(dx, v, me.mine);
-                        store_minus<TYPE, whole.value>(dgate, u, me.mine);
+                        store_lane<TYPE, whole.value>(dx, v, me.mine);
+                        store_lane<TYPE, whole.value>(dgate, u, me.mine);
                     }
                     dx -= row;
                     dgate -= row;
@@ -586,7 +573,11 @@ __global__ void __launch_bounds__(TEAMS * kTeam * 32, 2 / TEAMS) k_scan_back(Sca
         dgate_out -= TEAMS * round_steps * row;
         t -= TEAMS * round_steps;
     }
-    if (me.part == 0 && me.in_time == 0 && a.dstate && team == (rounds ? (rounds - 1) % TEAMS : 0)) me.store_state(a.dstate, carry);
+    if (me.part == 0 && me.in_time == 0 && a.dstate && team == (rounds ? (rounds - 1) % TEAMS : 0)) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) carry[p] = minus(carry[p]);
+        me.store_state(a.dstate, carry);
+    }
 }
 
 // What the segments but the last (backward: but the first) do to a state: a CTA takes a piece of a segment, each of its warps an eighth of that, joined at the end.
@@ -643,7 +634,7 @@ __global__ void __launch_bounds__(kPartWarps * 32, 2) k_scan_parts(ScanArgs a)
                 if (s >= valid) continue;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    const float2 z = taken<TYPE>(pair_of<TYPE>(g, p)), nz = make_float2(-z.x, -z.y), sum = add2(pair_of<TYPE>(w, p), mine[p].b);
+                    const float2 z = taken<TYPE>(pair_of<TYPE>(g, p)), nz = minus(z), sum = sub2(mine[p].b, pair_of<TYPE>(w, p));
                     mine[p].b = fma2(nz, sum, sum);
                     mine[p].c = fma2(nz, mine[p].c, mine[p].c);
                 }
