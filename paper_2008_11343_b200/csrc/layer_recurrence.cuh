@@ -9,7 +9,8 @@ namespace {
 // more: what the rounding of a, 2^-25, forgets of a state every step so adds up over a span at most, and a state that has reached its input stays there however long it is held.  Where
 // the span forgets more than half, h + (B - C h) would leave the rounding of a state that is gone (2^-24 of it) in the one that is there; the state goes to B + A h.
 // Backward, with G_t the gradient of h_t and k what arrives from later steps:  G = dh + k,  dx = z G,  dgate = G (h_(t-1) - x) a z,  k = G - z G;  a span takes k to
-// B + A k.  The states come from `starts`, those that the forward pass had before every 8 steps, and x and gate again.
+// B + A k.  A z below 2^-25 is lost there, as in binary32 at large: a gradient held over 10^5 such steps is off by some 10^-3.  The states come from `starts`, those that the forward pass
+// had before every 8 steps, and x and gate again, h - z h + z x: h - z (h - x) would leave the rounding of a state that is gone, too.
 //
 // A lane holds 8 bytes of channels (two pairs of 16-bit ones, one pair of binary32), a warp a slab of 256 bytes, over a span of 8 steps, whose operands fit into registers.
 // Eight warps lie one behind the other in time (in a short sequence fewer, and several slabs together): a round of the loop.  Per round each warp forms its span's (B, A or C),
@@ -17,8 +18,9 @@ namespace {
 // for that, the two halves of one CTA that take turns at a slab's rounds; one team forms its spans (bound by the exponentials and reciprocals) while the other one finishes.
 // Where there are fewer slabs than SMs, a sequence is cut into segments, whose (B, A or C) a kernel of its own forms first; each segment then begins with the state behind those
 // before it.  The operands come by asynchronous copies two rounds ahead, each warp its own.  Inputs are read once (before the last segment twice) and outputs written once.
-// 8 x 4096 x 2048 bfloat16: 70 to 74 us, 5.5 TB/s (in step, 16 warps: 86; clusters of two CTAs: 92; two channels a lane: 82); backward 119 to 125 us; 1 x 32,768 x 1024: 65 us (clusters of 16
-// CTAs that exchange every round: 135).  Bound by HBM where there are slabs for two teams an SM; else by the rounds, whose exponentials and reciprocals take a quarter to a half of the time.
+// 8 x 4096 x 2048 bfloat16: 69 us on the same inputs again, 73 to 76 on new ones, 5.3 TB/s (in step, 16 warps: 86; clusters of two CTAs: 92; two channels a lane: 82); backward 119, and
+// 127 to 132; 1 x 32,768 x 1024: 64 to 68 us (clusters of 16 CTAs that exchange every round: 135), backward 85.  With h + (B - C h) alone, and the states of the backward pass by
+// h - z (h - x): 69, 116, 62 and 84.  Bound by HBM where there are slabs for two teams an SM; else by the rounds, whose exponentials and reciprocals take a quarter to a half of the time.
 constexpr int kSpan = 8, kTeam = 8;                                 // steps; warps
 constexpr int kRowBytes = 256;
 constexpr int kStartsPad = 128;                                     // rows of starts: whole slabs of either type
@@ -88,7 +90,7 @@ __device__ __forceinline__ uint2 shared_words(uint32_t a) { uint2 v; asm volatil
 __device__ __forceinline__ uint32_t shared_word(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
 
 // What a warp fetches of one input: a span's rows of a slab a time, to shared memory.  UNIT: the bytes that rows are aligned to.  Rows of 16-bit elements that are
-// aligned to nothing more are copied by the aligned words that hold them, and shifted where they are read (8 x 4096 x 1001: 136 us; by plain loads of the elements 259).
+// aligned to nothing more are copied by the aligned words that hold them, and shifted where they are read (8 x 4096 x 1001: 132 us; by plain loads of the elements 259).
 template <int UNIT> constexpr int kPitch = kRowBytes + (UNIT == 2 ? 8 : 0);
 template <int UNIT> constexpr int kSpanBytes = kSpan * kPitch<UNIT>;
 template <int TYPE, int UNIT>
