@@ -1,5 +1,5 @@
 // Element types, sums and error reporting of the operators beside the step.
-// Part of libapms.so: included by operators.cu.
+// Part of libapms.so: included by operators.cu and layers.cu.
 #pragma once
 
 namespace {
